@@ -2,12 +2,14 @@
 
 The planner itself is the HIP library ``libtopoep.so`` behind the C ABI of
 ``include/topoep.h``; ``paper_2609_35481_amd.topoep`` is its thin binding.
-The binding is imported lazily so that ``paper_2609_35481_amd.build`` works
-before the library exists.
+The operators beside it (router, layer for a few tokens, gradient clip) are
+the same library's ``include/topoep_moe.h``, bound by
+``paper_2609_35481_amd.moe``.  The bindings are imported lazily so that
+``paper_2609_35481_amd.build`` works before the library exists.
 """
 import importlib
 
-__all__ = ["topoep", "build"]
+__all__ = ["topoep", "moe", "build"]
 
 
 def __getattr__(name):

@@ -1,0 +1,319 @@
+"""Thin Python binding of the operators beside the planner (include/topoep_moe.h).
+
+  route, route_backward   the router: top-k ids (what a planner takes) and
+                          weights of every token, and its gradient; route is
+                          differentiable where the logits ask for a gradient
+  moe_few                 a whole mixture-of-experts layer for up to 128 tokens
+  grad_norm, clip_grads   the global gradient norm over many tensors and the
+                          clip
+
+Argument checks and marshalling only: torch provides device memory and the
+current stream, every step runs in the HIP kernels of libtopoep.so.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+import functools
+
+import torch
+
+from .topoep import OK, TopoepError, _lib, _stream_ptr
+
+F32, BF16, F16 = 0, 1, 2
+SOFTMAX, SIGMOID = 0, 1
+MAX_EXPERTS = 1024
+MAX_TOPK = 64
+MAX_TOKENS = 128
+
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_SCORES = {"softmax": SOFTMAX, "sigmoid": SIGMOID}
+_ORDERS = {"2": 0, 2: 0, 2.0: 0, "inf": 1, float("inf"): 1}
+
+
+class Router(ctypes.Structure):
+    """topoep_router: E, k, expert groups, scores and the logits' type."""
+    _fields_ = [("num_experts", ctypes.c_int32), ("topk", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("top_groups", ctypes.c_int32), ("scoring", ctypes.c_int32), ("renorm", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class Moe(ctypes.Structure):
+    """topoep_moe: H, I, the experts whose weights are here, their type."""
+    _fields_ = [("hidden", ctypes.c_int32), ("inter", ctypes.c_int32), ("local_experts", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class Grad(ctypes.Structure):
+    """topoep_grad: one tensor of a gradient set."""
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32)]
+
+
+_vp, _i32, _i64, _f32, _size = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t)
+_PR, _PM, _PS = ctypes.POINTER(Router), ctypes.POINTER(Moe), ctypes.POINTER(_size)
+for _name, _args in (
+        ("topoep_route", [_PR, _vp, _i64, _i32, _vp, _vp, _vp, _vp]),
+        ("topoep_route_backward", [_PR, _vp, _i64, _i32, _vp, _vp, _vp, _i64, _vp]),
+        ("topoep_moe_workspace_bytes", [_PM, _PR, _i32, _PS]),
+        ("topoep_moe_few", [_PM, _PR, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _size, _vp]),
+        ("topoep_grads_workspace_bytes", [_i32, _PS]),
+        ("topoep_grad_norm", [_vp, _i32, _f32, _i32, _vp, _vp, _size, _vp]),
+        ("topoep_clip_grads", [_vp, _i32, _f32, _i32, _f32, _vp, _vp, _vp, _size, _vp])):
+    _fn = getattr(_lib, _name)
+    _fn.restype, _fn.argtypes = ctypes.c_int, _args
+
+EXPORTS = ("topoep_route", "topoep_route_backward", "topoep_moe_workspace_bytes", "topoep_moe_few",
+           "topoep_grads_workspace_bytes", "topoep_grad_norm", "topoep_clip_grads")
+
+
+@functools.lru_cache(maxsize=256)
+def router(E, k, dtype=torch.float32, scoring="softmax", renorm=True, scale=1.0, groups=1, top_groups=1) -> Router:
+    """The sizes and rules of a router (plain values, so one struct serves
+    every call that names the same)."""
+    if dtype not in _TYPES:
+        raise TypeError("logits must be float32, bfloat16 or float16, not %s" % dtype)
+    if scoring not in _SCORES:
+        raise ValueError("scoring is 'softmax' or 'sigmoid', not %r" % (scoring,))
+    return Router(E, k, groups, top_groups, _SCORES[scoring], int(bool(renorm)), _TYPES[dtype], scale)
+
+
+def _check(rc, name):
+    if rc != OK:
+        raise TopoepError(name, rc)
+
+
+def _rows(t, name):
+    """A CUDA matrix whose rows are dense."""
+    if not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % name)
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError("%s must be a matrix of dense rows that do not overlap" % name)
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def _dense(t, name, shape, dtype, device):
+    if t.dtype != dtype or t.device != device:
+        raise TypeError("%s must be %s on %s" % (name, dtype, device))
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be contiguous of shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    return t
+
+
+def _on(device):
+    """The library's calls go to the current device: the tensors' own."""
+    if torch.cuda.current_device() != device.index:
+        raise ValueError("the tensors are on %s, the current device is cuda:%d" % (device, torch.cuda.current_device()))
+
+
+def _on_stream(stream):
+    """What a call allocates belongs to the stream its kernels run on: one
+    named by the caller is made the current one for the call."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)))
+    return torch.cuda.stream(stream)
+
+
+def _route(r, logits, bias):
+    ld = _rows(logits, "logits")
+    T, E = logits.shape
+    dev = logits.device
+    _on(dev)
+    if bias is not None:
+        _dense(bias, "bias", (E,), torch.float32, dev)
+    ids = torch.empty((T, r.topk), dtype=torch.int32, device=dev)
+    weights = torch.empty((T, r.topk), dtype=torch.float32, device=dev)
+    _check(_lib.topoep_route(r, logits.data_ptr(), ld, T, bias.data_ptr() if bias is not None else None,
+                             ids.data_ptr(), weights.data_ptr(), _stream_ptr(None, dev)), "topoep_route")
+    return ids, weights
+
+
+def _backward(r, logits, ids, grad_weights):
+    ld = _rows(logits, "logits")
+    T, E = logits.shape
+    dev = logits.device
+    _on(dev)
+    _dense(ids, "ids", (T, r.topk), torch.int32, dev)
+    _dense(grad_weights, "grad_weights", (T, r.topk), torch.float32, dev)
+    out = torch.empty((T, E), dtype=logits.dtype, device=dev)
+    _check(_lib.topoep_route_backward(r, logits.data_ptr(), ld, T, ids.data_ptr(), grad_weights.data_ptr(),
+                                      out.data_ptr(), E, _stream_ptr(None, dev)), "topoep_route_backward")
+    return out
+
+
+class _Route(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, bias, r):
+        ids, weights = _route(r, logits, bias)
+        ctx.save_for_backward(logits, ids)
+        ctx.mark_non_differentiable(ids)
+        ctx.router = r
+        return ids, weights
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, _, grad_weights):
+        logits, ids = ctx.saved_tensors
+        return _backward(ctx.router, logits, ids, grad_weights.contiguous()), None, None
+
+
+def route(logits, k, scoring="softmax", renorm=True, scale=1.0, bias=None, groups=1, top_groups=1, stream=None):
+    """Enqueue topoep_route: (ids int32 [T, k], weights float32 [T, k]) of the
+    logits [T, E].  The ids are what a planner takes; the weights carry a
+    gradient to logits that require one (a bias gets none)."""
+    r = router(logits.shape[1] if logits.dim() == 2 else 0, k, logits.dtype, scoring, renorm, scale, groups,
+               top_groups)
+    with _on_stream(stream):
+        if torch.is_grad_enabled() and logits.requires_grad:
+            return _Route.apply(logits, bias, r)
+        return _route(r, logits, bias)
+
+
+def route_backward(logits, ids, grad_weights, scoring="softmax", renorm=True, scale=1.0, stream=None):
+    """Enqueue topoep_route_backward: the logits' gradient [T, E] in their
+    type from the weights' [T, k]."""
+    r = router(logits.shape[1] if logits.dim() == 2 else 0, ids.shape[1] if ids.dim() == 2 else 0, logits.dtype,
+               scoring, renorm, scale)
+    with _on_stream(stream):
+        return _backward(r, logits, ids, grad_weights)
+
+
+def moe_workspace_bytes(H, I, E, L, k, T, dtype=torch.bfloat16) -> int:
+    """Bytes of zero-filled workspace moe_few needs for T tokens or fewer."""
+    out = _size(0)
+    m = Moe(H, I, L, _TYPES.get(dtype, -1))
+    _check(_lib.topoep_moe_workspace_bytes(m, router(E, k), T, out), "topoep_moe_workspace_bytes")
+    return out.value
+
+
+def moe_few(x, gate, up, down, k, scoring="softmax", renorm=True, scale=1.0, bias=None, groups=1, top_groups=1,
+            expert_slot=None, workspace=None, stream=None):
+    """Enqueue topoep_moe_few: (out [T, H], ids int32 [T, k], weights float32
+    [T, k]) of the tokens x [T, H], at most 128, through a layer with the
+    router gate [E, H] and the experts up [L, 2I, H] (gate rows, then up rows)
+    and down [L, H, I], bfloat16 or float16.  expert_slot [E] says where an
+    expert lies among the L here (-1: elsewhere; it adds nothing).
+
+    workspace: a zero-filled byte tensor kept between calls
+    (moe_workspace_bytes; any larger one serves too); None makes one for the call."""
+    with _on_stream(stream):
+        return _few(x, gate, up, down, k, (scoring, renorm, scale, groups, top_groups), bias, expert_slot, workspace)
+
+
+def _few(x, gate, up, down, k, rules, bias, expert_slot, workspace):
+    ldx = _rows(x, "x")
+    dev, dtype = x.device, x.dtype
+    _on(dev)
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("x must be bfloat16 or float16, not %s" % dtype)
+    T, H = x.shape
+    if gate.dim() != 2 or up.dim() != 3 or down.dim() != 3:
+        raise ValueError("gate is [E, H], up [L, 2I, H], down [L, H, I]")
+    E, (L, _, I) = gate.shape[0], down.shape
+    _dense(gate, "gate", (E, H), dtype, dev)
+    _dense(up, "up", (L, 2 * I, H), dtype, dev)
+    _dense(down, "down", (L, H, I), dtype, dev)
+    if bias is not None:
+        _dense(bias, "bias", (E,), torch.float32, dev)
+    if expert_slot is not None:
+        _dense(expert_slot, "expert_slot", (E,), torch.int32, dev)
+    r = router(E, k, torch.float32, *rules)
+    m = Moe(H, I, L, _TYPES[dtype])
+    if workspace is None:
+        workspace = torch.zeros(moe_workspace_bytes(H, I, E, L, k, T, dtype) + 256, dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous on %s" % dev)
+    ws = (workspace.data_ptr() + 255) & ~255
+    size = workspace.numel() * workspace.element_size() - (ws - workspace.data_ptr())
+    out = torch.empty((T, H), dtype=dtype, device=dev)
+    ids = torch.empty((T, k), dtype=torch.int32, device=dev)
+    weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    _check(_lib.topoep_moe_few(m, r, x.data_ptr(), ldx, T, gate.data_ptr(),
+                               bias.data_ptr() if bias is not None else None,
+                               expert_slot.data_ptr() if expert_slot is not None else None, up.data_ptr(),
+                               down.data_ptr(), out.data_ptr(), ids.data_ptr(), weights.data_ptr(), ws, max(size, 0),
+                               _stream_ptr(None, dev)), "topoep_moe_few")
+    return out, ids, weights
+
+
+def _dense_any_order(t):
+    """Dense memory in whatever order of axes, each element once."""
+    if t.is_contiguous():
+        return True
+    size = 1
+    for n, s in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n != 1), key=lambda v: v[1]):
+        if s != size:
+            return False
+        size *= n
+    return True
+
+
+def _grad_set(grads, outs):
+    n = len(grads)
+    table = (Grad * n)()
+    device = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+    for i, g in enumerate(grads):
+        o = g if outs is None else outs[i]
+        for t in (g, o):
+            if not t.is_cuda or t.device != device:
+                raise ValueError("tensor %d is on %s, not %s" % (i, t.device, device))
+            if t.dtype not in _TYPES:
+                raise TypeError("tensor %d is %s, not float32, bfloat16 or float16" % (i, t.dtype))
+        if not _dense_any_order(g) or (o is not g and (o.shape != g.shape or o.stride() != g.stride())):
+            raise ValueError("tensor %d must be dense, and its output of the same shape and strides" % i)
+        table[i] = (g.data_ptr(), o.data_ptr(), g.numel(), _TYPES[g.dtype], _TYPES[o.dtype])
+    _on(device)
+    return table, n, device
+
+
+def _order(ord):
+    if ord not in _ORDERS:
+        raise ValueError("ord is 2 or inf, not %r" % (ord,))
+    return _ORDERS[ord]
+
+
+@functools.lru_cache(maxsize=64)
+def grads_workspace_bytes(count) -> int:
+    out = _size(0)
+    _check(_lib.topoep_grads_workspace_bytes(count, out), "topoep_grads_workspace_bytes")
+    return out.value
+
+
+def _grads_workspace(count, device):
+    ws = torch.empty(grads_workspace_bytes(count) + 256, dtype=torch.uint8, device=device)
+    return ws, (ws.data_ptr() + 255) & ~255
+
+
+def grad_norm(grads, scale=1.0, ord=2, stream=None):
+    """Enqueue topoep_grad_norm: scale times the 2-norm (or, with ord inf, the
+    largest magnitude) over a list of tensors, as a float32 scalar tensor."""
+    table, n, dev = _grad_set(grads, None)
+    with _on_stream(stream):
+        norm = torch.empty((), dtype=torch.float32, device=dev)
+        ws, ptr = _grads_workspace(n, dev)
+        _check(_lib.topoep_grad_norm(table, n, scale, _order(ord), norm.data_ptr(), ptr, grads_workspace_bytes(n),
+                                     _stream_ptr(None, dev)), "topoep_grad_norm")
+    return norm
+
+
+def clip_grads(grads, max_norm, scale=1.0, ord=2, outs=None, norm=None, stream=None):
+    """Enqueue topoep_clip_grads: every gradient times scale * min(1, max_norm /
+    (norm + 1e-6)), in place or into `outs` (same shapes and strides, any
+    of the three types); returns the norm.  norm: a given one (float32 scalar tensor,
+    already scaled), say of a whole group of ranks; None takes this set's.  A norm that
+    is not finite leaves every tensor as it is."""
+    if outs is not None and len(outs) != len(grads):
+        raise ValueError("%d outs for %d grads" % (len(outs), len(grads)))
+    table, n, dev = _grad_set(grads, outs)
+    if norm is not None:
+        _dense(norm, "norm", (), torch.float32, dev)
+    with _on_stream(stream):
+        total = torch.empty((), dtype=torch.float32, device=dev) if norm is None else norm
+        ws, ptr = _grads_workspace(n, dev)
+        _check(_lib.topoep_clip_grads(table, n, scale, _order(ord), max_norm,
+                                      norm.data_ptr() if norm is not None else None,
+                                      total.data_ptr() if norm is None else None, ptr, grads_workspace_bytes(n),
+                                      _stream_ptr(None, dev)), "topoep_clip_grads")
+    return total
