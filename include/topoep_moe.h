@@ -99,8 +99,8 @@ int topoep_route_backward(const topoep_router *r, const void *logits, int64_t ld
                           const float *grad_weights, void *grad_logits, int64_t ldg, void *stream);
 
 typedef struct topoep_moe {
-  int32_t hidden;        /* H, a multiple of 8                                       */
-  int32_t inter;         /* I, a multiple of 8                                       */
+  int32_t hidden;        /* H, a multiple of 8, at most 2^17                         */
+  int32_t inter;         /* I, a multiple of 8, at most 2^17; H I <= 2^30            */
   int32_t local_experts; /* L >= 1 experts whose weights are here                    */
   int32_t dtype;         /* of x, the weights and out: TOPOEP_BF16 or TOPOEP_F16     */
 } topoep_moe;
@@ -118,8 +118,8 @@ int topoep_moe_workspace_bytes(const topoep_moe *m, const topoep_router *r, int3
  *   h_j   = silu(up[s_j][0:I] x_t) * (up[s_j][I:2I] x_t)
  *   out_t = sum_{j: s_j >= 0} w_j down[s_j] h_j
  *
- *   x            device [T, H], row t at x + t * ldx elements (ldx >= H, a
- *                multiple of 8), 16-byte aligned, as are the weights and out
+ *   x            device [T, H], row t at x + t * ldx elements (H <= ldx < 2^24,
+ *                a multiple of 8), 16-byte aligned, as are the weights and out
  *   gate         device [E, H]
  *   bias         device float [E] or NULL, as topoep_route
  *   expert_slot  device int32 [E] or NULL: where each expert's weights lie in

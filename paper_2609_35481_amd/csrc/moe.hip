@@ -27,7 +27,6 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
 constexpr int kTile = 16;                       // rows and columns of a matrix tile
-constexpr int kMaxCols = TOPOEP_MOE_MAX_TOKENS / kTile;
 
 // D += A B on 16 rows, 16 columns and 32 of the inner axis: lane l holds 8
 // inner elements from (l / 16) * 8 of row (column) l % 16, and of D the rows
@@ -40,24 +39,27 @@ template <> __device__ inline v4f mfma<F16>(v4i a, v4i b, v4f d) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), d, 0, 0, 0);
 }
 
-// Eight elements at p[k], zero where not ok.
-template <class T>
-__device__ inline v4i load8(const T *p, int k, bool ok) {
+// 16 bytes at base + at, zero where not ok.  The base is the workgroup's, the
+// place the lane's own 32-bit one, so that an address costs no arithmetic.
+__device__ inline v4i load16(const char *base, uint32_t at, bool ok) {
   v4i v = {0, 0, 0, 0};
-  if (ok) v = *reinterpret_cast<const v4i *>(p + k);
+  if (ok) v = *reinterpret_cast<const v4i *>(base + at);
   return v;
 }
 
-struct Lists {          // the pairs by expert, in the workspace
-  int32_t *active;      // [1] experts with pairs
-  int32_t *slot;        // [E] their weights' place
-  int32_t *begin;       // [E + 1] their first pair
-  int32_t *pairs;       // [T * k] pair t * k + j
+// The pairs (token, choice) by expert, in the workspace.  Waves append to
+// them in any order: an expert's pairs are columns of a product, each
+// computed by itself, and experts are taken in the order of their ids, so no
+// result depends on that order.
+struct Lists {
+  uint32_t *active;     // [E / 32 rounded up] bit e % 32 of word e / 32: expert e has pairs
+  int32_t *count;       // [E] its pairs
+  int32_t *pairs;       // [E, T] t * k + j
 };
 
 struct Layer {
   RouterArgs r;
-  int T, H, I, L, splits;
+  int T, H, I, L;
   const void *x;
   int64_t ldx;
   const void *gate;
@@ -67,45 +69,135 @@ struct Layer {
   void *out;
   int32_t *ids;
   float *weights;
-  float *logits;        // [splits, T, E]
+  float *logits;        // [kSplits, T, E]
   void *hidden;         // [T * k, I]
+  float *each;          // [T * k, H] what each pair's expert gives
   Lists lists;
 };
 
+// ---------------------------------------------------------------- products
+
+// How a matrix instruction's operands are laid over the weights.  P = 1: A
+// holds 16 rows, 32 elements of each (64 bytes a row and load).  P = 2 and 4:
+// A holds 16 / P rows, 32 P consecutive elements of each, a row of A being one
+// part of 32 (128 and 256 bytes a row and load), and B the same parts of 16 / P
+// columns; of D only the products of equal parts are kept.  Memory gives 16
+// rows of 64 bytes 5.0 to 6.2 TB/s, 4 rows of 256 bytes, read past the caches,
+// 7.0 (768 MB, rows of 4 to 28 KB), which the dropped products are cheap for:
+// a tile of 16 rows takes P A operands, so P times the instructions.
+template <int P>
+struct Parts {
+  static constexpr int kCols = kTile / P;    // rows of an A operand, columns of a B operand
+  static constexpr int kStep = 32 * P;       // elements of the inner axis
+  // This lane's place in its row of a step.
+  static __device__ int place() { return lane_id() % kTile / kCols * 32 + (lane_id() >> 4) * 8; }
+};
+
+// The inner axis is streamed in runs of S steps: loads of the next run are in
+// flight while this one is multiplied.  Rows and columns that do not exist
+// read an existing one instead (their products are dropped), so that no load
+// of a full run depends on a condition.
+template <class T, int P, int NA, int C, int S>
+struct Run {
+  v4i a[S][NA], b[S][C];
+  __device__ void load(const char *rows, const uint32_t (&row)[NA], const char *cols, const uint32_t (&col)[C]) {
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const v4i *p = reinterpret_cast<const v4i *>(rows + row[i] + Parts<P>::kStep * 2 * s);
+        a[s][i] = P > 1 ? __builtin_nontemporal_load(p) : *p;
+      }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int s = 0; s < S; ++s) b[s][c] = *reinterpret_cast<const v4i *>(cols + col[c] + Parts<P>::kStep * 2 * s);
+  }
+  __device__ void multiply(v4f (&d)[NA][C]) const {
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) d[i][c] = mfma<T>(a[s][i], b[s][c], d[i][c]);
+  }
+};
+
+// d += rows * columns over k in [0, n): runs `first`, first + every, ... of
+// this wave, from the `turn`-th of them on and round (tiles that run side by side
+// then read different places of their rows), and its share of the steps behind
+// the last run.  row, col: bytes from rows and cols to the lane's own place
+// (Parts::place()) of k = 0.
+template <class T, int P, int S, int NA, int C>
+__device__ inline void stream(const char *rows, const uint32_t (&row)[NA], const char *cols, const uint32_t (&col)[C],
+                              int n, int first, int every, uint32_t turn, v4f (&d)[NA][C]) {
+  constexpr int kRun = Parts<P>::kStep * S;
+  const int full = n / kRun;
+  if (first < full) {
+    const int mine = (full - first + every - 1) / every, step = every * kRun, end = (first + mine * every) * kRun;
+    int k = (first + (int)(turn % (uint32_t)mine) * every) * kRun;
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+      Run<T, P, NA, C, S> x;
+      x.load(rows + k * 2, row, cols + k * 2, col);
+      k += step;
+      if (k >= end) k = first * kRun;
+      x.multiply(d);
+    }
+  }
+  // the rest, a step at a time: what lies behind the axis reads the row's start and counts as zero
+  const int place = Parts<P>::place();
+#pragma unroll 1
+  for (int k = full * kRun + first * Parts<P>::kStep; k < n; k += every * Parts<P>::kStep) {
+    const bool in = k + place < n;
+    const uint32_t at = in ? (uint32_t)k * 2u : 0u - (uint32_t)place * 2u;
+    const v4i zero = {0, 0, 0, 0};
+    v4i w[NA], b[C];
+#pragma unroll
+    for (int i = 0; i < NA; ++i) w[i] = *reinterpret_cast<const v4i *>(rows + (row[i] + at));
+#pragma unroll
+    for (int c = 0; c < C; ++c) b[c] = *reinterpret_cast<const v4i *>(cols + (col[c] + at));
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < NA; ++i) d[i][c] = mfma<T>(in ? w[i] : zero, in ? b[c] : zero, d[i][c]);
+  }
+}
+
 // ---------------------------------------------------------------- logits
 
-constexpr int kGateWaves = 4;
+constexpr int kGateWaves = 8;
+constexpr int kSplits = 8;   // parts of the hidden axis, each a workgroup's
 
 template <class T, int C>
 __global__ __launch_bounds__(64 * kGateWaves) void gate_kernel(Layer a) {
-  __shared__ v4f part[kGateWaves][C][64];
-  const int lane = lane_id(), wave = threadIdx.x >> 6, col = lane & 15, inner = (lane >> 4) * 8;
-  const int e = blockIdx.x * kTile + col;
-  const T *row = static_cast<const T *>(a.gate) + (int64_t)e * a.H;
-  v4f d[C] = {};
-  const int step = 32 * kGateWaves * a.splits;
-  for (int k = ((int)blockIdx.y * kGateWaves + wave) * 32 + inner; k - inner < a.H; k += step) {
-    const v4i w = load8(row, k, e < a.r.E && k < a.H);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int t = c * kTile + col;
-      d[c] = mfma<T>(w, load8(static_cast<const T *>(a.x) + t * a.ldx, k, t < a.T && k < a.H), d[c]);
+  __shared__ v4f part[kGateWaves][64];
+  if (blockIdx.x == 0 && blockIdx.y == 0)   // the routing kernel appends to these
+    for (int e = threadIdx.x; e < a.r.E; e += 64 * kGateWaves) {
+      a.lists.count[e] = 0;
+      if ((e & 31) == 0) a.lists.active[e >> 5] = 0;
     }
-  }
+  const int lane = lane_id(), wave = uniform_i32(threadIdx.x >> 6), col = lane & 15, inner = (lane >> 4) * 8;
+  const uint32_t row[1] = {((uint32_t)imin(blockIdx.x * kTile + col, a.r.E - 1) * a.H + inner) * 2u};
+  uint32_t src[C];
 #pragma unroll
-  for (int c = 0; c < C; ++c) part[wave][c][lane] = d[c];
-  __syncthreads();
-  for (int i = threadIdx.x; i < C * 64; i += 64 * kGateWaves) {
-    const int c = i >> 6, l = i & 63, t = c * kTile + (l & 15);
-    v4f s = part[0][c][l];
+  for (int c = 0; c < C; ++c) src[c] = ((uint32_t)imin(c * kTile + col, a.T - 1) * (uint32_t)a.ldx + inner) * 2u;
+  v4f d[1][C] = {};
+  stream<T, 1, 2>(static_cast<const char *>(a.gate), row, static_cast<const char *>(a.x), src, a.H, blockIdx.y * kGateWaves + wave, kSplits * kGateWaves, 0, d);
 #pragma unroll
-    for (int w = 1; w < kGateWaves; ++w) s += part[w][c][l];
-    if (t >= a.T) continue;
-    float *to = a.logits + ((int64_t)blockIdx.y * a.T + t) * a.r.E;
+  for (int c = 0; c < C; ++c) {
+    if (c > 0) __syncthreads();
+    part[wave][lane] = d[0][c];
+    __syncthreads();
+    const int l = threadIdx.x, t = c * kTile + (l & 15), e = blockIdx.x * kTile + (l >> 4) * 4;
+    if (l < 64 && t < a.T) {
+      v4f s = part[0][l];
 #pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) {
-      const int o = blockIdx.x * kTile + (l >> 4) * 4 + i4;
-      if (o < a.r.E) to[o] = s[i4];
+      for (int w = 1; w < kGateWaves; ++w) s += part[w][l];
+      float *to = a.logits + ((int64_t)blockIdx.y * a.T + t) * a.r.E + e;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (e + j < a.r.E) to[j] = s[j];
     }
   }
 }
@@ -118,223 +210,309 @@ __global__ __launch_bounds__(256) void few_route_kernel(Layer a) {
   const int wave = threadIdx.x >> 6, sub = lane_id();
   const int t = blockIdx.x * 4 + wave;
   const bool live = t < a.T;
+  const float *from = a.logits + (int64_t)(live ? t : 0) * a.r.E;
   float x[V], b[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int e = sub * V + v;
-    x[v] = -INFINITY;
-    b[v] = 0.0f;
-    if (e < a.r.E) {
-      float s = 0.0f;
-      for (int i = 0; i < a.splits; ++i) s += a.logits[((int64_t)i * a.T + (live ? t : 0)) * a.r.E + e];
-      x[v] = clean_logit(s);
-      if (a.bias) b[v] = a.bias[e];
-    }
+    const int e = imin(sub * V + v, a.r.E - 1);
+    float part[kSplits];
+#pragma unroll
+    for (int i = 0; i < kSplits; ++i) part[i] = from[(int64_t)i * a.T * a.r.E + e];
+    b[v] = a.bias ? a.bias[e] : 0.0f;
+    float s = part[0];
+#pragma unroll
+    for (int i = 1; i < kSplits; ++i) s += part[i];
+    x[v] = sub * V + v < a.r.E ? clean_logit(s) : -INFINITY;
   }
   route_row<64, V>(a.r, x, b, sub, scratch[wave], live, a.ids + (int64_t)t * a.r.k, a.weights + (int64_t)t * a.r.k);
+  if (live && sub < a.r.k) {
+    const int e = (int)scratch[wave][2 * sub], s = a.slot ? a.slot[e] : e;
+    if ((unsigned)s < (unsigned)a.L) {
+      const int at = atomicAdd(&a.lists.count[e], 1);
+      a.lists.pairs[(int64_t)e * a.T + at] = t * a.r.k + sub;
+      if (at == 0) atomicOr(&a.lists.active[e >> 5], 1u << (e & 31));
+    }
+  }
 }
 
-constexpr int kListThreads = 1024;
-
-__global__ __launch_bounds__(kListThreads) void few_lists_kernel(Layer a) {
-  __shared__ int count[TOPOEP_ROUTER_MAX_EXPERTS], first[TOPOEP_ROUTER_MAX_EXPERTS],
-      place[TOPOEP_ROUTER_MAX_EXPERTS], tmp[kListThreads / 64 + 1];
-  const int e = threadIdx.x, pairs = a.T * a.r.k;
-  count[e] = 0;
-  __syncthreads();
-  for (int p = threadIdx.x; p < pairs; p += kListThreads) {
-    const int id = a.ids[p], s = a.slot ? a.slot[id] : id;
-    if ((unsigned)s < (unsigned)a.L) atomicAdd(&count[id], 1);
-  }
-  __syncthreads();
-  const int n = count[e];
-  first[e] = n;
-  place[e] = n > 0;
-  __syncthreads();
-  const int total = block_excl_scan(first, TOPOEP_ROUTER_MAX_EXPERTS, tmp);
-  const int active = block_excl_scan(place, TOPOEP_ROUTER_MAX_EXPERTS, tmp);
-  if (n > 0) {
-    a.lists.slot[place[e]] = a.slot ? a.slot[e] : e;
-    a.lists.begin[place[e]] = first[e];
-  }
-  if (e == 0) {
-    a.lists.active[0] = active;
-    a.lists.begin[active] = total;
-  }
-  __syncthreads();
-  for (int p = threadIdx.x; p < pairs; p += kListThreads) {
-    const int id = a.ids[p], s = a.slot ? a.slot[id] : id;
-    if ((unsigned)s < (unsigned)a.L) a.lists.pairs[atomicAdd(&first[id], 1)] = p;
-  }
+// The n-th expert with pairs, by id; -1 where there are fewer.
+__device__ inline int nth_active(const Layer &a, int n) {
+  const int words = (a.r.E + 31) / 32;
+  const uint32_t w = lane_id() < words ? a.lists.active[lane_id()] : 0u;
+  const int ones = __popc(w), before = wave_incl_scan(ones) - ones;
+  const uint64_t has = __ballot(before <= n && n < before + ones);
+  if (has == 0) return -1;
+  const int l = __ffsll((unsigned long long)has) - 1;
+  uint32_t bits = (uint32_t)__builtin_amdgcn_readlane((int)w, l);
+  for (int skip = n - __builtin_amdgcn_readlane(before, l); skip > 0; --skip) bits &= bits - 1;
+  return l * 32 + __ffs((int)bits) - 1;
 }
 
 // ---------------------------------------------------------------- experts
 
-constexpr int kUpWaves = 4;
+template <class T> __device__ inline float saturate(float f) { return f; }
+template <> __device__ inline float saturate<F16>(float f) { return f > 65504.0f ? 65504.0f : f < -65504.0f ? -65504.0f : f; }
 
-// One wave's share of a tile of 16 gate and 16 up rows against C tiles of
-// columns, `src[c]` the lane's column (null: none).
-template <class T, int C>
-__device__ inline void up_tile(const T *gate, const T *up, bool row, const T *const (&src)[kMaxCols], int H, int wave,
-                               v4f (&g)[kMaxCols], v4f (&u)[kMaxCols]) {
-  const int inner = (lane_id() >> 4) * 8;
-#pragma unroll 4
-  for (int k = wave * 32 + inner; k - inner < H; k += 32 * kUpWaves) {
-    const bool in = k < H;
-    const v4i wg = load8(gate, k, row && in), wu = load8(up, k, row && in);
+constexpr int kExpertWaves = 4;
+
+// Steps of a run by P and C.
+constexpr int run_steps(int P, int C) { return P == 4 ? (C == 1 ? 2 : 1) : C <= 4 ? 2 : 1; }
+
+// A tile of 16 M rows of one expert against 16 / P * C of its pairs.  Rows: 8 M
+// hidden units' gate rows and their up rows (Up), or 16 M outputs.  KS = 1: the
+// tile is the wave's own; KS = kExpertWaves: the workgroup's waves share it, each
+// with its part of the runs.
+template <class T, bool Up, int P, int M, int C, int KS>
+__device__ inline void expert_tile(const Layer &a, const char *weights, const int32_t *pairs, int count, int tile,
+                                   v4f (*part)[64]) {
+  constexpr int R = Parts<P>::kCols, kRows = Up ? 8 * M : 16 * M, NA = P * M;
+  const int lane = lane_id(), wave = uniform_i32(threadIdx.x >> 6), place = Parts<P>::place(), at0 = tile * kRows;
+  const int n = Up ? a.H : a.I;
+  uint32_t row[NA], src[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const v4i b = load8(src[c], k, src[c] && in);
-      g[c] = mfma<T>(wg, b, g[c]);
-      u[c] = mfma<T>(wu, b, u[c]);
+  for (int i = 0; i < NA; ++i) {
+    const int r = i * R + lane % R;
+    row[i] = ((uint32_t)(Up ? r / (8 * M) * a.I + imin(at0 + r % (8 * M), a.I - 1) : imin(at0 + r, a.H - 1)) * n + place) * 2u;
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int at = c * R + lane % R, p = pairs[at < count ? at : 0];
+    src[c] = ((Up ? (uint32_t)(p / a.r.k) * (uint32_t)a.ldx : (uint32_t)p * (uint32_t)a.I) + place) * 2u;
+  }
+  const char *cols = static_cast<const char *>(Up ? a.x : a.hidden);
+  v4f d[NA][C] = {};
+  // eight tiles side by side run on eight XCDs
+  stream<T, P, run_steps(P, C)>(weights, row, cols, src, n, KS == 1 ? 0 : wave, KS, tile >> 3, d);
+  // this lane: rows q * 4 + 0..3 of part p, column `token` of part `of`
+  const int q = (lane >> 4) % (R / 4), p = (lane >> 4) / (R / 4), token = lane % R, of = lane % kTile / R;
+  constexpr int CE = C < 2 ? 1 : 2;   // columns' operands whose sums are joined at a time
+  v4f (*own)[64] = KS == 1 ? part + wave * CE * M : part;
+#pragma unroll
+  for (int c0 = 0; c0 < C; c0 += CE) {
+    if (KS == 1) wave_sync(); else __syncthreads();
+    if (p == of) {
+#pragma unroll
+      for (int c = 0; c < CE; ++c)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+          own[((KS == 1 ? 0 : wave * CE) + c) * M][((i * P + p) * (R / 4) + q) * R + token] = d[i][c0 + c];
+    }
+    if (KS == 1) wave_sync(); else __syncthreads();
+    const auto sum = [&](int c, int quad, int t) {   // rows quad * 4 + 0..3 of the tile
+      const v4f *from = &own[c * M][((quad * 4 / R * P) * (R / 4) + quad % (R / 4)) * R + t];
+      v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+      for (int i = 0; i < KS * P; ++i) s += from[i / P * CE * M * 64 + i % P * (R / 4) * R];
+      return s;
+    };
+    constexpr int kQuads = Up ? 2 * M : 4 * M;
+#pragma unroll 1
+    for (int o = KS == 1 ? lane : (int)threadIdx.x; o < CE * R * kQuads; o += KS * 64) {
+      const int quad = o % kQuads, t = o / kQuads % R, c = o / kQuads / R, at = at0 + quad * 4, n0 = (c0 + c) * R + t;
+      if (n0 >= count || at >= (Up ? a.I : a.H)) continue;
+      const int64_t pair = pairs[n0];
+      const v4f g = sum(c, quad, t);
+      if (Up) {
+        const v4f u = sum(c, quad + 2 * M, t);
+        T h[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[j] = from_float<T>(saturate<T>(g[j] * sigmoid(g[j]) * u[j]));
+        __builtin_memcpy(static_cast<T *>(a.hidden) + pair * a.I + at, h, sizeof(h));
+      } else {
+        *reinterpret_cast<v4f *>(a.each + pair * a.H + at) = g;
+      }
     }
   }
 }
 
-template <class T> __device__ inline float saturate(float f) { return f; }
-template <> __device__ inline float saturate<F16>(float f) { return f > 65504.0f ? 65504.0f : f < -65504.0f ? -65504.0f : f; }
+// How many pairs an expert has, about; any number is served by each.
+enum Load { kOne, kFew, kMany };   // at most 4; mostly up to 16; more
 
+template <int Kind> constexpr int tile_rows(bool up) { return (up ? 8 : 16) * (Kind == kMany ? 2 : 1); }
+
+// Workgroup b takes tile b % groups (KS = 1: its waves four tiles side by side) of
+// the experts b / groups, b / groups + gridDim / groups, ... of those with pairs.
+template <class T, bool Up, int KS, int Kind>
+__global__ __launch_bounds__(64 * kExpertWaves, Kind == kMany ? 3 : 4) void expert_kernel(Layer a, int groups) {
+  __shared__ v4f part[kExpertWaves * (Kind == kOne ? 1 : Kind == kFew ? 2 : 4)][64];
+  constexpr int kRows = tile_rows<Kind>(Up);
+  const int tiles = ((Up ? a.I : a.H) + kRows - 1) / kRows, group = (int)blockIdx.x % groups;
+  const int tile = KS == 1 ? group * kExpertWaves + uniform_i32(threadIdx.x >> 6) : group;
+  if (tile >= tiles) return;
+  for (int i = blockIdx.x / groups;; i += gridDim.x / groups) {
+    const int e = nth_active(a, i);
+    if (e < 0) return;
+    const int count = a.lists.count[e];
+    const int32_t *pairs = a.lists.pairs + (int64_t)e * a.T;
+    const int64_t slot = a.slot ? a.slot[e] : e;
+    const char *w = Up ? static_cast<const char *>(a.up) + slot * 4 * a.I * a.H
+                       : static_cast<const char *>(a.down) + slot * 2 * a.H * a.I;
+    if (Kind == kOne) {
+      expert_tile<T, Up, 4, 1, 1, KS>(a, w, pairs, count, tile, part);
+    } else if (Kind == kFew) {
+      if (count <= 4) expert_tile<T, Up, 4, 1, 1, KS>(a, w, pairs, count, tile, part);
+      else if (count <= 8) expert_tile<T, Up, 4, 1, 2, KS>(a, w, pairs, count, tile, part);
+      else
+        for (int at = 0; at < count; at += 16) expert_tile<T, Up, 2, 1, 2, KS>(a, w, pairs + at, count - at, tile, part);
+    } else {
+      if (count <= 16) expert_tile<T, Up, 1, 2, 1, KS>(a, w, pairs, count, tile, part);
+      else if (count <= 32) expert_tile<T, Up, 1, 2, 2, KS>(a, w, pairs, count, tile, part);
+      else
+        for (int at = 0; at < count; at += 64) expert_tile<T, Up, 1, 2, 4, KS>(a, w, pairs + at, count - at, tile, part);
+    }
+  }
+}
+
+// out_t = sum over t's choices in order, of those whose expert is here.
 template <class T>
-__global__ __launch_bounds__(64 * kUpWaves) void up_kernel(Layer a) {
-  __shared__ v4f part[kUpWaves][2][kMaxCols][64];
-  const int tiles = (a.I + kTile - 1) / kTile;
-  const int n = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-  if (n >= a.lists.active[0]) return;
-  const int lane = lane_id(), wave = threadIdx.x >> 6, col = lane & 15;
-  const int begin = a.lists.begin[n], count = a.lists.begin[n + 1] - begin;
-  const int i = tile * kTile + col;
-  const T *gate = static_cast<const T *>(a.up) + ((int64_t)a.lists.slot[n] * 2 * a.I + i) * a.H;
-  const T *up = gate + (int64_t)a.I * a.H;
-  const T *src[kMaxCols];
-  v4f g[kMaxCols] = {}, u[kMaxCols] = {};
-#pragma unroll
-  for (int c = 0; c < kMaxCols; ++c) {
-    const int at = c * kTile + col;
-    src[c] = at < count ? static_cast<const T *>(a.x) + a.lists.pairs[begin + at] / a.r.k * a.ldx : nullptr;
+__global__ __launch_bounds__(256) void combine_kernel(Layer a) {
+  const int t = blockIdx.y, h = (blockIdx.x * 256 + threadIdx.x) * 4, p0 = t * a.r.k;
+  int here = 0;
+  float weight = 0.0f;
+  if (lane_id() < a.r.k) {
+    const int e = a.ids[p0 + lane_id()], slot = a.slot ? a.slot[e] : e;
+    here = (unsigned)slot < (unsigned)a.L;
+    weight = a.weights[p0 + lane_id()];
   }
-  const int cols = (count + kTile - 1) / kTile;
-  if (cols <= 1) up_tile<T, 1>(gate, up, i < a.I, src, a.H, wave, g, u);
-  else if (cols <= 2) up_tile<T, 2>(gate, up, i < a.I, src, a.H, wave, g, u);
-  else if (cols <= 4) up_tile<T, 4>(gate, up, i < a.I, src, a.H, wave, g, u);
-  else up_tile<T, 8>(gate, up, i < a.I, src, a.H, wave, g, u);
+  const float *from = a.each + (int64_t)p0 * a.H + imin(h, a.H - 4);
+  v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (uint64_t left = __ballot(here); left != 0;) {
+    v4f v[8];
+    float w[8];
 #pragma unroll
-  for (int c = 0; c < kMaxCols; ++c)
-    if (c < cols) {
-      part[wave][0][c][lane] = g[c];
-      part[wave][1][c][lane] = u[c];
+    for (int i = 0; i < 8; ++i) {   // up to eight choices in flight; the rest repeat the last with weight zero
+      const int j = left != 0 ? __ffsll((unsigned long long)left) - 1 : -1;
+      w[i] = j < 0 ? 0.0f : __uint_as_float((uint32_t)readlane_i32((int)__float_as_uint(weight), j < 0 ? 0 : j));
+      if (j >= 0) v[i] = *reinterpret_cast<const v4f *>(from + (int64_t)j * a.H);
+      else v[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      left &= left - 1;
     }
-  __syncthreads();
-  for (int o = threadIdx.x; o < cols * 64; o += 64 * kUpWaves) {
-    const int c = o >> 6, l = o & 63, at = c * kTile + (l & 15), row = tile * kTile + (l >> 4) * 4;
-    v4f sg = part[0][0][c][l], su = part[0][1][c][l];
 #pragma unroll
-    for (int w = 1; w < kUpWaves; ++w) {
-      sg += part[w][0][c][l];
-      su += part[w][1][c][l];
-    }
-    if (at >= count || row >= a.I) continue;
-    T h[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) h[j] = from_float<T>(saturate<T>(sg[j] * sigmoid(sg[j]) * su[j]));
-    __builtin_memcpy(static_cast<T *>(a.hidden) + (int64_t)a.lists.pairs[begin + at] * a.I + row, h, sizeof(h));
+    for (int i = 0; i < 8; ++i) s += w[i] * v[i];
   }
+  if (h >= a.H) return;
+  T out[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) out[j] = from_float<T>(s[j]);
+  __builtin_memcpy(static_cast<T *>(a.out) + (int64_t)t * a.H + h, out, sizeof(out));
 }
 
 constexpr int kDownWaves = 8;
 
-template <class T, int C>
-__device__ inline void down_tile(const T *down, bool row, const T *const (&src)[kMaxCols], int lo, int hi,
-                                 v4f (&d)[kMaxCols]) {
-  const int inner = (lane_id() >> 4) * 8;
-#pragma unroll 4
-  for (int k = lo + inner; k - inner < hi; k += 32) {
-    const v4i w = load8(down, k, row && k < hi);
+// One unit of a wave: `len` of the inner axis from `lo` of one expert's pairs,
+// against the tile's 16 / P outputs.  The tile's rows are the outputs P times
+// over, each time against another P-th of the axis, and its columns the
+// tokens P times over, likewise; the products of one part's rows with another
+// part's columns are dropped.
+template <class T, int P, int C>
+__device__ inline void down_unit(const Layer &a, const char *weights, uint32_t row, const int32_t *pairs, int count, int lo, int len,
+                                 v4f *mine) {
+  constexpr int R = kTile / P;
+  const int lane = lane_id(), col = lane & 15, inner = (lane >> 4) * 8;
+  const int q = ((len + P - 1) / P + 7) & ~7;   // a part's length; the last may be shorter
+  uint32_t src[C];
+  int pair[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) d[c] = mfma<T>(w, load8(src[c], k, src[c] && k < hi), d[c]);
+  for (int c = 0; c < C; ++c) {
+    const int at = c * R + col % R;
+    pair[c] = pairs[at < count ? at : 0];
+    src[c] = ((uint32_t)pair[c] * (uint32_t)a.I + lo + col / R * q + inner) * 2u;
+    if (at >= count) pair[c] = -1;
   }
+  const char *cols = static_cast<const char *>(a.hidden);
+  const uint32_t rows[1] = {row + (lo + col / R * q + inner) * 2u};
+  v4f d[1][C] = {};
+  const int last = len - (P - 1) * q;   // may be negative for short axes
+  const int my = imin(q, len - col / R * q);
+  constexpr int S = C <= 2 ? 4 : 2;
+  const int safe = last > 0 ? last / (32 * S) * (32 * S) : 0;
+  stream<T, 1, S>(weights, rows, cols, src, safe, 0, 1, blockIdx.x / 8, d);
+  for (int k = safe; k < q; k += 32) {
+    const bool in = k + inner < my;
+#pragma unroll
+    for (int c = 0; c < C; ++c) d[0][c] = mfma<T>(load16(weights + k * 2, rows[0], in), load16(cols + k * 2, src[c], in), d[0][c]);
+  }
+  // column l % 16 of part col / R, rows (l / 16) * 4 + 0..3 of part (l / 16) * 4 / R
+  const bool keep = (lane >> 4) * 4 / R == col / R;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    if (keep && pair[c] >= 0) {
+      v4f *to = mine + pair[c] / a.r.k * 4 + (lane >> 4);
+      *to = *to + a.weights[pair[c]] * d[0][c];
+    }
 }
 
-template <class T>
+template <class T, int P, int MC>
 __global__ __launch_bounds__(64 * kDownWaves) void down_kernel(Layer a) {
-  extern __shared__ v4f sums[];   // [kDownWaves][T][4]: 16 outputs of every token, by wave
-  const int lane = lane_id(), wave = threadIdx.x >> 6, col = lane & 15;
+  extern __shared__ v4f sums[];   // [kDownWaves][T][4]: the 16 rows of every token, by wave
+  constexpr int R = kTile / P;
+  const int lane = lane_id(), wave = uniform_i32(threadIdx.x >> 6);
   const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i = threadIdx.x; i < kDownWaves * a.T * 4; i += 64 * kDownWaves) sums[i] = zero;
   __syncthreads();
-  const int active = a.lists.active[0];
-  // parts of I so that every wave has a unit
+  int active = lane < (a.r.E + 31) / 32 ? __popc(a.lists.active[lane]) : 0;
+  active = readlane_i32(wave_incl_scan(active), 63);
+  // parts of the axis so that every wave has a unit
   int parts = 1;
   while (parts < kDownWaves && active * parts < kDownWaves) parts *= 2;
   const int len = ((a.I + parts - 1) / parts + 31) & ~31;
-  const int o = blockIdx.x * kTile + col;
+  const int o = imin(blockIdx.x * R + (lane & 15) % R, a.H - 1);
   v4f *mine = sums + wave * a.T * 4;
   for (int unit = wave; unit < active * parts; unit += kDownWaves) {
-    const int n = unit / parts, lo = unit % parts * len, hi = lo + len < a.I ? lo + len : a.I;
-    const int begin = a.lists.begin[n], count = a.lists.begin[n + 1] - begin;
-    const T *down = static_cast<const T *>(a.down) + ((int64_t)a.lists.slot[n] * a.H + o) * a.I;
-    const T *src[kMaxCols];
-    int pair[kMaxCols];
-    v4f d[kMaxCols] = {};
-#pragma unroll
-    for (int c = 0; c < kMaxCols; ++c) {
-      const int at = c * kTile + col;
-      pair[c] = at < count ? a.lists.pairs[begin + at] : -1;
-      src[c] = at < count ? static_cast<const T *>(a.hidden) + (int64_t)pair[c] * a.I : nullptr;
+    const int e = nth_active(a, unit / parts), lo = unit % parts * len;
+    if (lo >= a.I) continue;
+    const int count = a.lists.count[e], m = imin(len, a.I - lo);
+    const int32_t *pairs = a.lists.pairs + (int64_t)e * a.T;
+    const char *w = static_cast<const char *>(a.down) + (int64_t)(a.slot ? a.slot[e] : e) * a.H * a.I * 2;
+    const uint32_t row = (uint32_t)o * (uint32_t)a.I * 2u;
+    for (int at = 0; at < count; at += MC * R) {
+      const int left = imin(count - at, MC * R), cols = (left + R - 1) / R;
+      if (MC == 1 || cols <= 1) down_unit<T, P, 1>(a, w, row, pairs + at, left, lo, m, mine);
+      else if (MC == 2 || cols <= 2) down_unit<T, P, MC < 2 ? 1 : 2>(a, w, row, pairs + at, left, lo, m, mine);
+      else down_unit<T, P, MC < 4 ? 1 : 4>(a, w, row, pairs + at, left, lo, m, mine);
     }
-    const int cols = (count + kTile - 1) / kTile;
-    if (cols <= 1) down_tile<T, 1>(down, o < a.H, src, lo, hi, d);
-    else if (cols <= 2) down_tile<T, 2>(down, o < a.H, src, lo, hi, d);
-    else if (cols <= 4) down_tile<T, 4>(down, o < a.H, src, lo, hi, d);
-    else down_tile<T, 8>(down, o < a.H, src, lo, hi, d);
-#pragma unroll
-    for (int c = 0; c < kMaxCols; ++c)
-      if (c < cols && pair[c] >= 0) {
-        v4f *to = mine + pair[c] / a.r.k * 4 + (lane >> 4);
-        *to = *to + a.weights[pair[c]] * d[c];
-      }
     wave_sync();
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < a.T * 4; i += 64 * kDownWaves) {
-    v4f s = sums[i];
+  for (int i = threadIdx.x; i < a.T * (R / 4); i += 64 * kDownWaves) {
+    const int t = i / (R / 4), at = i % (R / 4), row = blockIdx.x * R + at * 4;
+    v4f s = zero;
 #pragma unroll
-    for (int w = 1; w < kDownWaves; ++w) s += sums[w * a.T * 4 + i];
-    const int row = blockIdx.x * kTile + (i & 3) * 4;
+    for (int w = 0; w < kDownWaves; ++w)
+#pragma unroll
+      for (int p = 0; p < P; ++p) s += sums[(w * a.T + t) * 4 + p * (R / 4) + at];
     if (row >= a.H) continue;
     T out[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) out[j] = from_float<T>(s[j]);
-    __builtin_memcpy(static_cast<T *>(a.out) + (int64_t)(i >> 2) * a.H + row, out, sizeof(out));
+    __builtin_memcpy(static_cast<T *>(a.out) + (int64_t)t * a.H + row, out, sizeof(out));
   }
 }
 
 // ---------------------------------------------------------------- host
 
-int gate_splits(int E, int H) {
-  const int tiles = (E + kTile - 1) / kTile, most = (H + 32 * kGateWaves - 1) / (32 * kGateWaves);
-  int s = 1;
-  while (s < 8 && s * 2 <= most && tiles * s < 128) s *= 2;
-  return s;
-}
-
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-struct Parts {
-  size_t lists, pairs, logits, hidden, total;
+struct Places {
+  size_t active, count, pairs, logits, hidden, each, total;
 };
 
-Parts parts_of(const topoep_moe *m, const topoep_router *r, int T) {
-  Parts p;
+Places places_of(const topoep_moe *m, const topoep_router *r, int T) {
+  Places p;
   const size_t E = (size_t)r->num_experts, pairs = (size_t)T * r->topk;
-  size_t at = 256;   // control words
-  p.lists = at;
-  at += align256((2 * E + 2) * sizeof(int32_t));
+  size_t at = 0;
+  p.active = at;
+  at += align256((E + 31) / 32 * sizeof(uint32_t));
+  p.count = at;
+  at += align256(E * sizeof(int32_t));
   p.pairs = at;
-  at += align256(pairs * sizeof(int32_t));
+  at += align256(E * T * sizeof(int32_t));
   p.logits = at;
-  at += align256((size_t)gate_splits(r->num_experts, m->hidden) * T * E * sizeof(float));
+  at += align256(kSplits * T * E * sizeof(float));
   p.hidden = at;
   at += align256(pairs * m->inter * 2);
+  p.each = at;
+  at += align256(pairs * m->hidden * sizeof(float));
   p.total = at;
   return p;
 }
@@ -342,7 +520,8 @@ Parts parts_of(const topoep_moe *m, const topoep_router *r, int T) {
 int check_layer(const topoep_moe *m, const topoep_router *r, int32_t T) {
   if (!m || !r) return TOPOEP_EINVAL;
   if (m->hidden < 8 || (m->hidden & 7) || m->inter < 8 || (m->inter & 7) || m->local_experts < 1) return TOPOEP_EINVAL;
-  if (m->hidden > 1 << 20 || m->inter > 1 << 20) return TOPOEP_EINVAL;
+  // an expert's matrices, the tokens and the hidden rows are addressed by 32-bit byte offsets
+  if (m->hidden > 1 << 17 || m->inter > 1 << 17 || (int64_t)m->hidden * m->inter > 1 << 30) return TOPOEP_EINVAL;
   if (m->dtype != TOPOEP_BF16 && m->dtype != TOPOEP_F16) return TOPOEP_EINVAL;
   topoep_router own = *r;
   own.dtype = TOPOEP_F32;   // not read: the logits never leave 32 bits
@@ -356,11 +535,53 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 
 bool launched() { return hipGetLastError() == hipSuccess; }
 
+template <class T, bool Up, int Kind>
+int enqueue_experts(const Layer &a, hipStream_t st) {
+  const int rows = tile_rows<Kind>(Up), tiles = ((Up ? a.I : a.H) + rows - 1) / rows;
+  const int experts = imin(imin(a.T * a.r.k, a.r.E), a.L);   // with pairs, about
+  const dim3 block(64 * kExpertWaves);
+  // A wave to a tile where there are tiles for all of the chip's 4096 places, or
+  // for half of them and rows are short (62 against 66 us for 32 experts, H = 2048,
+  // I = 768); else the workgroup to a tile (two experts, H = 4096, I = 14336: 130
+  // against 169 us)
+  const int64_t all = (int64_t)experts * tiles;
+  if (all < 2048 || (all < 4096 && (Up ? a.H : a.I) > 2048)) {
+    hipLaunchKernelGGL((expert_kernel<T, Up, kExpertWaves, Kind>), dim3((unsigned)experts * tiles), block, 0, st, a, tiles);
+  } else {
+    const int groups = (tiles + kExpertWaves - 1) / kExpertWaves;
+    hipLaunchKernelGGL((expert_kernel<T, Up, 1, Kind>), dim3((unsigned)experts * groups), block, 0, st, a, groups);
+  }
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
+template <class T, bool Up>
+int enqueue_experts(const Layer &a, hipStream_t st) {
+  if (a.T <= 4) return enqueue_experts<T, Up, kOne>(a, st);
+  if (a.T * a.r.k <= 8 * a.r.E) return enqueue_experts<T, Up, kFew>(a, st);
+  return enqueue_experts<T, Up, kMany>(a, st);
+}
+
+template <class T, int P>
+int enqueue_down_parts(const Layer &a, int cols, hipStream_t st) {
+  const dim3 grid((a.H + kTile / P - 1) / (kTile / P)), block(64 * kDownWaves);
+  const size_t lds = kDownWaves * a.T * 4 * sizeof(v4f);
+  if (cols <= 1) hipLaunchKernelGGL((down_kernel<T, P, 1>), grid, block, lds, st, a);
+  else if (cols <= 2) hipLaunchKernelGGL((down_kernel<T, P, 2>), grid, block, lds, st, a);
+  else hipLaunchKernelGGL((down_kernel<T, P, 4>), grid, block, lds, st, a);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
+template <class T>
+int enqueue_down(const Layer &a, int cols, hipStream_t st) {
+  if (a.H >= 16 * 512) return enqueue_down_parts<T, 1>(a, cols, st);
+  return enqueue_down_parts<T, 2>(a, cols, st);
+}
+
 template <class T>
 int enqueue(const Layer &a, hipStream_t st) {
   const int E = a.r.E, cols = (a.T + kTile - 1) / kTile;
   (void)hipGetLastError();
-  const dim3 gg((E + kTile - 1) / kTile, a.splits), gb(64 * kGateWaves);
+  const dim3 gg((E + kTile - 1) / kTile, kSplits), gb(64 * kGateWaves);
   if (cols <= 1) hipLaunchKernelGGL((gate_kernel<T, 1>), gg, gb, 0, st, a);
   else if (cols <= 2) hipLaunchKernelGGL((gate_kernel<T, 2>), gg, gb, 0, st, a);
   else if (cols <= 4) hipLaunchKernelGGL((gate_kernel<T, 4>), gg, gb, 0, st, a);
@@ -373,15 +594,13 @@ int enqueue(const Layer &a, hipStream_t st) {
   else if (E <= 512) hipLaunchKernelGGL((few_route_kernel<8>), rg, rb, 0, st, a);
   else hipLaunchKernelGGL((few_route_kernel<16>), rg, rb, 0, st, a);
   if (!launched()) return TOPOEP_EHIP;
-  hipLaunchKernelGGL(few_lists_kernel, dim3(1), dim3(kListThreads), 0, st, a);
-  if (!launched()) return TOPOEP_EHIP;
-  // experts with pairs: at most one a pair, one an expert (several experts may share a slot)
-  const int most = imin(a.T * a.r.k, E);
-  const int tiles = (a.I + kTile - 1) / kTile;
-  hipLaunchKernelGGL((up_kernel<T>), dim3((unsigned)most * tiles), dim3(64 * kUpWaves), 0, st, a);
-  if (!launched()) return TOPOEP_EHIP;
-  hipLaunchKernelGGL((down_kernel<T>), dim3((a.H + kTile - 1) / kTile), dim3(64 * kDownWaves),
-                     kDownWaves * a.T * 4 * sizeof(v4f), st, a);
+  int rc = enqueue_experts<T, true>(a, st);
+  if (rc != TOPOEP_OK) return rc;
+  const int experts = imin(imin(a.T * a.r.k, E), a.L);
+  if (a.T * a.r.k <= 16 && (int64_t)experts * a.H * a.I <= 1 << 25) return enqueue_down<T>(a, cols, st);
+  rc = enqueue_experts<T, false>(a, st);
+  if (rc != TOPOEP_OK) return rc;
+  hipLaunchKernelGGL((combine_kernel<T>), dim3((a.H + 1023) / 1024, a.T), dim3(256), 0, st, a);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
@@ -393,7 +612,7 @@ int topoep_moe_workspace_bytes(const topoep_moe *m, const topoep_router *r, int3
   const int rc = check_layer(m, r, T);
   if (rc != TOPOEP_OK) return rc;
   if (!bytes_out) return TOPOEP_EINVAL;
-  *bytes_out = parts_of(m, r, T).total;
+  *bytes_out = places_of(m, r, T).total;
   return TOPOEP_OK;
 }
 
@@ -404,9 +623,9 @@ int topoep_moe_few(const topoep_moe *m, const topoep_router *r, const void *x, i
   if (rc != TOPOEP_OK) return rc;
   if (T == 0) return TOPOEP_OK;
   if (!x || !gate || !up || !down || !out || !ids || !weights || !workspace) return TOPOEP_EINVAL;
-  if (ldx < m->hidden || (ldx & 7) || ldx > (int64_t)1 << 40) return TOPOEP_EINVAL;
+  if (ldx < m->hidden || (ldx & 7) || ldx >= 1 << 24) return TOPOEP_EINVAL;
   if (!aligned16(x) || !aligned16(gate) || !aligned16(up) || !aligned16(down) || !aligned16(out)) return TOPOEP_EINVAL;
-  const Parts p = parts_of(m, r, T);
+  const Places p = places_of(m, r, T);
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < p.total) return TOPOEP_EWORKSPACE;
   char *ws = static_cast<char *>(workspace);
   Layer a;
@@ -415,7 +634,6 @@ int topoep_moe_few(const topoep_moe *m, const topoep_router *r, const void *x, i
   a.H = m->hidden;
   a.I = m->inter;
   a.L = m->local_experts;
-  a.splits = gate_splits(r->num_experts, m->hidden);
   a.x = x;
   a.ldx = ldx;
   a.gate = gate;
@@ -428,10 +646,9 @@ int topoep_moe_few(const topoep_moe *m, const topoep_router *r, const void *x, i
   a.weights = weights;
   a.logits = reinterpret_cast<float *>(ws + p.logits);
   a.hidden = ws + p.hidden;
-  int32_t *lists = reinterpret_cast<int32_t *>(ws + p.lists);
-  a.lists.active = lists;
-  a.lists.slot = lists + 1;
-  a.lists.begin = lists + 1 + r->num_experts;
+  a.each = reinterpret_cast<float *>(ws + p.each);
+  a.lists.active = reinterpret_cast<uint32_t *>(ws + p.active);
+  a.lists.count = reinterpret_cast<int32_t *>(ws + p.count);
   a.lists.pairs = reinterpret_cast<int32_t *>(ws + p.pairs);
   hipStream_t st = static_cast<hipStream_t>(stream);
   return m->dtype == TOPOEP_BF16 ? enqueue<Bf16>(a, st) : enqueue<F16>(a, st);
