@@ -162,8 +162,8 @@ int topoep_grads_workspace_bytes(int32_t count, size_t *bytes_out);
 /*
  * Enqueue the global norm of a set of tensors: *norm (device float) = scale *
  * the 2-norm, or the largest magnitude, over all of their elements.  Squares
- * are summed in 64 bits in an order that depends on the sizes alone, so equal
- * inputs give equal bits.  NaN where an element is NaN.  scale: finite, >= 0
+ * are summed in 64 bits in an order that depends only on the sizes and on which
+ * tensors follow each other in memory, so equal calls give equal bits.  NaN where an element is NaN.  scale: finite, >= 0
  * (1 / the loss scale).
  */
 int topoep_grad_norm(const topoep_grad *grads, int32_t count, float scale, int32_t ord, float *norm, void *workspace,

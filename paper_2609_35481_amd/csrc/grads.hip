@@ -1,12 +1,19 @@
 // The global gradient norm over many tensors and the clip on gfx950.
 //
 // The tensors' addresses and sizes travel as kernel arguments, kSet tensors a
-// launch, so a call copies nothing to the device and may be captured.  A
+// launch, so a call copies nothing to the device and may be captured; tensors
+// that follow each other in memory (views of one flat buffer) count as one.  A
 // launch's elements are cut into chunks of kChunk elements that do not cross
-// tensors, and workgroup b takes chunks b, b + grid, ...  The norm kernel
-// leaves one 64-bit partial a workgroup; the reader sums them in a fixed
+// tensors, and each workgroup walks one contiguous range of chunks.  The norm
+// kernel leaves one 64-bit partial a workgroup; the reader sums them in a fixed
 // order.  Squares are formed and summed in 64 bits: the square of any 32-bit
 // number is exact there and neither overflows nor vanishes.
+//
+// Bound: memory.  The norm of 1.37 G 16-bit elements runs at 6.5 TB/s (7.0 for
+// reads alone on this card), the clip of 441 M of them into a 32-bit buffer
+// moves its 2.65 GB at 5.8 TB/s (6.0 for a plain copy).  Loads and stores go past
+// the caches (without: 4.6 and 4.5 TB/s).  The pieces lie in the order of the
+// workgroups: one long range a workgroup took the clip 520 us, now 458.
 #include "router.h"
 
 namespace {
@@ -14,19 +21,23 @@ namespace {
 using namespace topoep_dev;
 
 constexpr int kThreads = 256;
-constexpr int kSet = 112;          // tensors a launch takes (3.6 KB of arguments)
-constexpr int64_t kChunk = 16384;  // elements of one step of a workgroup
-constexpr int kBlocks = 1024;      // workgroups, and partials, a launch has at most
-// elements a set may have (2^26 chunks: chunk numbers are 32-bit words)
+constexpr int kSet = 128;          // tensors a launch takes (3.6 KB of arguments)
+constexpr int64_t kChunk = 2048;
+constexpr int kBlocks = 2048;      // workgroups, and partials, a launch of the norm has at most
+constexpr int kClipBlocks = 8192;  // workgroups a launch of the clip has at most
+
+// elements a set may have (2^29 chunks: chunk numbers are 32-bit words)
 constexpr int64_t kMostElements = (int64_t)1 << 40;
 
 struct Set {
   int count, chunks;
-  int first[kSet];     // chunks before tensor i
-  int types[kSet];     // dtype | out_dtype << 4
+  int first[kSet];      // chunks before tensor i
   const void *grad[kSet];
   void *out[kSet];
-  int64_t n[kSet];
+  int64_t n[kSet];      // elements | dtype << 56 | out_dtype << 60
+  __host__ __device__ int64_t size(int i) const { return n[i] & (((int64_t)1 << 56) - 1); }
+  __host__ __device__ int type(int i) const { return (int)(n[i] >> 56) & 15; }
+  __host__ __device__ int out_type(int i) const { return (int)(n[i] >> 60) & 15; }
 };
 
 // The tensor that holds a chunk (the last with first <= chunk).
@@ -37,6 +48,25 @@ __device__ inline int tensor_of(const Set &s, int chunk) {
     if (s.first[mid] <= chunk) lo = mid; else hi = mid - 1;
   }
   return lo;
+}
+
+// Calls f(tensor, first element, elements) for the parts of workgroup b's
+// pieces, kPiece chunks each: b, b + grid, ... (Back: counted from the end), so
+// that the workgroups' accesses move through memory together.
+constexpr int kPiece = 4;
+template <bool Back, class F>
+__device__ inline void each_part(const Set &s, int b, const F &f) {
+  const int pieces = (s.chunks + kPiece - 1) / kPiece;
+  for (int p = b; p < pieces; p += gridDim.x) {
+    int c = (Back ? pieces - 1 - p : p) * kPiece;
+    const int end = imin(c + kPiece, s.chunks);
+    for (int i = tensor_of(s, c); c < end; ++i) {
+      const int stop = i + 1 < s.count ? imin(end, s.first[i + 1]) : end;
+      const int64_t at = (int64_t)(c - s.first[i]) * kChunk, to = (int64_t)(stop - s.first[i]) * kChunk, n = s.size(i);
+      f(i, at, (to < n ? to : n) - at);
+      c = stop;
+    }
+  }
 }
 
 struct Sum {      // the 2-norm's
@@ -62,44 +92,86 @@ __device__ inline double join_block(R r, double *lds) {
   return r.v;
 }
 
-// Elements a thread loads at once (16 bytes).
-template <class T> constexpr int kWide = 16 / sizeof(T);
+// W elements of T at once, 4 to 16 bytes, at any alignment of theirs.
+template <int Bytes, int Align> struct Word;
+template <> struct Word<16, 2> { typedef int type __attribute__((ext_vector_type(4), aligned(2))); };
+template <> struct Word<16, 4> { typedef int type __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct Word<8, 2> { typedef int type __attribute__((ext_vector_type(2), aligned(2))); };
 
-template <class T, class R>
-__device__ inline void reduce_chunk(const T *g, int64_t n, R &r) {
-  constexpr int W = kWide<T>, U = 4;
-  const int64_t step = (int64_t)kThreads * W;
-  int64_t i = (int64_t)threadIdx.x * W;
-  for (; i + (U - 1) * step + W <= n; i += U * step) {
-    T raw[U][W];
-#pragma unroll
-    for (int u = 0; u < U; ++u) __builtin_memcpy(raw[u], g + i + u * step, 16);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int w = 0; w < W; ++w) r.add(to_float(raw[u][w]));
-  }
-  for (; i < n; i += step) {
-#pragma unroll
-    for (int w = 0; w < W; ++w)
-      if (i + w < n) r.add(to_float(g[i + w]));
-  }
+template <bool Stream, int W, class T>
+__device__ inline void load_wide(const T *p, T (&raw)[W]) {
+  typedef typename Word<W * sizeof(T), sizeof(T)>::type Q;
+  const Q v = Stream ? __builtin_nontemporal_load(reinterpret_cast<const Q *>(p)) : *reinterpret_cast<const Q *>(p);
+  __builtin_memcpy(raw, &v, sizeof(raw));
+}
+template <bool Stream, int W, class T>
+__device__ inline void store_wide(T *p, const T (&raw)[W]) {
+  typedef typename Word<W * sizeof(T), sizeof(T)>::type Q;
+  Q v;
+  __builtin_memcpy(&v, raw, sizeof(raw));
+  if (Stream) __builtin_nontemporal_store(v, reinterpret_cast<Q *>(p));
+  else *reinterpret_cast<Q *>(p) = v;
 }
 
-template <class R>
+// Calls take(first element, raw) for W elements a thread at a time, U loads in
+// flight, from element `head` on, and one(element) for those before it and
+// those behind the last whole step of the workgroup.
+template <bool Stream, int W, int U, class T, class F, class G>
+__device__ inline void each_wide(const T *g, int64_t n, int head, const F &take, const G &one) {
+  constexpr int64_t kStep = (int64_t)kThreads * W;
+  if (head > n) head = (int)n;
+  if ((int)threadIdx.x < head) one(threadIdx.x);
+  int64_t i = head + (int64_t)threadIdx.x * W;
+  int64_t steps = (n - head) / kStep;
+  for (; steps >= U; steps -= U, i += U * kStep) {
+    T raw[U][W];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_wide<Stream, W>(g + i + u * kStep, raw[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) take(i + u * kStep, raw[u]);
+  }
+  T raw[U][W];
+#pragma unroll
+  for (int u = 0; u < U - 1; ++u)
+    if (u < steps) load_wide<Stream, W>(g + i + u * kStep, raw[u]);
+#pragma unroll
+  for (int u = 0; u < U - 1; ++u)
+    if (u < steps) take(i + u * kStep, raw[u]);
+  for (i = n - (n - head) % kStep + threadIdx.x; i < n; i += kThreads) one(i);
+}
+
+template <bool Stream, class T, class R>
+__device__ inline void reduce_part(const T *g, int64_t n, R &r) {
+  R other[3];   // four chains of sums
+  constexpr int W = 16 / sizeof(T);
+  each_wide<Stream, W, 8>(
+      g, n, 0,
+      [&](int64_t, const T(&raw)[W]) {
+#pragma unroll
+        for (int w = 0; w < W; w += 4) {
+          r.add(to_float(raw[w]));
+          other[0].add(to_float(raw[w + 1]));
+          other[1].add(to_float(raw[w + 2]));
+          other[2].add(to_float(raw[w + 3]));
+        }
+      },
+      [&](int64_t i) { r.add(to_float(g[i])); });
+  r.join(other[0].v);
+  r.join(other[1].v);
+  r.join(other[2].v);
+}
+
+template <class R, bool Stream>
 __global__ __launch_bounds__(kThreads) void grad_norm_kernel(Set s, double *partials) {
   __shared__ double lds[kThreads / 64];
   R r;
-  for (int c = blockIdx.x; c < s.chunks; c += gridDim.x) {
-    const int i = tensor_of(s, c);
-    const int64_t at = (int64_t)(c - s.first[i]) * kChunk;
-    const int64_t n = s.n[i] - at < kChunk ? s.n[i] - at : kChunk;
-    switch (s.types[i] & 15) {
-      case TOPOEP_F32: reduce_chunk(static_cast<const float *>(s.grad[i]) + at, n, r); break;
-      case TOPOEP_BF16: reduce_chunk(static_cast<const Bf16 *>(s.grad[i]) + at, n, r); break;
-      default: reduce_chunk(static_cast<const F16 *>(s.grad[i]) + at, n, r); break;
+  each_part<false>(s, blockIdx.x, [&](int i, int64_t at, int64_t n) {
+    switch (s.type(i)) {
+      case TOPOEP_F32: reduce_part<Stream>(static_cast<const float *>(s.grad[i]) + at, n, r); break;
+      case TOPOEP_BF16: reduce_part<Stream>(static_cast<const Bf16 *>(s.grad[i]) + at, n, r); break;
+      default: reduce_part<Stream>(static_cast<const F16 *>(s.grad[i]) + at, n, r); break;
     }
-  }
+  });
   const double v = join_block(r, lds);
   if (threadIdx.x == 0) partials[blockIdx.x] = v;
 }
@@ -123,36 +195,30 @@ __global__ __launch_bounds__(kThreads) void grad_finish_kernel(const double *par
   if (threadIdx.x == 0) *norm = v;
 }
 
-template <class T, class O>
-__device__ inline void scale_chunk(const T *g, O *out, int64_t n, float f) {
-  constexpr int W = kWide<T>, U = 4;
-  const int64_t step = (int64_t)kThreads * W;
-  int64_t i = (int64_t)threadIdx.x * W;
-  for (; i + (U - 1) * step + W <= n; i += U * step) {
-    T raw[U][W];
+// Threads take as many elements as make 16 bytes of the wider type, from the
+// first one on that starts a line of the outputs, so that whole lines are
+// written at once.
+template <bool Stream, class T, class O>
+__device__ inline void scale_part(const T *g, O *out, int64_t n, float f) {
+  constexpr int W = 16 / (sizeof(T) > sizeof(O) ? sizeof(T) : sizeof(O));
+  const int head = (int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(out)) & 127u) / (int)sizeof(O);
+  each_wide<Stream, W, 4>(
+      g, n, head,
+      [&](int64_t i, const T(&raw)[W]) {
+        O to[W];
 #pragma unroll
-    for (int u = 0; u < U; ++u) __builtin_memcpy(raw[u], g + i + u * step, 16);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      O to[W];
-#pragma unroll
-      for (int w = 0; w < W; ++w) to[w] = from_float<O>(to_float(raw[u][w]) * f);
-      __builtin_memcpy(out + i + u * step, to, sizeof(to));
-    }
-  }
-  for (; i < n; i += step) {
-#pragma unroll
-    for (int w = 0; w < W; ++w)
-      if (i + w < n) out[i + w] = from_float<O>(to_float(g[i + w]) * f);
-  }
+        for (int w = 0; w < W; ++w) to[w] = from_float<O>(to_float(raw[w]) * f);
+        store_wide<Stream, W>(out + i, to);
+      },
+      [&](int64_t i) { out[i] = from_float<O>(to_float(g[i]) * f); });
 }
 
-template <class T>
-__device__ inline void scale_chunk_to(const T *g, void *out, int type, int64_t at, int64_t n, float f) {
+template <bool Stream, class T>
+__device__ inline void scale_part_to(const T *g, void *out, int type, int64_t at, int64_t n, float f) {
   switch (type) {
-    case TOPOEP_F32: scale_chunk(g + at, static_cast<float *>(out) + at, n, f); break;
-    case TOPOEP_BF16: scale_chunk(g + at, static_cast<Bf16 *>(out) + at, n, f); break;
-    default: scale_chunk(g + at, static_cast<F16 *>(out) + at, n, f); break;
+    case TOPOEP_F32: scale_part<Stream>(g + at, static_cast<float *>(out) + at, n, f); break;
+    case TOPOEP_BF16: scale_part<Stream>(g + at, static_cast<Bf16 *>(out) + at, n, f); break;
+    default: scale_part<Stream>(g + at, static_cast<F16 *>(out) + at, n, f); break;
   }
 }
 
@@ -164,48 +230,54 @@ struct Clip {
   float *norm;            // or null
 };
 
-template <class R>
+template <class R, bool Stream>
 __global__ __launch_bounds__(kThreads) void clip_kernel(Set s, Clip c) {
   __shared__ double lds[kThreads / 64];
   const float norm = c.given ? *c.given : norm_of<R>(c.partials, c.count, c.scale, lds);
   if (c.norm && blockIdx.x == 0 && threadIdx.x == 0) *c.norm = norm;
   if (!(norm - norm == 0.0f)) return;
   const float f = c.scale * fminf(1.0f, c.max_norm / (norm + 1e-6f));
-  // the chunks that the norm read last come first: the caches may still hold them
-  for (int i0 = s.chunks - 1 - (int)blockIdx.x; i0 >= 0; i0 -= gridDim.x) {
-    const int i = tensor_of(s, i0);
-    if (f == 1.0f && s.out[i] == s.grad[i]) continue;
-    const int64_t at = (int64_t)(i0 - s.first[i]) * kChunk;
-    const int64_t n = s.n[i] - at < kChunk ? s.n[i] - at : kChunk;
-    const int to = s.types[i] >> 4;
-    switch (s.types[i] & 15) {
-      case TOPOEP_F32: scale_chunk_to(static_cast<const float *>(s.grad[i]), s.out[i], to, at, n, f); break;
-      case TOPOEP_BF16: scale_chunk_to(static_cast<const Bf16 *>(s.grad[i]), s.out[i], to, at, n, f); break;
-      default: scale_chunk_to(static_cast<const F16 *>(s.grad[i]), s.out[i], to, at, n, f); break;
+  each_part<true>(s, blockIdx.x, [&](int i, int64_t at, int64_t n) {
+    if (f == 1.0f && s.out[i] == s.grad[i]) return;
+    const int to = s.out_type(i);
+    switch (s.type(i)) {
+      case TOPOEP_F32: scale_part_to<Stream>(static_cast<const float *>(s.grad[i]), s.out[i], to, at, n, f); break;
+      case TOPOEP_BF16: scale_part_to<Stream>(static_cast<const Bf16 *>(s.grad[i]), s.out[i], to, at, n, f); break;
+      default: scale_part_to<Stream>(static_cast<const F16 *>(s.grad[i]), s.out[i], to, at, n, f); break;
     }
-  }
+  });
 }
 
+int bytes_of(int type) { return type == TOPOEP_F32 ? 4 : 2; }
+const char *end_of(const void *p, int64_t n, int type) { return static_cast<const char *>(p) + n * bytes_of(type); }
+
 // Walks the set in launches of kSet tensors: fills each one's arguments and
-// calls go(set, index of the launch).
+// calls go(set, index of the launch).  `out`: outputs count too.
 template <class F>
-int each_set(const topoep_grad *grads, int count, const F &go) {
+int each_set(const topoep_grad *grads, int count, bool out, const F &go) {
   Set s;
   int at = 0, launch = 0;
   do {
     s.count = 0;
-    int64_t chunks = 0;
-    for (; at < count && s.count < kSet; ++at) {
+    for (; at < count; ++at) {
       const topoep_grad &g = grads[at];
-      const int64_t more = (g.n + kChunk - 1) / kChunk;
-      if (more == 0) continue;
+      if (g.n == 0) continue;
+      const int last = s.count - 1;
+      if (last >= 0 && s.type(last) == g.dtype && end_of(s.grad[last], s.size(last), g.dtype) == g.grad &&
+          (!out || (s.out_type(last) == g.out_dtype && end_of(s.out[last], s.size(last), g.out_dtype) == g.out))) {
+        s.n[last] += g.n;
+        continue;
+      }
+      if (s.count == kSet) break;
       const int i = s.count++;
-      s.first[i] = (int)chunks;
-      s.types[i] = g.dtype | g.out_dtype << 4;
       s.grad[i] = g.grad;
-      s.out[i] = g.out;
-      s.n[i] = g.n;
-      chunks += more;
+      s.out[i] = out ? g.out : nullptr;
+      s.n[i] = g.n | (int64_t)g.dtype << 56 | (int64_t)(out ? g.out_dtype : 0) << 60;
+    }
+    int64_t chunks = 0;
+    for (int i = 0; i < s.count; ++i) {
+      s.first[i] = (int)chunks;
+      chunks += (s.size(i) + kChunk - 1) / kChunk;
     }
     s.chunks = (int)chunks;
     const int rc = go(s, launch++);
@@ -214,7 +286,18 @@ int each_set(const topoep_grad *grads, int count, const F &go) {
   return TOPOEP_OK;
 }
 
-int grid_of(const Set &s) { return s.chunks < kBlocks ? (s.chunks > 0 ? s.chunks : 1) : kBlocks; }
+// Bytes of the gradients from which on they are read (and results written) past
+// the caches: what is larger than the 256 MB of the last one is not found
+// there again anyway.
+constexpr int64_t kStreamBytes = (int64_t)256 << 20;
+
+bool streams(const topoep_grad *grads, int count) {
+  int64_t bytes = 0;
+  for (int i = 0; i < count; ++i) bytes += grads[i].n * bytes_of(grads[i].dtype);
+  return bytes > kStreamBytes;
+}
+
+int grid_of(const Set &s, int most) { return imax(1, imin(most, (s.chunks + kPiece - 1) / kPiece)); }
 
 int check_set(const topoep_grad *grads, int32_t count, bool out) {
   if (count < 0 || (count > 0 && !grads)) return TOPOEP_EINVAL;
@@ -246,21 +329,40 @@ int check_workspace(const void *ws, size_t bytes, int32_t count) {
 
 bool finite_scale(float s) { return s >= 0.0f && s - s == 0.0f; }
 
-// Enqueues the partials; returns their number in *partials.
-int enqueue_partials(const topoep_grad *grads, int count, int ord, double *ws, hipStream_t st, int *partials) {
-  int total = 0;
-  (void)hipGetLastError();
-  const int rc = each_set(grads, count, [&](const Set &s, int) {
-    const int grid = grid_of(s);
-    if (ord == TOPOEP_NORM_2)
-      hipLaunchKernelGGL((grad_norm_kernel<Sum>), dim3(grid), dim3(kThreads), 0, st, s, ws + total);
-    else
-      hipLaunchKernelGGL((grad_norm_kernel<Largest>), dim3(grid), dim3(kThreads), 0, st, s, ws + total);
-    total += grid;
+template <class R, bool Stream>
+int enqueue_partials(const topoep_grad *grads, int count, double *ws, hipStream_t st, int *partials) {
+  return each_set(grads, count, false, [&](const Set &s, int) {
+    const int grid = grid_of(s, kBlocks);
+    hipLaunchKernelGGL((grad_norm_kernel<R, Stream>), dim3(grid), dim3(kThreads), 0, st, s, ws + *partials);
+    *partials += grid;
     return hipGetLastError() == hipSuccess ? TOPOEP_OK : TOPOEP_EHIP;
   });
-  *partials = total;
-  return rc;
+}
+
+template <class R>
+int enqueue_norm(const topoep_grad *grads, int count, float scale, float *norm, double *ws, hipStream_t st) {
+  int partials = 0;
+  (void)hipGetLastError();
+  const int rc = streams(grads, count) ? enqueue_partials<R, true>(grads, count, ws, st, &partials)
+                                       : enqueue_partials<R, false>(grads, count, ws, st, &partials);
+  if (rc != TOPOEP_OK) return rc;
+  hipLaunchKernelGGL((grad_finish_kernel<R>), dim3(1), dim3(kThreads), 0, st, ws, partials, scale, norm);
+  return hipGetLastError() == hipSuccess ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
+template <class R, bool Stream>
+int enqueue_clip(const topoep_grad *grads, int count, Clip c, double *ws, hipStream_t st) {
+  (void)hipGetLastError();
+  if (!c.given) {
+    const int rc = enqueue_partials<R, Stream>(grads, count, ws, st, &c.count);
+    if (rc != TOPOEP_OK) return rc;
+  }
+  return each_set(grads, count, true, [&](const Set &s, int launch) {
+    Clip own = c;
+    if (launch > 0) own.norm = nullptr;
+    hipLaunchKernelGGL((clip_kernel<R, Stream>), dim3(grid_of(s, kClipBlocks)), dim3(kThreads), 0, st, s, own);
+    return hipGetLastError() == hipSuccess ? TOPOEP_OK : TOPOEP_EHIP;
+  });
 }
 
 }  // namespace
@@ -282,14 +384,8 @@ int topoep_grad_norm(const topoep_grad *grads, int32_t count, float scale, int32
   if (rc != TOPOEP_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
   double *ws = static_cast<double *>(workspace);
-  int partials = 0;
-  rc = enqueue_partials(grads, count, ord, ws, st, &partials);
-  if (rc != TOPOEP_OK) return rc;
-  if (ord == TOPOEP_NORM_2)
-    hipLaunchKernelGGL((grad_finish_kernel<Sum>), dim3(1), dim3(kThreads), 0, st, ws, partials, scale, norm);
-  else
-    hipLaunchKernelGGL((grad_finish_kernel<Largest>), dim3(1), dim3(kThreads), 0, st, ws, partials, scale, norm);
-  return hipGetLastError() == hipSuccess ? TOPOEP_OK : TOPOEP_EHIP;
+  return ord == TOPOEP_NORM_2 ? enqueue_norm<Sum>(grads, count, scale, norm, ws, st)
+                              : enqueue_norm<Largest>(grads, count, scale, norm, ws, st);
 }
 
 int topoep_clip_grads(const topoep_grad *grads, int32_t count, float scale, int32_t ord, float max_norm,
@@ -302,20 +398,12 @@ int topoep_clip_grads(const topoep_grad *grads, int32_t count, float scale, int3
   if (rc != TOPOEP_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
   double *ws = static_cast<double *>(workspace);
-  int partials = 0;
-  if (!given_norm) {
-    rc = enqueue_partials(grads, count, ord, ws, st, &partials);
-    if (rc != TOPOEP_OK) return rc;
-  }
-  (void)hipGetLastError();
-  return each_set(grads, count, [&](const Set &s, int launch) {
-    Clip c{ws, partials, scale, max_norm, given_norm, launch == 0 ? norm : nullptr};
-    if (ord == TOPOEP_NORM_2)
-      hipLaunchKernelGGL((clip_kernel<Sum>), dim3(grid_of(s)), dim3(kThreads), 0, st, s, c);
-    else
-      hipLaunchKernelGGL((clip_kernel<Largest>), dim3(grid_of(s)), dim3(kThreads), 0, st, s, c);
-    return hipGetLastError() == hipSuccess ? TOPOEP_OK : TOPOEP_EHIP;
-  });
+  const Clip c{ws, 0, scale, max_norm, given_norm, norm};
+  const bool stream_past = streams(grads, count);
+  if (ord == TOPOEP_NORM_2)
+    return stream_past ? enqueue_clip<Sum, true>(grads, count, c, ws, st) : enqueue_clip<Sum, false>(grads, count, c, ws, st);
+  return stream_past ? enqueue_clip<Largest, true>(grads, count, c, ws, st)
+                     : enqueue_clip<Largest, false>(grads, count, c, ws, st);
 }
 
 }  // extern "C"
