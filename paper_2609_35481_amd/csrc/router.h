@@ -42,10 +42,13 @@ template <> __device__ inline Bf16 from_float<Bf16>(float f) { return Bf16{float
 template <> __device__ inline F16 from_float<F16>(float f) { return F16{(_Float16)f}; }
 
 // A logit as the router takes it: NaN and -inf masked (-inf), +inf the
-// largest finite number.
+// largest finite number.  A median with a NaN among its operands is the least
+// of the others; -inf goes by a register, or the compiler takes the median for
+// the minimum of the other two, which gives a NaN the largest number.
 __device__ inline float clean_logit(float x) {
-  x = x != x ? -INFINITY : x;
-  return x > 3.402823466e38f ? 3.402823466e38f : x;
+  float low = -INFINITY;
+  asm("" : "+v"(low));
+  return __builtin_amdgcn_fmed3f(x, low, 3.402823466e38f);
 }
 
 // The float's place in ascending order.  k + 0 makes -0 and +0 one key.

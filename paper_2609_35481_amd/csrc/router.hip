@@ -35,6 +35,278 @@ __global__ __launch_bounds__(kThreads) void route_kernel(Route a) {
   }
 }
 
+// ---------------------------------------------------------------- sorted lists
+
+// Up to eight experts a token: a few lanes hold a row, V experts each, and
+// keep the K largest as a sorted list; lists are merged over the lanes, after
+// which every lane holds the row's.  An entry is the key as a 64-bit float,
+// whose low bits, zero in every converted 32-bit float, hold the expert's id so
+// that of equal keys the lower id is the larger number: a comparison and its
+// exchange are one maximum and one minimum, with no tie to look after.
+// -inf (masked) becomes -2^129, below every 32-bit float, an overflown key 2^129;
+// what cannot be chosen lies below them all.
+constexpr int kIdBits = 10;
+constexpr uint32_t kIdMask = (1u << kIdBits) - 1;
+static_assert(TOPOEP_ROUTER_MAX_EXPERTS <= (int)kIdMask + 1, "ids fit an entry");
+
+// The larger and the smaller of two numbers, neither of them a signalling NaN
+// (fmax and fmin would first quiet their operands, an instruction each: a
+// third of all).
+__device__ inline double larger(double a, double b) {
+  double r;
+  asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ inline double smaller(double a, double b) {
+  double r;
+  asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+
+// anti: the id's complement in kIdBits, which goes into the low bits as it is
+// where the key is not negative, and complemented again where it is.
+template <bool Bias>
+__device__ inline double entry(float key, uint32_t anti) {
+  double d = key + 0.0f;   // -0 and +0 are one key
+  if (Bias) {
+    d = d != d ? -0x1p129 : d;
+    d = smaller(d, 0x1p129);
+  }
+  d = larger(d, -0x1p129);
+  const uint64_t u = (uint64_t)__double_as_longlong(d);
+  const uint32_t code = ((uint32_t)((int32_t)(u >> 32) >> 31) ^ anti) & kIdMask;
+  return __longlong_as_double((int64_t)(u | code));
+}
+__device__ inline int entry_id(double e) {
+  const uint64_t u = (uint64_t)__double_as_longlong(e);
+  return (int)(((uint32_t)u ^ ~(uint32_t)((int32_t)(u >> 32) >> 31)) & kIdMask);
+}
+
+__device__ inline void order(double &a, double &b) {   // a >= b
+  const double hi = larger(a, b), lo = smaller(a, b);
+  a = hi;
+  b = lo;
+}
+
+// A list that rises and then falls, or the reverse, in descending order.
+template <int K>
+__device__ inline void settle(double (&l)[K]) {
+#pragma unroll
+  for (int d = K / 2; d > 0; d /= 2)
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      if ((i & d) == 0) order(l[i], l[i + d]);
+}
+
+template <int K>
+__device__ inline void sort(double (&l)[K]) {
+  if constexpr (K == 4) {
+    order(l[0], l[2]); order(l[1], l[3]);
+    order(l[0], l[1]); order(l[2], l[3]);
+    order(l[1], l[2]);
+  } else {   // 19 exchanges: two halves of four, then their merge
+    static_assert(K == 8, "");
+    order(l[0], l[2]); order(l[1], l[3]); order(l[4], l[6]); order(l[5], l[7]);
+    order(l[0], l[1]); order(l[2], l[3]); order(l[4], l[5]); order(l[6], l[7]);
+    order(l[1], l[2]); order(l[5], l[6]);
+    order(l[0], l[4]); order(l[1], l[5]); order(l[2], l[6]); order(l[3], l[7]);
+    order(l[2], l[4]); order(l[3], l[5]);
+    order(l[1], l[2]); order(l[3], l[4]); order(l[5], l[6]);
+  }
+}
+
+// l: the K largest of two descending lists.
+template <int K>
+__device__ inline void merge(double (&l)[K], const double (&o)[K]) {
+#pragma unroll
+  for (int i = 0; i < K; ++i) l[i] = larger(l[i], o[K - 1 - i]);
+  settle(l);
+}
+
+template <int C>
+__device__ inline double dpp_movd(double v) { return __longlong_as_double((int64_t)dpp_mov64<C>((uint64_t)__double_as_longlong(v))); }
+
+// Lanes exchange with a partner of the other half of 2, 4, 8 and 16 lanes
+// (neighbour, next but one, mirror images), LPT lanes in all.
+template <int K, int C>
+__device__ inline void merge_over(double (&l)[K]) {
+  // a lane move may read a register two wait states after its writing at the
+  // earliest; the compiler counts them for its own instructions only
+  if constexpr (K == 4)
+    asm volatile("s_nop 1" : "+v"(l[0]), "+v"(l[1]), "+v"(l[2]), "+v"(l[3]));
+  else
+    asm volatile("s_nop 1" : "+v"(l[0]), "+v"(l[1]), "+v"(l[2]), "+v"(l[3]), "+v"(l[4]), "+v"(l[5]), "+v"(l[6]), "+v"(l[7]));
+  double o[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) o[i] = dpp_movd<C>(l[i]);
+  merge(l, o);
+}
+template <int LPT, int K>
+__device__ inline void merge_row(double (&l)[K]) {
+  if (LPT > 1) merge_over<K, 0xB1>(l);
+  if (LPT > 2) merge_over<K, 0x4E>(l);
+  if (LPT > 4) merge_over<K, 0x141>(l);
+  if (LPT > 8) merge_over<K, 0x140>(l);
+}
+template <int LPT>
+__device__ inline float few_max(float v) {
+  if (LPT > 1) v = fmaxf(v, dpp_movf<0xB1>(v));
+  if (LPT > 2) v = fmaxf(v, dpp_movf<0x4E>(v));
+  if (LPT > 4) v = fmaxf(v, dpp_movf<0x141>(v));
+  if (LPT > 8) v = fmaxf(v, dpp_movf<0x140>(v));
+  return v;
+}
+template <int LPT>
+__device__ inline float few_sum(float v) {
+  if (LPT > 1) v += dpp_movf<0xB1>(v);
+  if (LPT > 2) v += dpp_movf<0x4E>(v);
+  if (LPT > 4) v += dpp_movf<0x141>(v);
+  if (LPT > 8) v += dpp_movf<0x140>(v);
+  return v;
+}
+
+// GL: groups a lane holds (a group may also span 2, 4 or 8 lanes: GL = 1); 0: no
+// groups.  Places beyond E hold masked logits of ids that no expert has: any
+// expert comes before them.
+template <class T, int LPT, int V, int K, int GL, bool Bias>
+__global__ __launch_bounds__(kThreads) void route_list_kernel(Route a) {
+  constexpr int kRows = kThreads / LPT;
+  const int sub = threadIdx.x % LPT, E = a.r.E, base = sub * V;
+  const int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / LPT;
+  const bool live = t < a.T;
+  const T *row = static_cast<const T *>(a.logits) + (live ? t : (int64_t)a.T - 1) * a.ld;
+  const uint32_t anti = (uint32_t)base ^ kIdMask;   // V is a power of two: ids base + v are base ^ v
+  float x[V], b[Bias ? V : 1];
+  load_logits<T, V>(row, base, E, x);
+  if constexpr (Bias) {
+    if (base + V <= E) {
+      __builtin_memcpy(b, a.bias + base, sizeof(b));
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) b[v] = base + v < E ? a.bias[base + v] : 0.0f;
+    }
+  }
+  const auto key = [&](int v) { return Bias ? x[v] + b[Bias ? v : 0] : x[v]; };
+  bool open[GL > 0 ? GL : 1];
+  if constexpr (GL > 0) {
+    // the groups' largest keys, as a list of (key, group)
+    constexpr int M = V / GL;
+    const int span = a.r.per_group / V;   // lanes a group spans, where it spans any
+    double best[8];
+    int mine[GL];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) best[i] = -0x1p200;
+#pragma unroll
+    for (int g = 0; g < GL; ++g) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int m = 0; m < M; ++m) top = fmaxf(top, key(g * M + m));   // passes over a NaN key, which counts as -inf
+      if (GL == 1) {
+        if (span > 1) top = fmaxf(top, dpp_movf<0xB1>(top));
+        if (span > 2) top = fmaxf(top, dpp_movf<0x4E>(top));
+        if (span > 4) top = fmaxf(top, dpp_movf<0x141>(top));
+      }
+      mine[g] = GL == 1 && span > 1 ? sub / span : sub * GL + g;
+      if (mine[g] < a.r.groups && (GL > 1 || span <= 1 || sub % span == 0))
+        best[g] = entry<Bias>(top, (uint32_t)mine[g] ^ kIdMask);
+    }
+    sort(best);
+    merge_row<LPT>(best);
+#pragma unroll
+    for (int g = 0; g < GL; ++g) {
+      open[g] = false;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) open[g] |= i < a.r.top_groups && entry_id(best[i]) == mine[g];
+    }
+  }
+  double l[K];
+#pragma unroll
+  for (int c = 0; c < (V + K - 1) / K; ++c) {
+    double o[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      const int v = c * K + i;
+      if (v >= V) {
+        o[i] = -0x1p200;
+        continue;
+      }
+      o[i] = entry<Bias>(key(v < V ? v : 0), anti ^ (uint32_t)v);
+      if (GL > 0) o[i] = open[GL > 0 ? (v < V ? v : 0) / (V / (GL > 0 ? GL : 1)) : 0] ? o[i] : -0x1p200;
+    }
+    sort(o);
+    if (c == 0) {
+#pragma unroll
+      for (int i = 0; i < K; ++i) l[i] = o[i];
+    } else {
+      merge(l, o);
+    }
+  }
+  merge_row<LPT>(l);
+  float s[K];   // the chosen logits, then their weights
+#pragma unroll
+  for (int j = 0; j < K; ++j) s[j] = (float)l[j];   // the key: -2^129 becomes -inf again
+  if (Bias) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) s[j] = j < a.r.k ? clean_logit(to_float(row[entry_id(l[j])])) : -INFINITY;
+  }
+  if (a.r.sigmoid) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+      s[j] = j < a.r.k ? __builtin_amdgcn_rcpf(1.0f + __expf(-s[j])) : 0.0f;
+      sum += s[j];
+    }
+    const float f = a.r.renorm ? (sum > 0.0f ? a.r.scale / sum : 0.0f) : a.r.scale;
+#pragma unroll
+    for (int j = 0; j < K; ++j) s[j] *= f;
+  } else {
+    float m, sum = 0.0f;
+    if (a.r.renorm) {
+      m = s[0];
+#pragma unroll
+      for (int j = 1; j < K; ++j) m = j < a.r.k ? fmaxf(m, s[j]) : m;
+#pragma unroll
+      for (int j = 0; j < K; ++j) sum += j < a.r.k && m != -INFINITY ? __expf(s[j] - m) : 0.0f;
+    } else {
+      m = x[0];
+#pragma unroll
+      for (int v = 1; v < V; ++v) m = fmaxf(m, x[v]);
+      m = few_max<LPT>(m);
+      const float from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int v = 0; v < V; ++v) sum += __expf(x[v] - from);
+      sum = few_sum<LPT>(sum);
+    }
+    const float f = sum > 0.0f ? a.r.scale / sum : 0.0f, from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int j = 0; j < K; ++j) s[j] = __expf(s[j] - from) * f;
+  }
+  if (!live) return;
+  int32_t *ids = a.ids + t * a.r.k;
+  float *weights = a.weights + t * a.r.k;
+  if (sub == 0) {
+    if (a.r.k == K) {
+      int32_t id[K];
+#pragma unroll
+      for (int j = 0; j < K; ++j) id[j] = entry_id(l[j]);
+      __builtin_memcpy(ids, id, sizeof(id));
+    } else {
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        if (j < a.r.k) ids[j] = entry_id(l[j]);
+    }
+  }
+  if (sub == 1) {
+    if (a.r.k == K) {
+      __builtin_memcpy(weights, s, sizeof(s));
+    } else {
+#pragma unroll
+      for (int j = 0; j < K; ++j)
+        if (j < a.r.k) weights[j] = s[j];
+    }
+  }
+}
+
 struct RouteBackward {
   RouterArgs r;
   const void *logits;
@@ -165,6 +437,52 @@ struct Backward {
   }
 };
 
+template <class T, int LPT, int V, int K, int GL>
+int enqueue_list(const Route &a, hipStream_t st) {
+  (void)hipGetLastError();
+  const dim3 grid((unsigned)(((int64_t)a.T * LPT + kThreads - 1) / kThreads)), block(kThreads);
+  if (a.bias) hipLaunchKernelGGL((route_list_kernel<T, LPT, V, K, GL, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((route_list_kernel<T, LPT, V, K, GL, false>), grid, block, 0, st, a);
+  return hipGetLastError() == hipSuccess ? TOPOEP_OK : TOPOEP_EHIP;
+}
+template <class T, int LPT>
+int enqueue_groups(const Route &a, int per_lane, hipStream_t st) {
+  if (per_lane == 4) return enqueue_list<T, LPT, 32, 8, 4>(a, st);
+  if (per_lane == 2) return enqueue_list<T, LPT, 32, 8, 2>(a, st);
+  return enqueue_list<T, LPT, 32, 8, 1>(a, st);
+}
+template <class T, int K>
+int enqueue_lists(const Route &a, hipStream_t st) {
+  if (a.r.E <= 16) return enqueue_list<T, 4, 4, K, 0>(a, st);
+  if (a.r.E <= 32) return enqueue_list<T, 4, 8, K, 0>(a, st);
+  if (a.r.E <= 64) return enqueue_list<T, 4, 16, K, 0>(a, st);
+  if (a.r.E <= 128) return enqueue_list<T, 4, 32, K, 0>(a, st);
+  if (a.r.E <= 256) return enqueue_list<T, 8, 32, K, 0>(a, st);
+  if (a.r.E <= 512) return enqueue_list<T, 16, 32, K, 0>(a, st);
+  return enqueue_list<T, 16, 64, K, 0>(a, st);
+}
+
+// Groups a lane of 32 experts holds whole (1, 2, 4; 1 also where a group is 1, 2, 4
+// or 8 lanes); 0 where groups and lanes do not fit.
+int groups_of_lane(const RouterArgs &r) {
+  const int m = r.per_group;
+  if (m == 8 || m == 16) return 32 / m;
+  return m == 32 || m == 64 || m == 128 || m == 256 ? 1 : 0;
+}
+
+template <class T>
+int enqueue_route(const Route &a, hipStream_t st) {
+  const RouterArgs &r = a.r;
+  if (r.k <= 8 && r.groups == 1) return r.k <= 4 ? enqueue_lists<T, 4>(a, st) : enqueue_lists<T, 8>(a, st);
+  const int per_lane = groups_of_lane(r);
+  if (r.k <= 8 && r.top_groups <= 8 && r.E > 64 && r.E <= 512 && per_lane > 0) {
+    if (r.E <= 128) return enqueue_groups<T, 4>(a, per_lane, st);
+    if (r.E <= 256) return enqueue_groups<T, 8>(a, per_lane, st);
+    return enqueue_groups<T, 16>(a, per_lane, st);
+  }
+  return launch_rows<T, Forward>(r.E, r.k, r.groups > 1 || a.T < 8192, a, a.T, st);
+}
+
 // Bytes from the first row to the end of the last fit a pointer's range.
 bool rows_fit(int T, int64_t ld, int E) { return ld >= E && (T < 2 || ld <= (INT64_MAX / 8 - E) / (T - 1)); }
 
@@ -181,11 +499,10 @@ int topoep_route(const topoep_router *r, const void *logits, int64_t ld, int32_t
   if (!logits || !ids || !weights) return TOPOEP_EINVAL;
   Route a{router_args(r), logits, ld, T, bias, ids, weights};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool wide = r->groups > 1 || T < 8192;
   switch (r->dtype) {
-    case TOPOEP_F32: return launch_rows<float, Forward>(a.r.E, a.r.k, wide, a, T, st);
-    case TOPOEP_BF16: return launch_rows<Bf16, Forward>(a.r.E, a.r.k, wide, a, T, st);
-    default: return launch_rows<F16, Forward>(a.r.E, a.r.k, wide, a, T, st);
+    case TOPOEP_F32: return enqueue_route<float>(a, st);
+    case TOPOEP_BF16: return enqueue_route<Bf16>(a, st);
+    default: return enqueue_route<F16>(a, st);
   }
 }
 
