@@ -204,17 +204,14 @@ __global__ __launch_bounds__(64 * kGateWaves) void gate_kernel(Layer a) {
 
 // ---------------------------------------------------------------- routing
 
+// Token t's logits, the partial sums joined in order, and the biases of a
+// lane's V experts.
 template <int V>
-__global__ __launch_bounds__(256) void few_route_kernel(Layer a) {
-  __shared__ uint32_t scratch[4][kRouteScratch];
-  const int wave = threadIdx.x >> 6, sub = lane_id();
-  const int t = blockIdx.x * 4 + wave;
-  const bool live = t < a.T;
-  const float *from = a.logits + (int64_t)(live ? t : 0) * a.r.E;
-  float x[V], b[V];
+__device__ inline void few_logits(const Layer &a, int t, float (&x)[V], float (&b)[V]) {
+  const float *from = a.logits + (int64_t)t * a.r.E;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int e = imin(sub * V + v, a.r.E - 1);
+    const int e = imin(lane_id() * V + v, a.r.E - 1);
     float part[kSplits];
 #pragma unroll
     for (int i = 0; i < kSplits; ++i) part[i] = from[(int64_t)i * a.T * a.r.E + e];
@@ -222,12 +219,28 @@ __global__ __launch_bounds__(256) void few_route_kernel(Layer a) {
     float s = part[0];
 #pragma unroll
     for (int i = 1; i < kSplits; ++i) s += part[i];
-    x[v] = sub * V + v < a.r.E ? clean_logit(s) : -INFINITY;
+    x[v] = lane_id() * V + v < a.r.E ? clean_logit(s) : -INFINITY;
   }
+}
+
+// An expert's place among the weights here, -1 where it is not here.
+__device__ inline int slot_of(const Layer &a, int e) {
+  const int s = a.slot ? a.slot[e] : e;
+  return (unsigned)s < (unsigned)a.L ? s : -1;
+}
+
+template <int V>
+__global__ __launch_bounds__(256) void few_route_kernel(Layer a) {
+  __shared__ uint32_t scratch[4][kRouteScratch];
+  const int wave = threadIdx.x >> 6, sub = lane_id();
+  const int t = blockIdx.x * 4 + wave;
+  const bool live = t < a.T;
+  float x[V], b[V];
+  few_logits<V>(a, live ? t : 0, x, b);
   route_row<64, V>(a.r, x, b, sub, scratch[wave], live, a.ids + (int64_t)t * a.r.k, a.weights + (int64_t)t * a.r.k);
   if (live && sub < a.r.k) {
-    const int e = (int)scratch[wave][2 * sub], s = a.slot ? a.slot[e] : e;
-    if ((unsigned)s < (unsigned)a.L) {
+    const int e = (int)scratch[wave][2 * sub];
+    if (slot_of(a, e) >= 0) {
       const int at = atomicAdd(&a.lists.count[e], 1);
       a.lists.pairs[(int64_t)e * a.T + at] = t * a.r.k + sub;
       if (at == 0) atomicOr(&a.lists.active[e >> 5], 1u << (e & 31));
@@ -255,14 +268,18 @@ template <> __device__ inline float saturate<F16>(float f) { return f > 65504.0f
 
 constexpr int kExpertWaves = 4;
 
-// Steps of a run by P and C.
-constexpr int run_steps(int P, int C) { return P == 4 ? (C == 1 ? 2 : 1) : C <= 4 ? 2 : 1; }
+// Steps of a run by P and C; with few tokens and shared tiles every load of a row
+// of 2048 elements is in flight at once.
+constexpr int run_steps(int P, int C, int KS) { return P == 4 ? (C == 1 ? (KS > 1 ? 4 : 2) : 1) : C <= 4 ? 2 : 1; }
 
 // A tile of 16 M rows of one expert against 16 / P * C of its pairs.  Rows: 8 M
 // hidden units' gate rows and their up rows (Up), or 16 M outputs.  KS = 1: the
 // tile is the wave's own; KS = kExpertWaves: the workgroup's waves share it, each
 // with its part of the runs.
-template <class T, bool Up, int P, int M, int C, int KS>
+// How many pairs an expert has, about; any number is served by each.
+enum Load { kOne, kFew, kMany };   // at most 4; mostly up to 16; more
+
+template <class T, bool Up, int P, int M, int C, int KS, int Kind>
 __device__ inline void expert_tile(const Layer &a, const char *weights, const int32_t *pairs, int count, int tile,
                                    v4f (*part)[64]) {
   constexpr int R = Parts<P>::kCols, kRows = Up ? 8 * M : 16 * M, NA = P * M;
@@ -276,13 +293,14 @@ __device__ inline void expert_tile(const Layer &a, const char *weights, const in
   }
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int at = c * R + lane % R, p = pairs[at < count ? at : 0];
+    const int at = c * R + lane % R;
+    const int p = pairs[at < count ? at : 0];
     src[c] = ((Up ? (uint32_t)(p / a.r.k) * (uint32_t)a.ldx : (uint32_t)p * (uint32_t)a.I) + place) * 2u;
   }
   const char *cols = static_cast<const char *>(Up ? a.x : a.hidden);
   v4f d[NA][C] = {};
   // eight tiles side by side run on eight XCDs
-  stream<T, P, run_steps(P, C)>(weights, row, cols, src, n, KS == 1 ? 0 : wave, KS, tile >> 3, d);
+  stream<T, P, run_steps(P, C, Kind == kOne ? KS : 1)>(weights, row, cols, src, n, KS == 1 ? 0 : wave, KS, tile >> 3, d);
   // this lane: rows q * 4 + 0..3 of part p, column `token` of part `of`
   const int q = (lane >> 4) % (R / 4), p = (lane >> 4) / (R / 4), token = lane % R, of = lane % kTile / R;
   constexpr int CE = C < 2 ? 1 : 2;   // columns' operands whose sums are joined at a time
@@ -325,9 +343,6 @@ __device__ inline void expert_tile(const Layer &a, const char *weights, const in
   }
 }
 
-// How many pairs an expert has, about; any number is served by each.
-enum Load { kOne, kFew, kMany };   // at most 4; mostly up to 16; more
-
 template <int Kind> constexpr int tile_rows(bool up) { return (up ? 8 : 16) * (Kind == kMany ? 2 : 1); }
 
 // Workgroup b takes tile b % groups (KS = 1: its waves four tiles side by side) of
@@ -348,19 +363,51 @@ __global__ __launch_bounds__(64 * kExpertWaves, Kind == kMany ? 3 : 4) void expe
     const char *w = Up ? static_cast<const char *>(a.up) + slot * 4 * a.I * a.H
                        : static_cast<const char *>(a.down) + slot * 2 * a.H * a.I;
     if (Kind == kOne) {
-      expert_tile<T, Up, 4, 1, 1, KS>(a, w, pairs, count, tile, part);
+      expert_tile<T, Up, 4, 1, 1, KS, Kind>(a, w, pairs, count, tile, part);
     } else if (Kind == kFew) {
-      if (count <= 4) expert_tile<T, Up, 4, 1, 1, KS>(a, w, pairs, count, tile, part);
-      else if (count <= 8) expert_tile<T, Up, 4, 1, 2, KS>(a, w, pairs, count, tile, part);
+      if (count <= 4) expert_tile<T, Up, 4, 1, 1, KS, Kind>(a, w, pairs, count, tile, part);
+      else if (count <= 8) expert_tile<T, Up, 4, 1, 2, KS, Kind>(a, w, pairs, count, tile, part);
       else
-        for (int at = 0; at < count; at += 16) expert_tile<T, Up, 2, 1, 2, KS>(a, w, pairs + at, count - at, tile, part);
+        for (int at = 0; at < count; at += 16) expert_tile<T, Up, 2, 1, 2, KS, Kind>(a, w, pairs + at, count - at, tile, part);
     } else {
-      if (count <= 16) expert_tile<T, Up, 1, 2, 1, KS>(a, w, pairs, count, tile, part);
-      else if (count <= 32) expert_tile<T, Up, 1, 2, 2, KS>(a, w, pairs, count, tile, part);
+      if (count <= 16) expert_tile<T, Up, 1, 2, 1, KS, Kind>(a, w, pairs, count, tile, part);
+      else if (count <= 32) expert_tile<T, Up, 1, 2, 2, KS, Kind>(a, w, pairs, count, tile, part);
       else
-        for (int at = 0; at < count; at += 64) expert_tile<T, Up, 1, 2, 4, KS>(a, w, pairs + at, count - at, tile, part);
+        for (int at = 0; at < count; at += 64) expert_tile<T, Up, 1, 2, 4, KS, Kind>(a, w, pairs + at, count - at, tile, part);
     }
   }
+}
+
+// One token: every wave routes it for itself, which takes the routing kernel's
+// 3.6 us and a launch off the path for 2 (one token, 128 experts of H = 2048, I =
+// 768: 26.7 us for the layer without); workgroup 0 leaves what the next kernel
+// reads.
+template <class T, int V>
+__global__ __launch_bounds__(64 * kExpertWaves, 4) void one_up_kernel(Layer a, int tiles) {
+  __shared__ uint32_t scratch[kExpertWaves][kRouteScratch];
+  __shared__ v4f part[kExpertWaves][64];
+  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id();
+  const bool writes = blockIdx.x == 0 && wave == 0;
+  float x[V], b[V];
+  few_logits<V>(a, 0, x, b);
+  route_row<64, V>(a.r, x, b, lane, scratch[wave], writes, a.ids, a.weights);
+  const int mine = lane < a.r.k ? (int)scratch[wave][2 * lane] : 0;
+  const int slot = lane < a.r.k ? slot_of(a, mine) : -1;
+  if (writes && slot >= 0) {
+    a.lists.count[mine] = 1;
+    a.lists.pairs[mine] = lane;
+    atomicOr(&a.lists.active[mine >> 5], 1u << (mine & 31));
+  }
+  const uint64_t here = __ballot(slot >= 0);
+  const int n = (int)blockIdx.x / tiles;
+  if (n >= __popcll((unsigned long long)here)) return;
+  const uint64_t before = __ballot(slot >= 0 && count_below(here, 0) == n);
+  const int j = __ffsll((unsigned long long)before) - 1;
+  int32_t *pair = reinterpret_cast<int32_t *>(scratch[wave]);
+  if (lane == 0) pair[0] = j;
+  wave_sync();
+  const char *w = static_cast<const char *>(a.up) + (int64_t)readlane_i32(slot, j) * 4 * a.I * a.H;
+  expert_tile<T, true, 4, 1, 1, kExpertWaves, kOne>(a, w, pair, 1, (int)blockIdx.x % tiles, part);
 }
 
 // out_t = sum over t's choices in order, of those whose expert is here.
@@ -370,8 +417,7 @@ __global__ __launch_bounds__(256) void combine_kernel(Layer a) {
   int here = 0;
   float weight = 0.0f;
   if (lane_id() < a.r.k) {
-    const int e = a.ids[p0 + lane_id()], slot = a.slot ? a.slot[e] : e;
-    here = (unsigned)slot < (unsigned)a.L;
+    here = slot_of(a, a.ids[p0 + lane_id()]) >= 0;
     weight = a.weights[p0 + lane_id()];
   }
   const float *from = a.each + (int64_t)p0 * a.H + imin(h, a.H - 4);
@@ -400,87 +446,78 @@ __global__ __launch_bounds__(256) void combine_kernel(Layer a) {
 constexpr int kDownWaves = 8;
 
 // One unit of a wave: `len` of the inner axis from `lo` of one expert's pairs,
-// against the tile's 16 / P outputs.  The tile's rows are the outputs P times
-// over, each time against another P-th of the axis, and its columns the
-// tokens P times over, likewise; the products of one part's rows with another
-// part's columns are dropped.
-template <class T, int P, int C>
-__device__ inline void down_unit(const Layer &a, const char *weights, uint32_t row, const int32_t *pairs, int count, int lo, int len,
-                                 v4f *mine) {
-  constexpr int R = kTile / P;
-  const int lane = lane_id(), col = lane & 15, inner = (lane >> 4) * 8;
-  const int q = ((len + P - 1) / P + 7) & ~7;   // a part's length; the last may be shorter
-  uint32_t src[C];
+// 4 NA outputs from row o0 on, 4 C columns.
+template <class T, int NA, int C>
+__device__ inline void down_unit(const Layer &a, const char *weights, int o0, const int32_t *pairs, int count, int lo,
+                                 int len, v4f *mine) {
+  const int lane = lane_id(), place = Parts<4>::place();
+  uint32_t row[NA], src[C];
   int pair[C];
 #pragma unroll
+  for (int i = 0; i < NA; ++i) row[i] = ((uint32_t)imin(o0 + 4 * i + lane % 4, a.H - 1) * a.I + place) * 2u;
+#pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int at = c * R + col % R;
+    const int at = c * 4 + lane % 4;
     pair[c] = pairs[at < count ? at : 0];
-    src[c] = ((uint32_t)pair[c] * (uint32_t)a.I + lo + col / R * q + inner) * 2u;
+    src[c] = ((uint32_t)pair[c] * (uint32_t)a.I + place) * 2u;
     if (at >= count) pair[c] = -1;
   }
   const char *cols = static_cast<const char *>(a.hidden);
-  const uint32_t rows[1] = {row + (lo + col / R * q + inner) * 2u};
-  v4f d[1][C] = {};
-  const int last = len - (P - 1) * q;   // may be negative for short axes
-  const int my = imin(q, len - col / R * q);
-  constexpr int S = C <= 2 ? 4 : 2;
-  const int safe = last > 0 ? last / (32 * S) * (32 * S) : 0;
-  stream<T, 1, S>(weights, rows, cols, src, safe, 0, 1, blockIdx.x / 8, d);
-  for (int k = safe; k < q; k += 32) {
-    const bool in = k + inner < my;
-#pragma unroll
-    for (int c = 0; c < C; ++c) d[0][c] = mfma<T>(load16(weights + k * 2, rows[0], in), load16(cols + k * 2, src[c], in), d[0][c]);
-  }
-  // column l % 16 of part col / R, rows (l / 16) * 4 + 0..3 of part (l / 16) * 4 / R
-  const bool keep = (lane >> 4) * 4 / R == col / R;
+  v4f d[NA][C] = {};
+  // four steps (512 elements) in flight, then two, then one
+  constexpr int kLong = 4 * Parts<4>::kStep;
+  const int most = len / kLong * kLong;
+  if (C == 1) stream<T, 4, 4>(weights + lo * 2, row, cols + lo * 2, src, most, 0, 1, blockIdx.x / 8, d);
+  const int done = C == 1 ? most : 0;
+  stream<T, 4, 2>(weights + (lo + done) * 2, row, cols + (lo + done) * 2, src, len - done, 0, 1, 0, d);
+  // part p's sums of outputs 4 i + 0..3 and column `token`
+  const int p = lane >> 4, of = lane % kTile / 4;
 #pragma unroll
   for (int c = 0; c < C; ++c)
-    if (keep && pair[c] >= 0) {
-      v4f *to = mine + pair[c] / a.r.k * 4 + (lane >> 4);
-      *to = *to + a.weights[pair[c]] * d[0][c];
+    if (p == of && pair[c] >= 0) {
+      v4f *to = mine + (pair[c] / a.r.k * 4 + p) * NA;
+#pragma unroll
+      for (int i = 0; i < NA; ++i) to[i] = to[i] + a.weights[pair[c]] * d[i][c];
     }
 }
 
-template <class T, int P, int MC>
-__global__ __launch_bounds__(64 * kDownWaves) void down_kernel(Layer a) {
-  extern __shared__ v4f sums[];   // [kDownWaves][T][4]: the 16 rows of every token, by wave
-  constexpr int R = kTile / P;
-  const int lane = lane_id(), wave = uniform_i32(threadIdx.x >> 6);
+// The products with `down` and the weighted sum in one, for few pairs: a
+// workgroup has 4 NA outputs of every token; its waves take the units (an
+// expert, a part of the inner axis) in turn, each into LDS sums of its own.
+template <class T, int NA>
+__global__ __launch_bounds__(64 * kDownWaves, 3) void down_kernel(Layer a) {
+  extern __shared__ v4f sums[];   // [kDownWaves][T][4 parts][NA]
+  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), size = a.T * 4 * NA;
   const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = threadIdx.x; i < kDownWaves * a.T * 4; i += 64 * kDownWaves) sums[i] = zero;
+  for (int i = threadIdx.x; i < kDownWaves * size; i += 64 * kDownWaves) sums[i] = zero;
   __syncthreads();
   int active = lane < (a.r.E + 31) / 32 ? __popc(a.lists.active[lane]) : 0;
   active = readlane_i32(wave_incl_scan(active), 63);
   // parts of the axis so that every wave has a unit
   int parts = 1;
   while (parts < kDownWaves && active * parts < kDownWaves) parts *= 2;
-  const int len = ((a.I + parts - 1) / parts + 31) & ~31;
-  const int o = imin(blockIdx.x * R + (lane & 15) % R, a.H - 1);
-  v4f *mine = sums + wave * a.T * 4;
+  const int len = ((a.I + parts - 1) / parts + 127) & ~127;
+  v4f *mine = sums + wave * size;
   for (int unit = wave; unit < active * parts; unit += kDownWaves) {
     const int e = nth_active(a, unit / parts), lo = unit % parts * len;
     if (lo >= a.I) continue;
     const int count = a.lists.count[e], m = imin(len, a.I - lo);
     const int32_t *pairs = a.lists.pairs + (int64_t)e * a.T;
     const char *w = static_cast<const char *>(a.down) + (int64_t)(a.slot ? a.slot[e] : e) * a.H * a.I * 2;
-    const uint32_t row = (uint32_t)o * (uint32_t)a.I * 2u;
-    for (int at = 0; at < count; at += MC * R) {
-      const int left = imin(count - at, MC * R), cols = (left + R - 1) / R;
-      if (MC == 1 || cols <= 1) down_unit<T, P, 1>(a, w, row, pairs + at, left, lo, m, mine);
-      else if (MC == 2 || cols <= 2) down_unit<T, P, MC < 2 ? 1 : 2>(a, w, row, pairs + at, left, lo, m, mine);
-      else down_unit<T, P, MC < 4 ? 1 : 4>(a, w, row, pairs + at, left, lo, m, mine);
-    }
+    const int o0 = blockIdx.x * 4 * NA;
+    if (count <= 4) down_unit<T, NA, 1>(a, w, o0, pairs, count, lo, m, mine);
+    else
+      for (int at = 0; at < count; at += 8) down_unit<T, NA, 2>(a, w, o0, pairs + at, count - at, lo, m, mine);
     wave_sync();
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < a.T * (R / 4); i += 64 * kDownWaves) {
-    const int t = i / (R / 4), at = i % (R / 4), row = blockIdx.x * R + at * 4;
+  for (int i = threadIdx.x; i < a.T * NA; i += 64 * kDownWaves) {
+    const int t = i / NA, at = i % NA, row = (blockIdx.x * NA + at) * 4;
     v4f s = zero;
 #pragma unroll
     for (int w = 0; w < kDownWaves; ++w)
 #pragma unroll
-      for (int p = 0; p < P; ++p) s += sums[(w * a.T + t) * 4 + p * (R / 4) + at];
+      for (int p = 0; p < 4; ++p) s += sums[w * size + (t * 4 + p) * NA + at];
     if (row >= a.H) continue;
     T out[4];
 #pragma unroll
@@ -561,20 +598,16 @@ int enqueue_experts(const Layer &a, hipStream_t st) {
   return enqueue_experts<T, Up, kMany>(a, st);
 }
 
-template <class T, int P>
-int enqueue_down_parts(const Layer &a, int cols, hipStream_t st) {
-  const dim3 grid((a.H + kTile / P - 1) / (kTile / P)), block(64 * kDownWaves);
-  const size_t lds = kDownWaves * a.T * 4 * sizeof(v4f);
-  if (cols <= 1) hipLaunchKernelGGL((down_kernel<T, P, 1>), grid, block, lds, st, a);
-  else if (cols <= 2) hipLaunchKernelGGL((down_kernel<T, P, 2>), grid, block, lds, st, a);
-  else hipLaunchKernelGGL((down_kernel<T, P, 4>), grid, block, lds, st, a);
+template <class T, int NA>
+int enqueue_down_rows(const Layer &a, hipStream_t st) {
+  hipLaunchKernelGGL((down_kernel<T, NA>), dim3((a.H + 4 * NA - 1) / (4 * NA)), dim3(64 * kDownWaves),
+                     kDownWaves * a.T * 4 * NA * sizeof(v4f), st, a);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
 template <class T>
-int enqueue_down(const Layer &a, int cols, hipStream_t st) {
-  if (a.H >= 16 * 512) return enqueue_down_parts<T, 1>(a, cols, st);
-  return enqueue_down_parts<T, 2>(a, cols, st);
+int enqueue_down(const Layer &a, hipStream_t st) {
+  return a.H <= 1024 ? enqueue_down_rows<T, 1>(a, st) : enqueue_down_rows<T, 2>(a, st);
 }
 
 template <class T>
@@ -587,6 +620,15 @@ int enqueue(const Layer &a, hipStream_t st) {
   else if (cols <= 4) hipLaunchKernelGGL((gate_kernel<T, 4>), gg, gb, 0, st, a);
   else hipLaunchKernelGGL((gate_kernel<T, 8>), gg, gb, 0, st, a);
   if (!launched()) return TOPOEP_EHIP;
+  const int experts = imin(imin(a.T * a.r.k, E), a.L), tiles = (a.I + 7) / 8;
+  if (a.T == 1 && E <= 256 && (int64_t)experts * tiles < 2048 && (int64_t)experts * a.H * a.I <= 1 << 25 && a.r.k <= 16) {
+    const dim3 grid((unsigned)experts * tiles), block(64 * kExpertWaves);
+    if (E <= 64) hipLaunchKernelGGL((one_up_kernel<T, 1>), grid, block, 0, st, a, tiles);
+    else if (E <= 128) hipLaunchKernelGGL((one_up_kernel<T, 2>), grid, block, 0, st, a, tiles);
+    else hipLaunchKernelGGL((one_up_kernel<T, 4>), grid, block, 0, st, a, tiles);
+    if (!launched()) return TOPOEP_EHIP;
+    return enqueue_down<T>(a, st);
+  }
   const dim3 rg((a.T + 3) / 4), rb(256);
   if (E <= 64) hipLaunchKernelGGL((few_route_kernel<1>), rg, rb, 0, st, a);
   else if (E <= 128) hipLaunchKernelGGL((few_route_kernel<2>), rg, rb, 0, st, a);
@@ -596,8 +638,7 @@ int enqueue(const Layer &a, hipStream_t st) {
   if (!launched()) return TOPOEP_EHIP;
   int rc = enqueue_experts<T, true>(a, st);
   if (rc != TOPOEP_OK) return rc;
-  const int experts = imin(imin(a.T * a.r.k, E), a.L);
-  if (a.T * a.r.k <= 16 && (int64_t)experts * a.H * a.I <= 1 << 25) return enqueue_down<T>(a, cols, st);
+  if (a.T * a.r.k <= 16 && (int64_t)experts * a.H * a.I <= 1 << 25) return enqueue_down<T>(a, st);
   rc = enqueue_experts<T, false>(a, st);
   if (rc != TOPOEP_OK) return rc;
   hipLaunchKernelGGL((combine_kernel<T>), dim3((a.H + 1023) / 1024, a.T), dim3(256), 0, st, a);

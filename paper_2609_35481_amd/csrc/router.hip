@@ -6,6 +6,8 @@ namespace {
 
 using namespace topoep_dev;
 
+typedef int v4i __attribute__((ext_vector_type(4)));
+
 constexpr int kThreads = 256;
 
 struct Route {
@@ -318,8 +320,76 @@ struct RouteBackward {
   int64_t ldg;
 };
 
-// d = gradient of the row's chosen scores lies in LDS by expert while the
-// row's lanes write their elements, and is cleared again after them.
+// The chosen scores' gradients, back through the renormalisation (and the
+// sigmoid): of the logits where only chosen ones count.  KP lanes hold a row's
+// choices; `in`: this lane has one.
+template <int KP>
+__device__ inline float chosen_gradient(const RouterArgs &r, bool in, float xj, float g) {
+  const auto sum_of = [](float v) { return KP == 64 ? row_sum<64>(v) : few_sum<KP>(v); };
+  if (r.sigmoid) {
+    const float s = in ? sigmoid(xj) : 0.0f;
+    if (r.renorm) {
+      const float sum = sum_of(s), mean = sum_of(g * s);
+      g = sum > 0.0f ? (g - mean / sum) / sum : 0.0f;
+    }
+    return g * s * sigmoid(-xj);
+  }
+  const float m = KP == 64 ? row_maxf<64>(xj) : few_max<KP>(xj);
+  const float e = m == -INFINITY ? 0.0f : __expf(xj - m);
+  const float sum = sum_of(e);
+  const float q = sum > 0.0f ? e / sum : 0.0f;
+  return q * (g - sum_of(g * q));
+}
+
+// Where only the chosen logits count, a wave takes `rows` rows at once: KP
+// lanes a row form its choices' gradients, which go into a dense image of the
+// rows in LDS, zero elsewhere; the image is written out in whole lines, and the
+// choices' places are cleared for the next rows.  Bound: memory, the output's
+// lines and those that hold a chosen logit.
+constexpr int kImageBytes = 4096;   // of a wave
+
+template <class T, int KP>
+__global__ __launch_bounds__(kThreads) void route_backward_chosen_kernel(RouteBackward a, int rows) {
+  constexpr int W = 16 / sizeof(T);
+  __shared__ v4i images[kThreads / 64][kImageBytes / 16];
+  const int lane = lane_id(), sub = lane % KP, slot = lane / KP, E = a.r.E;
+  const int wave = uniform_i32(threadIdx.x >> 6);
+  v4i *wide = images[wave];
+  T *image = reinterpret_cast<T *>(wide);
+  for (int i = lane; i < kImageBytes / 16; i += 64) wide[i] = v4i{0, 0, 0, 0};
+  wave_sync();
+  const int64_t every = (int64_t)gridDim.x * (kThreads / 64) * rows;
+  for (int64_t t0 = ((int64_t)blockIdx.x * (kThreads / 64) + wave) * rows; t0 < a.T; t0 += every) {
+    const int live = a.T - t0 < rows ? (int)(a.T - t0) : rows;
+    const bool mine = slot < live && sub < a.r.k;
+    const int64_t t = t0 + (mine ? slot : 0);
+    const int id = mine ? a.ids[t * a.r.k + sub] : -1;
+    const float g = mine ? a.r.scale * a.grad[t * a.r.k + sub] : 0.0f;
+    const bool in = (unsigned)id < (unsigned)E;
+    const float xj = in ? clean_logit(to_float(static_cast<const T *>(a.logits)[t * a.ld + id])) : -INFINITY;
+    const float d = chosen_gradient<KP>(a.r, in, xj, g);
+    if (in) image[slot * E + id] = from_float<T>(d);
+    wave_sync();
+    T *to = static_cast<T *>(a.out) + t0 * a.ldg;
+    if (a.ldg == E) {
+      const int n = live * E;
+      int i = lane * W;
+      for (; i + W <= n; i += 64 * W) __builtin_memcpy(to + i, image + i, 16);
+      if (i < n)
+        for (; i < n; ++i) to[i] = image[i];
+    } else {
+      for (int r = 0; r < live; ++r)
+        for (int i = lane; i < E; i += 64) to[r * a.ldg + i] = image[r * E + i];
+    }
+    wave_sync();
+    if (in) image[slot * E + id] = from_float<T>(0.0f);
+    wave_sync();
+  }
+}
+
+// Softmax scores over every logit: d = gradient of the row's chosen scores lies
+// in LDS by expert while the row's lanes write their elements, and is cleared
+// again after them.
 template <class T, int LPT, int V>
 __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward a) {
   constexpr int kRows = kThreads / LPT;
@@ -329,7 +399,6 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward 
 #pragma unroll
   for (int v = 0; v < V; ++v) d[sub * V + v] = 0.0f;
   wave_sync();
-  const bool whole = !a.r.sigmoid && !a.r.renorm;
   for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < a.T; t0 += (int64_t)gridDim.x * kRows) {
     const int64_t t = t0 + slot;
     const bool live = t < a.T;
@@ -339,48 +408,27 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward 
     const bool in = (unsigned)id < (unsigned)a.r.E;
     const float g = mine ? a.r.scale * a.grad[t * a.r.k + sub] : 0.0f;
     const float xj = in ? clean_logit(to_float(row[id])) : -INFINITY;   // masked: score 0
-    float p[V], back = 0.0f, dj;
-    if (whole) {
-      load_logits<T, V>(row, sub * V, a.r.E, p);
-      float m = p[0];
+    float p[V];
+    load_logits<T, V>(row, sub * V, a.r.E, p);
+    float m = p[0];
 #pragma unroll
-      for (int v = 1; v < V; ++v) m = fmaxf(m, p[v]);
-      m = row_maxf<LPT>(m);
-      float sum = 0.0f;
+    for (int v = 1; v < V; ++v) m = fmaxf(m, p[v]);
+    m = row_maxf<LPT>(m);
+    float sum = 0.0f;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        p[v] = m == -INFINITY ? 0.0f : __expf(p[v] - m);
-        sum += p[v];
-      }
-      sum = row_sum<LPT>(sum);
-      const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-      for (int v = 0; v < V; ++v) p[v] *= inv;
-      back = row_sum<LPT>(in && m != -INFINITY ? g * (__expf(xj - m) * inv) : 0.0f);
-      dj = g;
-    } else if (a.r.sigmoid) {
-      const float s = in ? sigmoid(xj) : 0.0f;
-      dj = g;
-      if (a.r.renorm) {
-        const float sum = row_sum<LPT>(s);
-        const float mean = row_sum<LPT>(g * s);
-        dj = sum > 0.0f ? (g - mean / sum) / sum : 0.0f;
-      }
-      dj *= s * sigmoid(-xj);
-    } else {
-      const float m = row_maxf<LPT>(xj);
-      const float e = m == -INFINITY ? 0.0f : __expf(xj - m);
-      const float sum = row_sum<LPT>(e);
-      const float q = sum > 0.0f ? e / sum : 0.0f;
-      dj = q * (g - row_sum<LPT>(g * q));
+    for (int v = 0; v < V; ++v) {
+      p[v] = m == -INFINITY ? 0.0f : __expf(p[v] - m);
+      sum += p[v];
     }
-    if (in) d[id] = dj;
+    sum = row_sum<LPT>(sum);
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const float back = row_sum<LPT>(in && m != -INFINITY ? g * (__expf(xj - m) * inv) : 0.0f);
+    if (in) d[id] = g;
     wave_sync();
     T out[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const float c = d[sub * V + v];
-      out[v] = from_float<T>(whole ? p[v] * (c - back) : c);
+      out[v] = from_float<T>(p[v] * inv * (d[sub * V + v] - back));
     }
     wave_sync();
     if (in) d[id] = 0.0f;
@@ -483,6 +531,21 @@ int enqueue_route(const Route &a, hipStream_t st) {
   return launch_rows<T, Forward>(r.E, r.k, r.groups > 1 || a.T < 8192, a, a.T, st);
 }
 
+template <class T, int KP>
+int enqueue_chosen(const RouteBackward &a, hipStream_t st) {
+  const int rows = imin(64 / KP, kImageBytes / (a.r.E * (int)sizeof(T)));
+  const int64_t blocks = ((int64_t)a.T + rows * (kThreads / 64) - 1) / (rows * (kThreads / 64));
+  (void)hipGetLastError();
+  hipLaunchKernelGGL((route_backward_chosen_kernel<T, KP>), dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(kThreads),
+                     0, st, a, rows);
+  return hipGetLastError() == hipSuccess ? TOPOEP_OK : TOPOEP_EHIP;
+}
+template <class T>
+int enqueue_backward(const RouteBackward &a, hipStream_t st) {
+  if (!a.r.sigmoid && !a.r.renorm) return launch_rows<T, Backward>(a.r.E, a.r.k, a.T < 8192, a, a.T, st);
+  return a.r.k <= 8 ? enqueue_chosen<T, 8>(a, st) : enqueue_chosen<T, 64>(a, st);
+}
+
 // Bytes from the first row to the end of the last fit a pointer's range.
 bool rows_fit(int T, int64_t ld, int E) { return ld >= E && (T < 2 || ld <= (INT64_MAX / 8 - E) / (T - 1)); }
 
@@ -517,11 +580,10 @@ int topoep_route_backward(const topoep_router *r, const void *logits, int64_t ld
   if (!logits || !ids || !grad_weights || !grad_logits) return TOPOEP_EINVAL;
   RouteBackward a{router_args(r), logits, ld, T, ids, grad_weights, grad_logits, ldg};
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool wide = T < 8192;
   switch (r->dtype) {
-    case TOPOEP_F32: return launch_rows<float, Backward>(a.r.E, a.r.k, wide, a, T, st);
-    case TOPOEP_BF16: return launch_rows<Bf16, Backward>(a.r.E, a.r.k, wide, a, T, st);
-    default: return launch_rows<F16, Backward>(a.r.E, a.r.k, wide, a, T, st);
+    case TOPOEP_F32: return enqueue_backward<float>(a, st);
+    case TOPOEP_BF16: return enqueue_backward<Bf16>(a, st);
+    default: return enqueue_backward<F16>(a, st);
   }
 }
 

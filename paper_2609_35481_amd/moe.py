@@ -12,13 +12,13 @@ current stream, every step runs in the HIP kernels of libtopoep.so.
 """
 from __future__ import annotations
 
-import contextlib
+import array
 import ctypes
 import functools
 
 import torch
 
-from .topoep import OK, TopoepError, _lib, _stream_ptr
+from .topoep import OK, TopoepError, _lib
 
 F32, BF16, F16 = 0, 1, 2
 SOFTMAX, SIGMOID = 0, 1
@@ -100,33 +100,34 @@ def _dense(t, name, shape, dtype, device):
     return t
 
 
-def _on(device):
-    """The library's calls go to the current device: the tensors' own."""
-    if torch.cuda.current_device() != device.index:
+def _stream_of(device):
+    """The current stream of the tensors' device, which has to be the current
+    device: the library's calls go there."""
+    if torch._C._cuda_getDevice() != device.index:
         raise ValueError("the tensors are on %s, the current device is cuda:%d" % (device, torch.cuda.current_device()))
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
-def _on_stream(stream):
-    """What a call allocates belongs to the stream its kernels run on: one
-    named by the caller is made the current one for the call."""
-    if stream is None:
-        return contextlib.nullcontext()
+def _on_stream(stream, call, *args):
+    """call(*args) with a stream named by the caller as the current one: what a
+    call allocates belongs to the stream its kernels run on."""
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)))
-    return torch.cuda.stream(stream)
+    with torch.cuda.stream(stream):
+        return call(*args)
 
 
 def _route(r, logits, bias):
     ld = _rows(logits, "logits")
     T, E = logits.shape
     dev = logits.device
-    _on(dev)
+    stream = _stream_of(dev)
     if bias is not None:
         _dense(bias, "bias", (E,), torch.float32, dev)
     ids = torch.empty((T, r.topk), dtype=torch.int32, device=dev)
     weights = torch.empty((T, r.topk), dtype=torch.float32, device=dev)
     _check(_lib.topoep_route(r, logits.data_ptr(), ld, T, bias.data_ptr() if bias is not None else None,
-                             ids.data_ptr(), weights.data_ptr(), _stream_ptr(None, dev)), "topoep_route")
+                             ids.data_ptr(), weights.data_ptr(), stream), "topoep_route")
     return ids, weights
 
 
@@ -134,12 +135,12 @@ def _backward(r, logits, ids, grad_weights):
     ld = _rows(logits, "logits")
     T, E = logits.shape
     dev = logits.device
-    _on(dev)
+    stream = _stream_of(dev)
     _dense(ids, "ids", (T, r.topk), torch.int32, dev)
     _dense(grad_weights, "grad_weights", (T, r.topk), torch.float32, dev)
     out = torch.empty((T, E), dtype=logits.dtype, device=dev)
     _check(_lib.topoep_route_backward(r, logits.data_ptr(), ld, T, ids.data_ptr(), grad_weights.data_ptr(),
-                                      out.data_ptr(), E, _stream_ptr(None, dev)), "topoep_route_backward")
+                                      out.data_ptr(), E, stream), "topoep_route_backward")
     return out
 
 
@@ -165,10 +166,11 @@ def route(logits, k, scoring="softmax", renorm=True, scale=1.0, bias=None, group
     gradient to logits that require one (a bias gets none)."""
     r = router(logits.shape[1] if logits.dim() == 2 else 0, k, logits.dtype, scoring, renorm, scale, groups,
                top_groups)
-    with _on_stream(stream):
-        if torch.is_grad_enabled() and logits.requires_grad:
-            return _Route.apply(logits, bias, r)
-        return _route(r, logits, bias)
+    if stream is not None:
+        return _on_stream(stream, route, logits, k, scoring, renorm, scale, bias, groups, top_groups)
+    if logits.requires_grad and torch.is_grad_enabled():
+        return _Route.apply(logits, bias, r)
+    return _route(r, logits, bias)
 
 
 def route_backward(logits, ids, grad_weights, scoring="softmax", renorm=True, scale=1.0, stream=None):
@@ -176,8 +178,9 @@ def route_backward(logits, ids, grad_weights, scoring="softmax", renorm=True, sc
     type from the weights' [T, k]."""
     r = router(logits.shape[1] if logits.dim() == 2 else 0, ids.shape[1] if ids.dim() == 2 else 0, logits.dtype,
                scoring, renorm, scale)
-    with _on_stream(stream):
-        return _backward(r, logits, ids, grad_weights)
+    if stream is not None:
+        return _on_stream(stream, _backward, r, logits, ids, grad_weights)
+    return _backward(r, logits, ids, grad_weights)
 
 
 def moe_workspace_bytes(H, I, E, L, k, T, dtype=torch.bfloat16) -> int:
@@ -198,14 +201,14 @@ def moe_few(x, gate, up, down, k, scoring="softmax", renorm=True, scale=1.0, bia
 
     workspace: a zero-filled byte tensor kept between calls
     (moe_workspace_bytes; any larger one serves too); None makes one for the call."""
-    with _on_stream(stream):
-        return _few(x, gate, up, down, k, (scoring, renorm, scale, groups, top_groups), bias, expert_slot, workspace)
+    args = (x, gate, up, down, k, (scoring, renorm, scale, groups, top_groups), bias, expert_slot, workspace)
+    return _few(*args) if stream is None else _on_stream(stream, _few, *args)
 
 
 def _few(x, gate, up, down, k, rules, bias, expert_slot, workspace):
     ldx = _rows(x, "x")
     dev, dtype = x.device, x.dtype
-    _on(dev)
+    stream = _stream_of(dev)
     if dtype not in (torch.bfloat16, torch.float16):
         raise TypeError("x must be bfloat16 or float16, not %s" % dtype)
     T, H = x.shape
@@ -234,7 +237,7 @@ def _few(x, gate, up, down, k, rules, bias, expert_slot, workspace):
                                bias.data_ptr() if bias is not None else None,
                                expert_slot.data_ptr() if expert_slot is not None else None, up.data_ptr(),
                                down.data_ptr(), out.data_ptr(), ids.data_ptr(), weights.data_ptr(), ws, max(size, 0),
-                               _stream_ptr(None, dev)), "topoep_moe_few")
+                               stream), "topoep_moe_few")
     return out, ids, weights
 
 
@@ -251,21 +254,23 @@ def _dense_any_order(t):
 
 
 def _grad_set(grads, outs):
-    n = len(grads)
-    table = (Grad * n)()
-    device = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+    """The set as the library takes it (an array of topoep_grad, four 64-bit
+    words each), its length and device."""
+    device = grads[0].get_device() if grads else torch.cuda.current_device()
+    words = []
     for i, g in enumerate(grads):
         o = g if outs is None else outs[i]
-        for t in (g, o):
-            if not t.is_cuda or t.device != device:
-                raise ValueError("tensor %d is on %s, not %s" % (i, t.device, device))
-            if t.dtype not in _TYPES:
-                raise TypeError("tensor %d is %s, not float32, bfloat16 or float16" % (i, t.dtype))
-        if not _dense_any_order(g) or (o is not g and (o.shape != g.shape or o.stride() != g.stride())):
-            raise ValueError("tensor %d must be dense, and its output of the same shape and strides" % i)
-        table[i] = (g.data_ptr(), o.data_ptr(), g.numel(), _TYPES[g.dtype], _TYPES[o.dtype])
-    _on(device)
-    return table, n, device
+        if g.get_device() != device or o.get_device() != device or device < 0:
+            raise ValueError("tensor %d is on %s and %s, the first on %s" % (i, g.device, o.device, grads[0].device))
+        kind, to = _TYPES.get(g.dtype), _TYPES.get(o.dtype)
+        if kind is None or to is None:
+            raise TypeError("tensor %d is %s, its output %s: float32, bfloat16 or float16" % (i, g.dtype, o.dtype))
+        if o is not g and o.shape != g.shape:
+            raise ValueError("tensor %d and its output differ in shape" % i)
+        if not (g.is_contiguous() and o.is_contiguous()) and not (_dense_any_order(g) and o.stride() == g.stride()):
+            raise ValueError("tensor %d must be dense, and its output of the same strides" % i)
+        words += (g.data_ptr(), o.data_ptr(), g.numel(), kind | to << 32)
+    return array.array("q", words), len(grads), torch.device("cuda", device)
 
 
 def _order(ord):
@@ -281,20 +286,17 @@ def grads_workspace_bytes(count) -> int:
     return out.value
 
 
-def _grads_workspace(count, device):
-    ws = torch.empty(grads_workspace_bytes(count) + 256, dtype=torch.uint8, device=device)
-    return ws, (ws.data_ptr() + 255) & ~255
-
-
 def grad_norm(grads, scale=1.0, ord=2, stream=None):
     """Enqueue topoep_grad_norm: scale times the 2-norm (or, with ord inf, the
     largest magnitude) over a list of tensors, as a float32 scalar tensor."""
+    if stream is not None:
+        return _on_stream(stream, grad_norm, grads, scale, ord)
     table, n, dev = _grad_set(grads, None)
-    with _on_stream(stream):
-        norm = torch.empty((), dtype=torch.float32, device=dev)
-        ws, ptr = _grads_workspace(n, dev)
-        _check(_lib.topoep_grad_norm(table, n, scale, _order(ord), norm.data_ptr(), ptr, grads_workspace_bytes(n),
-                                     _stream_ptr(None, dev)), "topoep_grad_norm")
+    queue = _stream_of(dev)
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    ws = torch.empty(grads_workspace_bytes(n), dtype=torch.uint8, device=dev)   # torch aligns to 512 bytes
+    _check(_lib.topoep_grad_norm(table.buffer_info()[0], n, scale, _order(ord), norm.data_ptr(), ws.data_ptr(),
+                                 ws.numel(), queue), "topoep_grad_norm")
     return norm
 
 
@@ -304,16 +306,17 @@ def clip_grads(grads, max_norm, scale=1.0, ord=2, outs=None, norm=None, stream=N
     of the three types); returns the norm.  norm: a given one (float32 scalar tensor,
     already scaled), say of a whole group of ranks; None takes this set's.  A norm that
     is not finite leaves every tensor as it is."""
+    if stream is not None:
+        return _on_stream(stream, clip_grads, grads, max_norm, scale, ord, outs, norm)
     if outs is not None and len(outs) != len(grads):
         raise ValueError("%d outs for %d grads" % (len(outs), len(grads)))
     table, n, dev = _grad_set(grads, outs)
-    if norm is not None:
+    queue = _stream_of(dev)
+    total = torch.empty((), dtype=torch.float32, device=dev) if norm is None else \
         _dense(norm, "norm", (), torch.float32, dev)
-    with _on_stream(stream):
-        total = torch.empty((), dtype=torch.float32, device=dev) if norm is None else norm
-        ws, ptr = _grads_workspace(n, dev)
-        _check(_lib.topoep_clip_grads(table, n, scale, _order(ord), max_norm,
-                                      norm.data_ptr() if norm is not None else None,
-                                      total.data_ptr() if norm is None else None, ptr, grads_workspace_bytes(n),
-                                      _stream_ptr(None, dev)), "topoep_clip_grads")
+    ws = torch.empty(grads_workspace_bytes(n), dtype=torch.uint8, device=dev)
+    _check(_lib.topoep_clip_grads(table.buffer_info()[0], n, scale, _order(ord), max_norm,
+                                  total.data_ptr() if norm is not None else None,
+                                  total.data_ptr() if norm is None else None, ws.data_ptr(), ws.numel(), queue),
+           "topoep_clip_grads")
     return total
