@@ -8,17 +8,18 @@
                           clip
 
 Argument checks and marshalling only: torch provides device memory and the
-current stream, every step runs in the HIP kernels of libtopoep.so.
+current stream, every step runs in the HIP kernels of libtopoep.so.  Importing this module fails
+loudly when the library, or _tensors (which reads lists of tensors), has not been built.
 """
 from __future__ import annotations
 
-import array
 import ctypes
 import functools
 
 import torch
 
 from .topoep import OK, TopoepError, _lib
+from . import _tensors
 
 F32, BF16, F16 = 0, 1, 2
 SOFTMAX, SIGMOID = 0, 1
@@ -241,36 +242,11 @@ def _few(x, gate, up, down, k, rules, bias, expert_slot, workspace):
     return out, ids, weights
 
 
-def _dense_any_order(t):
-    """Dense memory in whatever order of axes, each element once."""
-    if t.is_contiguous():
-        return True
-    size = 1
-    for n, s in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n != 1), key=lambda v: v[1]):
-        if s != size:
-            return False
-        size *= n
-    return True
-
-
 def _grad_set(grads, outs):
-    """The set as the library takes it (an array of topoep_grad, four 64-bit
-    words each), its length and device."""
-    device = grads[0].get_device() if grads else torch.cuda.current_device()
-    words = []
-    for i, g in enumerate(grads):
-        o = g if outs is None else outs[i]
-        if g.get_device() != device or o.get_device() != device or device < 0:
-            raise ValueError("tensor %d is on %s and %s, the first on %s" % (i, g.device, o.device, grads[0].device))
-        kind, to = _TYPES.get(g.dtype), _TYPES.get(o.dtype)
-        if kind is None or to is None:
-            raise TypeError("tensor %d is %s, its output %s: float32, bfloat16 or float16" % (i, g.dtype, o.dtype))
-        if o is not g and o.shape != g.shape:
-            raise ValueError("tensor %d and its output differ in shape" % i)
-        if not (g.is_contiguous() and o.is_contiguous()) and not (_dense_any_order(g) and o.stride() == g.stride()):
-            raise ValueError("tensor %d must be dense, and its output of the same strides" % i)
-        words += (g.data_ptr(), o.data_ptr(), g.numel(), kind | to << 32)
-    return array.array("q", words), len(grads), torch.device("cuda", device)
+    """The set as the library takes it (topoep_grad after topoep_grad), its
+    length and device."""
+    table, device = _tensors.pack(grads, outs)
+    return table, len(grads), torch.device("cuda", device if device >= 0 else torch.cuda.current_device())
 
 
 def _order(ord):
@@ -295,7 +271,7 @@ def grad_norm(grads, scale=1.0, ord=2, stream=None):
     queue = _stream_of(dev)
     norm = torch.empty((), dtype=torch.float32, device=dev)
     ws = torch.empty(grads_workspace_bytes(n), dtype=torch.uint8, device=dev)   # torch aligns to 512 bytes
-    _check(_lib.topoep_grad_norm(table.buffer_info()[0], n, scale, _order(ord), norm.data_ptr(), ws.data_ptr(),
+    _check(_lib.topoep_grad_norm(table, n, scale, _order(ord), norm.data_ptr(), ws.data_ptr(),
                                  ws.numel(), queue), "topoep_grad_norm")
     return norm
 
@@ -308,14 +284,12 @@ def clip_grads(grads, max_norm, scale=1.0, ord=2, outs=None, norm=None, stream=N
     is not finite leaves every tensor as it is."""
     if stream is not None:
         return _on_stream(stream, clip_grads, grads, max_norm, scale, ord, outs, norm)
-    if outs is not None and len(outs) != len(grads):
-        raise ValueError("%d outs for %d grads" % (len(outs), len(grads)))
     table, n, dev = _grad_set(grads, outs)
     queue = _stream_of(dev)
     total = torch.empty((), dtype=torch.float32, device=dev) if norm is None else \
         _dense(norm, "norm", (), torch.float32, dev)
     ws = torch.empty(grads_workspace_bytes(n), dtype=torch.uint8, device=dev)
-    _check(_lib.topoep_clip_grads(table.buffer_info()[0], n, scale, _order(ord), max_norm,
+    _check(_lib.topoep_clip_grads(table, n, scale, _order(ord), max_norm,
                                   total.data_ptr() if norm is not None else None,
                                   total.data_ptr() if norm is None else None, ws.data_ptr(), ws.numel(), queue),
            "topoep_clip_grads")
