@@ -167,8 +167,112 @@ __device__ inline float few_sum(float v) {
   return v;
 }
 
+// The groups' largest keys in LDS (`best`, a word a group), where groups and
+// lanes need not fit.
+template <int LPT, int V, class Key>
+__device__ inline void best_of_groups(const RouterArgs &r, int sub, uint32_t *best, const Key &key) {
+  const int base = sub * V, m = r.per_group;
+  for (int q = sub; q < r.groups; q += LPT) best[q] = 0;
+  wave_sync();
+  int g = base / m, pos = base - g * m;
+  float run = -INFINITY;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    run = fmaxf(run, key(v));   // passes over a NaN key, which counts as -inf
+    if (++pos == m || v == V - 1) {
+      if (g < r.groups) atomicMax(&best[g], key_word(run));
+      run = -INFINITY;
+      pos = 0;
+      ++g;
+    }
+  }
+  wave_sync();
+}
+
+// Up to eight open groups, as a list of (key, group).
+template <int LPT, bool Bias>
+__device__ inline void list_groups(const RouterArgs &r, int sub, const uint32_t *best, double (&l)[8]) {
+  double o[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) l[i] = -0x1p200;
+  for (int q0 = 0; q0 < r.groups; q0 += 8 * LPT) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int q = q0 + i * LPT + sub;
+      const uint32_t w = best[q < r.groups ? q : 0];
+      const float k = __uint_as_float(w & 0x80000000u ? w ^ 0x80000000u : ~w);
+      o[i] = entry<Bias>(k, (uint32_t)q ^ kIdMask);
+      o[i] = q < r.groups ? o[i] : -0x1p200;
+    }
+    sort(o);
+    merge(l, o);
+  }
+  merge_row<LPT>(l);
+}
+
+// Any number of open groups, a bit each: counted against each other.
+template <int LPT>
+__device__ inline uint64_t count_groups(const RouterArgs &r, int sub, const uint32_t *best) {
+  uint64_t mask = 0;
+  for (int q = sub; q < r.groups; q += LPT) {
+    const uint32_t mine = best[q];
+    int above = 0;
+    for (int o = 0; o < r.groups; ++o) {
+      const uint32_t w = best[o];
+      above += w > mine || (w == mine && o < q) ? 1 : 0;
+    }
+    mask |= above < r.top_groups ? 1ull << q : 0ull;
+  }
+  if (LPT > 1) mask |= dpp_mov64<0xB1>(mask);
+  if (LPT > 2) mask |= dpp_mov64<0x4E>(mask);
+  if (LPT > 4) mask |= dpp_mov64<0x141>(mask);
+  if (LPT > 8) mask |= dpp_mov64<0x140>(mask);
+  return mask;
+}
+
+// The row's list from the experts of its open groups alone, which are read
+// again: candidate c is expert c % m of open group c / m.  `chosen`: eight
+// words of LDS of the row's own.
+template <class T, int LPT, bool Bias>
+__device__ inline void list_candidates(const Route &a, const T *row, int sub, const double (&groups)[8], uint32_t *chosen,
+                                       double (&l)[8]) {
+  if (sub == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) chosen[i] = (uint32_t)(entry_id(groups[i]) * a.r.per_group);
+  }
+  wave_sync();
+  const int m = a.r.per_group, n = a.r.top_groups * m;
+  const uint32_t inverse = ((1u << 20) + (uint32_t)m - 1) / (uint32_t)m;   // exact: c m < 2^20
+  for (int c0 = 0; c0 < n; c0 += 8 * LPT) {
+    double o[8];
+    T raw[8];
+    float bias[8];
+    uint32_t id[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t c = (uint32_t)imin(c0 + i * LPT + sub, n - 1), j = c * inverse >> 20;
+      id[i] = chosen[j] + (c - j * (uint32_t)m);
+      raw[i] = row[id[i]];
+      bias[i] = Bias ? a.bias[id[i]] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = clean_logit(to_float(raw[i]));
+      o[i] = entry<Bias>(Bias ? x + bias[i] : x, id[i] ^ kIdMask);
+      o[i] = c0 + i * LPT + sub < n ? o[i] : -0x1p200;
+    }
+    sort(o);
+    if (c0 == 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) l[i] = o[i];
+    } else {
+      merge(l, o);
+    }
+  }
+}
+
 // GL: groups a lane holds (a group may also span 2, 4 or 8 lanes: GL = 1); 0: no
-// groups.  Places beyond E hold masked logits of ids that no expert has: any
+// groups; -1: groups of any size.  Places beyond E hold masked logits of ids that no expert has: any
 // expert comes before them.
 template <class T, int LPT, int V, int K, int GL, bool Bias>
 __global__ __launch_bounds__(kThreads) void route_list_kernel(Route a) {
@@ -189,58 +293,83 @@ __global__ __launch_bounds__(kThreads) void route_list_kernel(Route a) {
     }
   }
   const auto key = [&](int v) { return Bias ? x[v] + b[Bias ? v : 0] : x[v]; };
-  bool open[GL > 0 ? GL : 1];
-  if constexpr (GL > 0) {
-    // the groups' largest keys, as a list of (key, group)
-    constexpr int M = V / GL;
-    const int span = a.r.per_group / V;   // lanes a group spans, where it spans any
-    double best[8];
-    int mine[GL];
+  double l[K];
+  uint64_t lane_open = ~0ull;   // bit v: expert base + v's group is open
+  bool listed = false;          // l is made already
+  if constexpr (GL != 0) {
+    __shared__ uint32_t chosen[kRows][8];
+    double groups[8];
+    const int m = a.r.per_group;
+    const bool few = a.r.top_groups <= 8;
+    uint64_t mask = 0;
+    if constexpr (GL < 0) {
+      __shared__ uint32_t best[kRows][64];
+      best_of_groups<LPT, V>(a.r, sub, best[threadIdx.x / LPT], key);
+      if (few) list_groups<LPT, Bias>(a.r, sub, best[threadIdx.x / LPT], groups);
+      else mask = count_groups<LPT>(a.r, sub, best[threadIdx.x / LPT]);
+    } else {
+      constexpr int M = V / GL;
+      const int span = m / V;   // lanes a group spans, where it spans any
 #pragma unroll
-    for (int i = 0; i < 8; ++i) best[i] = -0x1p200;
+      for (int i = 0; i < 8; ++i) groups[i] = -0x1p200;
 #pragma unroll
-    for (int g = 0; g < GL; ++g) {
-      float top = -INFINITY;
+      for (int g = 0; g < GL; ++g) {
+        float top = -INFINITY;
 #pragma unroll
-      for (int m = 0; m < M; ++m) top = fmaxf(top, key(g * M + m));   // passes over a NaN key, which counts as -inf
-      if (GL == 1) {
-        if (span > 1) top = fmaxf(top, dpp_movf<0xB1>(top));
-        if (span > 2) top = fmaxf(top, dpp_movf<0x4E>(top));
-        if (span > 4) top = fmaxf(top, dpp_movf<0x141>(top));
+        for (int v = 0; v < M; ++v) top = fmaxf(top, key(g * M + v));   // passes over a NaN key, which counts as -inf
+        if (GL == 1) {
+          if (span > 1) top = fmaxf(top, dpp_movf<0xB1>(top));
+          if (span > 2) top = fmaxf(top, dpp_movf<0x4E>(top));
+          if (span > 4) top = fmaxf(top, dpp_movf<0x141>(top));
+        }
+        const int mine = GL == 1 && span > 1 ? sub / span : sub * GL + g;
+        if (mine < a.r.groups && (GL > 1 || span <= 1 || sub % span == 0))
+          groups[g] = entry<Bias>(top, (uint32_t)mine ^ kIdMask);
       }
-      mine[g] = GL == 1 && span > 1 ? sub / span : sub * GL + g;
-      if (mine[g] < a.r.groups && (GL > 1 || span <= 1 || sub % span == 0))
-        best[g] = entry<Bias>(top, (uint32_t)mine[g] ^ kIdMask);
+      sort(groups);
+      merge_row<LPT>(groups);
     }
-    sort(best);
-    merge_row<LPT>(best);
+    if (few && 2 * a.r.top_groups * m <= E) {   // half of the experts or fewer are left
+      list_candidates<T, LPT, Bias>(a, row, sub, groups, chosen[threadIdx.x / LPT], l);
+      listed = true;
+    } else {
+      if (few) {
 #pragma unroll
-    for (int g = 0; g < GL; ++g) {
-      open[g] = false;
+        for (int i = 0; i < 8; ++i) mask |= i < a.r.top_groups ? 1ull << entry_id(groups[i]) : 0ull;
+      }
+      lane_open = 0;
+      int g = base / m, pos = base - g * m;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) open[g] |= i < a.r.top_groups && entry_id(best[i]) == mine[g];
+      for (int v = 0; v < V; ++v) {
+        lane_open |= (g < a.r.groups ? (mask >> g) & 1 : 0ull) << v;
+        if (++pos == m) {
+          pos = 0;
+          ++g;
+        }
+      }
     }
   }
-  double l[K];
+  if (GL == 0 || !listed) {
 #pragma unroll
-  for (int c = 0; c < (V + K - 1) / K; ++c) {
-    double o[K];
+    for (int c = 0; c < (V + K - 1) / K; ++c) {
+      double o[K];
 #pragma unroll
-    for (int i = 0; i < K; ++i) {
-      const int v = c * K + i;
-      if (v >= V) {
-        o[i] = -0x1p200;
-        continue;
+      for (int i = 0; i < K; ++i) {
+        const int v = c * K + i;
+        if (v >= V) {
+          o[i] = -0x1p200;
+          continue;
+        }
+        o[i] = entry<Bias>(key(v < V ? v : 0), anti ^ (uint32_t)v);
+        if (GL != 0) o[i] = (lane_open >> (v < V ? v : 0)) & 1 ? o[i] : -0x1p200;
       }
-      o[i] = entry<Bias>(key(v < V ? v : 0), anti ^ (uint32_t)v);
-      if (GL > 0) o[i] = open[GL > 0 ? (v < V ? v : 0) / (V / (GL > 0 ? GL : 1)) : 0] ? o[i] : -0x1p200;
-    }
-    sort(o);
-    if (c == 0) {
+      sort(o);
+      if (c == 0) {
 #pragma unroll
-      for (int i = 0; i < K; ++i) l[i] = o[i];
-    } else {
-      merge(l, o);
+        for (int i = 0; i < K; ++i) l[i] = o[i];
+      } else {
+        merge(l, o);
+      }
     }
   }
   merge_row<LPT>(l);
@@ -499,15 +628,15 @@ int enqueue_groups(const Route &a, int per_lane, hipStream_t st) {
   if (per_lane == 2) return enqueue_list<T, LPT, 32, 8, 2>(a, st);
   return enqueue_list<T, LPT, 32, 8, 1>(a, st);
 }
-template <class T, int K>
+template <class T, int K, int GL>
 int enqueue_lists(const Route &a, hipStream_t st) {
-  if (a.r.E <= 16) return enqueue_list<T, 4, 4, K, 0>(a, st);
-  if (a.r.E <= 32) return enqueue_list<T, 4, 8, K, 0>(a, st);
-  if (a.r.E <= 64) return enqueue_list<T, 4, 16, K, 0>(a, st);
-  if (a.r.E <= 128) return enqueue_list<T, 4, 32, K, 0>(a, st);
-  if (a.r.E <= 256) return enqueue_list<T, 8, 32, K, 0>(a, st);
-  if (a.r.E <= 512) return enqueue_list<T, 16, 32, K, 0>(a, st);
-  return enqueue_list<T, 16, 64, K, 0>(a, st);
+  if (a.r.E <= 16) return enqueue_list<T, 4, 4, K, GL>(a, st);
+  if (a.r.E <= 32) return enqueue_list<T, 4, 8, K, GL>(a, st);
+  if (a.r.E <= 64) return enqueue_list<T, 4, 16, K, GL>(a, st);
+  if (a.r.E <= 128) return enqueue_list<T, 4, 32, K, GL>(a, st);
+  if (a.r.E <= 256) return enqueue_list<T, 8, 32, K, GL>(a, st);
+  if (a.r.E <= 512) return enqueue_list<T, 16, 32, K, GL>(a, st);
+  return enqueue_list<T, 16, 64, K, GL>(a, st);
 }
 
 // Groups a lane of 32 experts holds whole (1, 2, 4; 1 also where a group is 1, 2, 4
@@ -521,13 +650,14 @@ int groups_of_lane(const RouterArgs &r) {
 template <class T>
 int enqueue_route(const Route &a, hipStream_t st) {
   const RouterArgs &r = a.r;
-  if (r.k <= 8 && r.groups == 1) return r.k <= 4 ? enqueue_lists<T, 4>(a, st) : enqueue_lists<T, 8>(a, st);
+  if (r.k <= 8 && r.groups == 1) return r.k <= 4 ? enqueue_lists<T, 4, 0>(a, st) : enqueue_lists<T, 8, 0>(a, st);
   const int per_lane = groups_of_lane(r);
   if (r.k <= 8 && r.top_groups <= 8 && r.E > 64 && r.E <= 512 && per_lane > 0) {
     if (r.E <= 128) return enqueue_groups<T, 4>(a, per_lane, st);
     if (r.E <= 256) return enqueue_groups<T, 8>(a, per_lane, st);
     return enqueue_groups<T, 16>(a, per_lane, st);
   }
+  if (r.k <= 8) return enqueue_lists<T, 8, -1>(a, st);
   return launch_rows<T, Forward>(r.E, r.k, r.groups > 1 || a.T < 8192, a, a.T, st);
 }
 
