@@ -243,7 +243,7 @@ __global__ __launch_bounds__(256) void few_route_kernel(Layer a) {
     if (slot_of(a, e) >= 0) {
       const int at = atomicAdd(&a.lists.count[e], 1);
       a.lists.pairs[(int64_t)e * a.T + at] = t * a.r.k + sub;
-      if (at == 0) atomicOr(&a.lists.active[e >> 5], 1u << (e & 31));
+      atomicOr(&a.lists.active[e >> 5], 1u << (e & 31));   // each pair's: none waits for the count
     }
   }
 }
@@ -272,24 +272,24 @@ constexpr int kExpertWaves = 4;
 // of 2048 elements is in flight at once.
 constexpr int run_steps(int P, int C, int KS) { return P == 4 ? (C == 1 ? (KS > 1 ? 4 : 2) : 1) : C <= 4 ? 2 : 1; }
 
-// A tile of 16 M rows of one expert against 16 / P * C of its pairs.  Rows: 8 M
-// hidden units' gate rows and their up rows (Up), or 16 M outputs.  KS = 1: the
+// A tile of 16 rows of one expert against 16 / P * C of its pairs.  Rows: 8
+// hidden units' gate rows and their up rows (Up), or 16 outputs.  KS = 1: the
 // tile is the wave's own; KS = kExpertWaves: the workgroup's waves share it, each
 // with its part of the runs.
-// How many pairs an expert has, about; any number is served by each.
-enum Load { kOne, kFew, kMany };   // at most 4; mostly up to 16; more
+// How many pairs an expert has, about; kFew serves any number.
+enum Load { kOne, kFew };   // at most 4; mostly up to 16
 
-template <class T, bool Up, int P, int M, int C, int KS, int Kind>
+template <class T, bool Up, int P, int C, int KS, int Kind>
 __device__ inline void expert_tile(const Layer &a, const char *weights, const int32_t *pairs, int count, int tile,
                                    v4f (*part)[64]) {
-  constexpr int R = Parts<P>::kCols, kRows = Up ? 8 * M : 16 * M, NA = P * M;
+  constexpr int R = Parts<P>::kCols, kRows = Up ? 8 : 16;
   const int lane = lane_id(), wave = uniform_i32(threadIdx.x >> 6), place = Parts<P>::place(), at0 = tile * kRows;
   const int n = Up ? a.H : a.I;
-  uint32_t row[NA], src[C];
+  uint32_t row[P], src[C];
 #pragma unroll
-  for (int i = 0; i < NA; ++i) {
+  for (int i = 0; i < P; ++i) {
     const int r = i * R + lane % R;
-    row[i] = ((uint32_t)(Up ? r / (8 * M) * a.I + imin(at0 + r % (8 * M), a.I - 1) : imin(at0 + r, a.H - 1)) * n + place) * 2u;
+    row[i] = ((uint32_t)(Up ? (r >> 3) * a.I + imin(at0 + (r & 7), a.I - 1) : imin(at0 + r, a.H - 1)) * n + place) * 2u;
   }
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -298,13 +298,13 @@ __device__ inline void expert_tile(const Layer &a, const char *weights, const in
     src[c] = ((Up ? (uint32_t)(p / a.r.k) * (uint32_t)a.ldx : (uint32_t)p * (uint32_t)a.I) + place) * 2u;
   }
   const char *cols = static_cast<const char *>(Up ? a.x : a.hidden);
-  v4f d[NA][C] = {};
+  v4f d[P][C] = {};
   // eight tiles side by side run on eight XCDs
   stream<T, P, run_steps(P, C, Kind == kOne ? KS : 1)>(weights, row, cols, src, n, KS == 1 ? 0 : wave, KS, tile >> 3, d);
   // this lane: rows q * 4 + 0..3 of part p, column `token` of part `of`
   const int q = (lane >> 4) % (R / 4), p = (lane >> 4) / (R / 4), token = lane % R, of = lane % kTile / R;
   constexpr int CE = C < 2 ? 1 : 2;   // columns' operands whose sums are joined at a time
-  v4f (*own)[64] = KS == 1 ? part + wave * CE * M : part;
+  v4f (*own)[64] = KS == 1 ? part + wave * CE : part;
 #pragma unroll
   for (int c0 = 0; c0 < C; c0 += CE) {
     if (KS == 1) wave_sync(); else __syncthreads();
@@ -312,18 +312,18 @@ __device__ inline void expert_tile(const Layer &a, const char *weights, const in
 #pragma unroll
       for (int c = 0; c < CE; ++c)
 #pragma unroll
-        for (int i = 0; i < NA; ++i)
-          own[((KS == 1 ? 0 : wave * CE) + c) * M][((i * P + p) * (R / 4) + q) * R + token] = d[i][c0 + c];
+        for (int i = 0; i < P; ++i)
+          own[(KS == 1 ? 0 : wave * CE) + c][((i * P + p) * (R / 4) + q) * R + token] = d[i][c0 + c];
     }
     if (KS == 1) wave_sync(); else __syncthreads();
     const auto sum = [&](int c, int quad, int t) {   // rows quad * 4 + 0..3 of the tile
-      const v4f *from = &own[c * M][((quad * 4 / R * P) * (R / 4) + quad % (R / 4)) * R + t];
+      const v4f *from = &own[c][((quad * 4 / R * P) * (R / 4) + quad % (R / 4)) * R + t];
       v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-      for (int i = 0; i < KS * P; ++i) s += from[i / P * CE * M * 64 + i % P * (R / 4) * R];
+      for (int i = 0; i < KS * P; ++i) s += from[i / P * CE * 64 + i % P * (R / 4) * R];
       return s;
     };
-    constexpr int kQuads = Up ? 2 * M : 4 * M;
+    constexpr int kQuads = Up ? 2 : 4;
 #pragma unroll 1
     for (int o = KS == 1 ? lane : (int)threadIdx.x; o < CE * R * kQuads; o += KS * 64) {
       const int quad = o % kQuads, t = o / kQuads % R, c = o / kQuads / R, at = at0 + quad * 4, n0 = (c0 + c) * R + t;
@@ -331,7 +331,7 @@ __device__ inline void expert_tile(const Layer &a, const char *weights, const in
       const int64_t pair = pairs[n0];
       const v4f g = sum(c, quad, t);
       if (Up) {
-        const v4f u = sum(c, quad + 2 * M, t);
+        const v4f u = sum(c, quad + 2, t);
         T h[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) h[j] = from_float<T>(saturate<T>(g[j] * sigmoid(g[j]) * u[j]));
@@ -343,14 +343,12 @@ __device__ inline void expert_tile(const Layer &a, const char *weights, const in
   }
 }
 
-template <int Kind> constexpr int tile_rows(bool up) { return (up ? 8 : 16) * (Kind == kMany ? 2 : 1); }
-
 // Workgroup b takes tile b % groups (KS = 1: its waves four tiles side by side) of
 // the experts b / groups, b / groups + gridDim / groups, ... of those with pairs.
 template <class T, bool Up, int KS, int Kind>
-__global__ __launch_bounds__(64 * kExpertWaves, Kind == kMany ? 3 : 4) void expert_kernel(Layer a, int groups) {
-  __shared__ v4f part[kExpertWaves * (Kind == kOne ? 1 : Kind == kFew ? 2 : 4)][64];
-  constexpr int kRows = tile_rows<Kind>(Up);
+__global__ __launch_bounds__(64 * kExpertWaves, 4) void expert_kernel(Layer a, int groups) {
+  __shared__ v4f part[kExpertWaves * (Kind == kOne ? 1 : 2)][64];
+  constexpr int kRows = Up ? 8 : 16;
   const int tiles = ((Up ? a.I : a.H) + kRows - 1) / kRows, group = (int)blockIdx.x % groups;
   const int tile = KS == 1 ? group * kExpertWaves + uniform_i32(threadIdx.x >> 6) : group;
   if (tile >= tiles) return;
@@ -362,19 +360,117 @@ __global__ __launch_bounds__(64 * kExpertWaves, Kind == kMany ? 3 : 4) void expe
     const int64_t slot = a.slot ? a.slot[e] : e;
     const char *w = Up ? static_cast<const char *>(a.up) + slot * 4 * a.I * a.H
                        : static_cast<const char *>(a.down) + slot * 2 * a.H * a.I;
-    if (Kind == kOne) {
-      expert_tile<T, Up, 4, 1, 1, KS, Kind>(a, w, pairs, count, tile, part);
-    } else if (Kind == kFew) {
-      if (count <= 4) expert_tile<T, Up, 4, 1, 1, KS, Kind>(a, w, pairs, count, tile, part);
-      else if (count <= 8) expert_tile<T, Up, 4, 1, 2, KS, Kind>(a, w, pairs, count, tile, part);
-      else
-        for (int at = 0; at < count; at += 16) expert_tile<T, Up, 2, 1, 2, KS, Kind>(a, w, pairs + at, count - at, tile, part);
+    if (Kind == kOne || count <= 4) {
+      expert_tile<T, Up, 4, 1, KS, Kind>(a, w, pairs, count, tile, part);
+    } else if (count <= 8) {
+      expert_tile<T, Up, 4, 2, KS, Kind>(a, w, pairs, count, tile, part);
     } else {
-      if (count <= 16) expert_tile<T, Up, 1, 2, 1, KS, Kind>(a, w, pairs, count, tile, part);
-      else if (count <= 32) expert_tile<T, Up, 1, 2, 2, KS, Kind>(a, w, pairs, count, tile, part);
-      else
-        for (int at = 0; at < count; at += 64) expert_tile<T, Up, 1, 2, 4, KS, Kind>(a, w, pairs + at, count - at, tile, part);
+      for (int at = 0; at < count; at += 16) expert_tile<T, Up, 2, 2, KS, Kind>(a, w, pairs + at, count - at, tile, part);
     }
+  }
+}
+
+// Many pairs an expert: the columns' operands would cost more of the caches than
+// the rows' of memory, so a workgroup's waves share them.  A stage is 64 or 128 of
+// the inner axis of all of the expert's columns in LDS (chunks of 16 bytes, their
+// places turned by the column so that no bank is met twice), double-buffered;
+// each wave has 32 rows of its own (16 hidden units' gate and up rows, or 32
+// outputs) straight from memory, one stage ahead.
+template <class T, bool Up, int kStage>
+__global__ __launch_bounds__(64 * kExpertWaves, 2) void many_kernel(Layer a, int tiles) {
+  constexpr int kChunks = kStage / 8, kSteps = kStage / 32;
+  constexpr int kCols = TOPOEP_MOE_MAX_TOKENS / kTile, kEach = 64 * kExpertWaves / kChunks,
+                kUnits = TOPOEP_MOE_MAX_TOKENS / kEach;   // columns a pass of the workgroup stages, and passes
+  __shared__ v4i stage[2][TOPOEP_MOE_MAX_TOKENS][kChunks];
+  const int lane = lane_id(), wave = uniform_i32(threadIdx.x >> 6), r = lane & 15, place = (lane >> 4) * 8;
+  const int n = Up ? a.H : a.I, rows = Up ? a.I : a.H, stages = (n + kStage - 1) / kStage;
+  const int first = ((int)blockIdx.x % tiles * kExpertWaves + wave) * (Up ? 16 : 32);   // of this wave's units or outputs
+  for (int i = blockIdx.x / tiles;; i += gridDim.x / tiles) {
+    const int e = nth_active(a, i);
+    if (e < 0) return;
+    const int count = a.lists.count[e], cols = (count + kTile - 1) / kTile;
+    const int32_t *pairs = a.lists.pairs + (int64_t)e * a.T;
+    const int64_t slot = a.slot ? a.slot[e] : e;
+    const char *w = Up ? static_cast<const char *>(a.up) + slot * 4 * a.I * a.H
+                       : static_cast<const char *>(a.down) + slot * 2 * a.H * a.I;
+    const char *from = static_cast<const char *>(Up ? a.x : a.hidden);
+    uint32_t row[2], src[kUnits];
+    row[0] = ((uint32_t)imin(first + r, rows - 1) * n + place) * 2u;
+    row[1] = ((uint32_t)(Up ? a.I + imin(first + r, rows - 1) : imin(first + 16 + r, rows - 1)) * n + place) * 2u;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {   // this thread's columns and chunk of a stage
+      const int c = (int)threadIdx.x / kChunks + kEach * u, p = pairs[c < count ? c : 0];
+      src[u] = ((Up ? (uint32_t)(p / a.r.k) * (uint32_t)a.ldx : (uint32_t)p * (uint32_t)a.I) + threadIdx.x % kChunks * 8) * 2u;
+    }
+    v4i x[2][kSteps], b[kUnits];
+    v4f d[2][kCols] = {};
+    const v4i zero = {0, 0, 0, 0};
+    // what lies behind the axis reads its start and counts as zero
+    const auto load = [&](int k) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const bool in = k + 32 * s + place < n;
+          const v4i v = *reinterpret_cast<const v4i *>(w + (row[q] + (in ? (uint32_t)(k + 32 * s) * 2u : 0u - place * 2u)));
+          x[q][s] = in ? v : zero;
+        }
+      const uint32_t mine = threadIdx.x % kChunks * 8;
+      const bool in = k + (int)mine < n;
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u)
+        if (kEach * u < count) {
+          const v4i v = *reinterpret_cast<const v4i *>(from + (src[u] + (in ? (uint32_t)k * 2u : 0u - mine * 2u)));
+          b[u] = in ? v : zero;
+        }
+    };
+    // tiles that run side by side start at different places of their rows
+    int at_stage = (int)((uint32_t)((int)blockIdx.x % tiles >> 3) * 5u % (uint32_t)stages);
+    load(at_stage * kStage);
+    for (int g = 0; g < stages; ++g) {
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u)
+        if (kEach * u < count) {
+          const int c = (int)threadIdx.x / kChunks + kEach * u;
+          stage[g & 1][c][threadIdx.x % kChunks ^ (c & 7)] = b[u];
+        }
+      v4i now[2][kSteps];
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) now[q][s] = x[q][s];
+      __syncthreads();
+      at_stage = at_stage + 1 < stages ? at_stage + 1 : 0;
+      if (g + 1 < stages) load(at_stage * kStage);
+#pragma unroll
+      for (int c = 0; c < kCols; ++c)
+        if (c < cols) {
+#pragma unroll
+          for (int s = 0; s < kSteps; ++s) {
+            const int at = c * kTile + r;
+            const v4i col = stage[g & 1][at][(s * 4 + (lane >> 4)) ^ (at & 7)];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) d[q][c] = mfma<T>(now[q][s], col, d[q][c]);
+          }
+        }
+    }
+    const int at = first + (lane >> 4) * 4;   // this lane's four units or outputs, of column r of each tile
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+      if (c * kTile + r >= count) continue;
+      const int64_t pair = pairs[c * kTile + r];
+      if (Up) {
+        T h[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[j] = from_float<T>(saturate<T>(d[0][c][j] * sigmoid(d[0][c][j]) * d[1][c][j]));
+        if (at < rows) __builtin_memcpy(static_cast<T *>(a.hidden) + pair * a.I + at, h, sizeof(h));
+      } else {
+        float *to = a.each + pair * a.H + at;
+        if (at < rows) *reinterpret_cast<v4f *>(to) = d[0][c];
+        if (at + 16 < rows) *reinterpret_cast<v4f *>(to + 16) = d[1][c];
+      }
+    }
+    __syncthreads();   // before the next expert's stages
   }
 }
 
@@ -407,7 +503,7 @@ __global__ __launch_bounds__(64 * kExpertWaves, 4) void one_up_kernel(Layer a, i
   if (lane == 0) pair[0] = j;
   wave_sync();
   const char *w = static_cast<const char *>(a.up) + (int64_t)readlane_i32(slot, j) * 4 * a.I * a.H;
-  expert_tile<T, true, 4, 1, 1, kExpertWaves, kOne>(a, w, pair, 1, (int)blockIdx.x % tiles, part);
+  expert_tile<T, true, 4, 1, kExpertWaves, kOne>(a, w, pair, 1, (int)blockIdx.x % tiles, part);
 }
 
 // out_t = sum over t's choices in order, of those whose expert is here.
@@ -573,9 +669,8 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 bool launched() { return hipGetLastError() == hipSuccess; }
 
 template <class T, bool Up, int Kind>
-int enqueue_experts(const Layer &a, hipStream_t st) {
-  const int rows = tile_rows<Kind>(Up), tiles = ((Up ? a.I : a.H) + rows - 1) / rows;
-  const int experts = imin(imin(a.T * a.r.k, a.r.E), a.L);   // with pairs, about
+int enqueue_experts(const Layer &a, int experts, hipStream_t st) {
+  const int rows = Up ? 8 : 16, tiles = ((Up ? a.I : a.H) + rows - 1) / rows;
   const dim3 block(64 * kExpertWaves);
   // A wave to a tile where there are tiles for all of the chip's 4096 places, or
   // for half of them and rows are short (62 against 66 us for 32 experts, H = 2048,
@@ -593,9 +688,20 @@ int enqueue_experts(const Layer &a, hipStream_t st) {
 
 template <class T, bool Up>
 int enqueue_experts(const Layer &a, hipStream_t st) {
-  if (a.T <= 4) return enqueue_experts<T, Up, kOne>(a, st);
-  if (a.T * a.r.k <= 8 * a.r.E) return enqueue_experts<T, Up, kFew>(a, st);
-  return enqueue_experts<T, Up, kMany>(a, st);
+  const int experts = imin(imin(a.T * a.r.k, a.r.E), a.L);   // with pairs, about
+  if (a.T <= 4) return enqueue_experts<T, Up, kOne>(a, experts, st);
+  const int rows = kExpertWaves * (Up ? 16 : 32), tiles = ((Up ? a.I : a.H) + rows - 1) / rows;
+  // more than 12 pairs an expert (64 experts, 128 tokens, top-8: 163 us shared, 255
+  // not; 64 tokens: 154 either way)
+  if (a.T * a.r.k <= 12 * a.r.E) return enqueue_experts<T, Up, kFew>(a, experts, st);
+  // Stages of 128 read rows in longer pieces (8 experts of I = 14336: 672 us, 769
+  // with 64) but two workgroups fit a CU, not three: taken where the chip's rounds
+  // leave it no more than a seventh emptier (20 experts of I = 2048: 328 and 250 us)
+  const int blocks = experts * tiles, rounds2 = (blocks + 511) / 512, rounds3 = (blocks + 767) / 768;
+  const dim3 grid((unsigned)blocks), block(64 * kExpertWaves);
+  if (rounds2 * 512 * 6 <= rounds3 * 768 * 7) hipLaunchKernelGGL((many_kernel<T, Up, 128>), grid, block, 0, st, a, tiles);
+  else hipLaunchKernelGGL((many_kernel<T, Up, 64>), grid, block, 0, st, a, tiles);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
 template <class T, int NA>
