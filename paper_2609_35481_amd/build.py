@@ -27,7 +27,7 @@ HIPCC_FLAGS = [
 # library is LIB.
 STAMPS_LIB = os.path.join(HERE, "libtopoep_stamps.so")
 
-# The binding's reader of tensor lists, a Python module over torch's C++ tensors.
+# The binding's calls over torch's C++ tensors, a Python module.
 TENSORS_SRC = os.path.join(HERE, "csrc", "tensors.cpp")
 TENSORS_LIB = os.path.join(HERE, "_tensors.so")
 

@@ -1,15 +1,23 @@
-// Reads lists of torch tensors for the binding: a gradient set of hundreds of
-// tensors costs some 0.4 us a tensor in Python, more than its kernels take.
+// The binding's calls that take tensors as they come, over torch's C++ tensors:
+// in Python a gradient set of hundreds of tensors costs 0.4 us a tensor, and a
+// router call 6 us around its launch, more than their kernels take.
 //
 //   pack(grads, outs) -> (table, device)
+//     table: bytes, a topoep_grad for each tensor (outs None: the gradients
+//     themselves); device: the index of the GPU that all of them are on.
+//   route(entry, router, logits, bias, stream) -> (code, ids, weights)
+//   route_backward(entry, router, logits, ids, grad_weights, stream) -> (code, grad_logits)
+//     entry: the address of topoep_route (topoep_route_backward); router: of a
+//     topoep_router whose dtype is the logits'; code: what it returned.
 //
-// table: bytes, a topoep_grad for each tensor (outs None: the gradients
-// themselves); device: the index of the GPU that all of them are on.  Raises
 // TypeError and ValueError for what the library does not take.
 #define PY_SSIZE_T_CLEAN
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <ATen/ops/empty.h>
 #include <Python.h>
+
+#include <algorithm>
 
 #include "topoep_moe.h"
 
@@ -63,8 +71,7 @@ PyObject *fill(PyObject *grads, PyObject *outs) {
     to[i].dtype = from;
     to[i].out_dtype = into;
   }
-  PyObject *both = Py_BuildValue("(Ni)", table, device);
-  return both;
+  return Py_BuildValue("(Ni)", table, device);
 }
 
 PyObject *pack(PyObject *, PyObject *args) {
@@ -91,7 +98,96 @@ PyObject *pack(PyObject *, PyObject *args) {
   return result;
 }
 
-PyMethodDef methods[] = {{"pack", pack, METH_VARARGS, "pack(grads, outs) -> (bytes, device)"}, {nullptr, nullptr, 0, nullptr}};
+// Row stride of a matrix of dense rows that do not overlap; -1 (and an error)
+// for anything else.
+int64_t row_stride(const at::Tensor &t, const char *name) {
+  if (!t.is_cuda()) {
+    PyErr_Format(PyExc_TypeError, "%s must be a CUDA tensor", name);
+    return -1;
+  }
+  if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1) || (t.size(0) > 1 && t.stride(0) < t.size(1))) {
+    PyErr_Format(PyExc_ValueError, "%s must be a matrix of dense rows that do not overlap", name);
+    return -1;
+  }
+  return t.size(0) > 1 ? t.stride(0) : std::max(t.size(1), t.stride(0));
+}
+
+bool dense(const at::Tensor &t, const char *name, at::ScalarType type, const at::Tensor &like, at::IntArrayRef shape) {
+  if (t.scalar_type() != type || t.device() != like.device()) {
+    PyErr_Format(PyExc_TypeError, "%s must be %s on the logits' GPU", name, at::toString(type));
+    return false;
+  }
+  if (!t.sizes().equals(shape) || !t.is_contiguous()) {
+    PyErr_Format(PyExc_ValueError, "%s must be contiguous and of the shape that goes with the logits", name);
+    return false;
+  }
+  return true;
+}
+
+const at::Tensor *tensor_of(PyObject *o, const char *name) {
+  if (THPVariable_Check(o)) return &THPVariable_Unpack(o);
+  PyErr_Format(PyExc_TypeError, "%s is not a tensor", name);
+  return nullptr;
+}
+
+template <class F>
+PyObject *guarded(const F &f) {
+  try {
+    return f();
+  } catch (const std::exception &e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
+PyObject *route(PyObject *, PyObject *args) {
+  unsigned long long entry, router, stream;
+  PyObject *pl, *pb;
+  if (!PyArg_ParseTuple(args, "KKOOK", &entry, &router, &pl, &pb, &stream)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const topoep_router *r = reinterpret_cast<const topoep_router *>(router);
+    const at::Tensor *x = tensor_of(pl, "logits"), *b = pb == Py_None ? nullptr : tensor_of(pb, "bias");
+    if (!x || (pb != Py_None && !b)) return nullptr;
+    const int64_t ld = row_stride(*x, "logits");
+    if (ld < 0 || (b && !dense(*b, "bias", at::kFloat, *x, {x->size(1)}))) return nullptr;
+    const at::TensorOptions on = x->options();
+    at::Tensor ids = at::empty({x->size(0), r->topk}, on.dtype(at::kInt));
+    at::Tensor weights = at::empty({x->size(0), r->topk}, on.dtype(at::kFloat));
+    const int rc = x->size(0) > INT32_MAX ? TOPOEP_EINVAL
+                                          : reinterpret_cast<decltype(&topoep_route)>(entry)(
+                                                r, x->data_ptr(), ld, (int32_t)x->size(0), b ? b->data_ptr<float>() : nullptr,
+                                                ids.data_ptr<int32_t>(), weights.data_ptr<float>(),
+                                                reinterpret_cast<void *>(stream));
+    return Py_BuildValue("(iNN)", rc, THPVariable_Wrap(ids), THPVariable_Wrap(weights));
+  });
+}
+
+PyObject *route_backward(PyObject *, PyObject *args) {
+  unsigned long long entry, router, stream;
+  PyObject *pl, *pi, *pg;
+  if (!PyArg_ParseTuple(args, "KKOOOK", &entry, &router, &pl, &pi, &pg, &stream)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const topoep_router *r = reinterpret_cast<const topoep_router *>(router);
+    const at::Tensor *x = tensor_of(pl, "logits"), *ids = tensor_of(pi, "ids"), *g = tensor_of(pg, "grad_weights");
+    if (!x || !ids || !g) return nullptr;
+    const int64_t ld = row_stride(*x, "logits");
+    if (ld < 0 || !dense(*ids, "ids", at::kInt, *x, {x->size(0), r->topk}) ||
+        !dense(*g, "grad_weights", at::kFloat, *x, {x->size(0), r->topk}))
+      return nullptr;
+    at::Tensor out = at::empty({x->size(0), x->size(1)}, x->options());
+    const int rc = x->size(0) > INT32_MAX
+                       ? TOPOEP_EINVAL
+                       : reinterpret_cast<decltype(&topoep_route_backward)>(entry)(
+                             r, x->data_ptr(), ld, (int32_t)x->size(0), ids->data_ptr<int32_t>(), g->data_ptr<float>(),
+                             out.data_ptr(), x->size(1), reinterpret_cast<void *>(stream));
+    return Py_BuildValue("(iN)", rc, THPVariable_Wrap(out));
+  });
+}
+
+PyMethodDef methods[] = {{"route", route, METH_VARARGS, "route(entry, router, logits, bias, stream) -> (code, ids, weights)"},
+                         {"route_backward", route_backward, METH_VARARGS,
+                          "route_backward(entry, router, logits, ids, grad_weights, stream) -> (code, grad_logits)"},
+                         {"pack", pack, METH_VARARGS, "pack(grads, outs) -> (bytes, device)"}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

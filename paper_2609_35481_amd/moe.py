@@ -9,7 +9,7 @@
 
 Argument checks and marshalling only: torch provides device memory and the
 current stream, every step runs in the HIP kernels of libtopoep.so.  Importing this module fails
-loudly when the library, or _tensors (which reads lists of tensors), has not been built.
+loudly when the library, or _tensors (the calls that take torch's C++ tensors), has not been built.
 """
 from __future__ import annotations
 
@@ -64,6 +64,9 @@ for _name, _args in (
     _fn = getattr(_lib, _name)
     _fn.restype, _fn.argtypes = ctypes.c_int, _args
 
+_ROUTE = ctypes.cast(_lib.topoep_route, _vp).value
+_ROUTE_BACKWARD = ctypes.cast(_lib.topoep_route_backward, _vp).value
+
 EXPORTS = ("topoep_route", "topoep_route_backward", "topoep_moe_workspace_bytes", "topoep_moe_few",
            "topoep_grads_workspace_bytes", "topoep_grad_norm", "topoep_clip_grads")
 
@@ -104,6 +107,8 @@ def _dense(t, name, shape, dtype, device):
 def _stream_of(device):
     """The current stream of the tensors' device, which has to be the current
     device: the library's calls go there."""
+    if device.type != "cuda":
+        raise TypeError("tensors must be on a GPU, not on %s" % device)
     if torch._C._cuda_getDevice() != device.index:
         raise ValueError("the tensors are on %s, the current device is cuda:%d" % (device, torch.cuda.current_device()))
     return torch._C._cuda_getCurrentRawStream(device.index)
@@ -119,29 +124,15 @@ def _on_stream(stream, call, *args):
 
 
 def _route(r, logits, bias):
-    ld = _rows(logits, "logits")
-    T, E = logits.shape
-    dev = logits.device
-    stream = _stream_of(dev)
-    if bias is not None:
-        _dense(bias, "bias", (E,), torch.float32, dev)
-    ids = torch.empty((T, r.topk), dtype=torch.int32, device=dev)
-    weights = torch.empty((T, r.topk), dtype=torch.float32, device=dev)
-    _check(_lib.topoep_route(r, logits.data_ptr(), ld, T, bias.data_ptr() if bias is not None else None,
-                             ids.data_ptr(), weights.data_ptr(), stream), "topoep_route")
+    rc, ids, weights = _tensors.route(_ROUTE, ctypes.addressof(r), logits, bias, _stream_of(logits.device))
+    _check(rc, "topoep_route")
     return ids, weights
 
 
 def _backward(r, logits, ids, grad_weights):
-    ld = _rows(logits, "logits")
-    T, E = logits.shape
-    dev = logits.device
-    stream = _stream_of(dev)
-    _dense(ids, "ids", (T, r.topk), torch.int32, dev)
-    _dense(grad_weights, "grad_weights", (T, r.topk), torch.float32, dev)
-    out = torch.empty((T, E), dtype=logits.dtype, device=dev)
-    _check(_lib.topoep_route_backward(r, logits.data_ptr(), ld, T, ids.data_ptr(), grad_weights.data_ptr(),
-                                      out.data_ptr(), E, stream), "topoep_route_backward")
+    rc, out = _tensors.route_backward(_ROUTE_BACKWARD, ctypes.addressof(r), logits, ids, grad_weights,
+                                      _stream_of(logits.device))
+    _check(rc, "topoep_route_backward")
     return out
 
 
