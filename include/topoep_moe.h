@@ -115,7 +115,7 @@ int topoep_moe_workspace_bytes(const topoep_moe *m, const topoep_router *r, int3
  * tokens.  With t's experts e_j and weights w_j from the router on the logits
  * x_t gate^T (held in 32 bits; r->dtype is not read), and s_j = slot[e_j]:
  *
- *   h_j   = silu(up[s_j][0:I] x_t) * (up[s_j][I:2I] x_t)
+ *   h_j   = silu(up[s_j][0:I] x_t) * (up[s_j][I:2I] x_t),  silu(z) = z / (1 + exp(-z))
  *   out_t = sum_{j: s_j >= 0} w_j down[s_j] h_j
  *
  *   x            device [T, H], row t at x + t * ldx elements (H <= ldx < 2^24,
@@ -130,10 +130,9 @@ int topoep_moe_workspace_bytes(const topoep_moe *m, const topoep_router *r, int3
  *   down         device [L, H, I]
  *   out          device out [T, H], dense
  *   ids, weights device out [T, k]: the router's
- *   workspace    topoep_moe_workspace_bytes bytes, 256-byte aligned,
- *                zero-filled before its first call; every call leaves it
- *                ready for the next, of any sizes it is large enough for.
- *                Calls that share one are ordered on one stream.
+ *   workspace    topoep_moe_workspace_bytes bytes, 256-byte aligned; nothing
+ *                in it is kept between calls or has to be cleared.  Calls that
+ *                share one are ordered on one stream.
  *
  * Products are accumulated in 32 bits; h is rounded to the weights' type
  * (f16: saturated at its largest finite value).  TOPOEP_EINVAL: null
@@ -163,20 +162,23 @@ int topoep_grads_workspace_bytes(int32_t count, size_t *bytes_out);
  * Enqueue the global norm of a set of tensors: *norm (device float) = scale *
  * the 2-norm, or the largest magnitude, over all of their elements.  Squares
  * are summed in 64 bits in an order that depends only on the sizes and on which
- * tensors follow each other in memory, so equal calls give equal bits.  NaN where an element is NaN.  scale: finite, >= 0
- * (1 / the loss scale).
+ * tensors follow each other in memory, so equal calls give equal bits.  NaN
+ * where an element is NaN.  scale: finite, >= 0 (1 / the loss scale).
+ * TOPOEP_EINVAL: null pointers, negative sizes or more than 2^40 elements, unknown
+ * types or norms, pointers not aligned to their elements; TOPOEP_EWORKSPACE:
+ * workspace too small or not 256-byte aligned.
  */
 int topoep_grad_norm(const topoep_grad *grads, int32_t count, float scale, int32_t ord, float *norm, void *workspace,
                      size_t workspace_bytes, void *stream);
 
 /*
- * Enqueue the clip: out = grad * (scale * min(1, max_norm / (norm + 1e-6))) for every
- * element.  given_norm: device float, the norm to clip by (a group's, say,
+ * Enqueue the clip: out = grad * (scale * min(1, max_norm / (norm + 1e-6))) for
+ * every element.  given_norm: device float, the norm to clip by (a group's, say,
  * already scaled), or NULL: that of topoep_grad_norm over this set, which is
  * also written to *norm (may be NULL).  Where the norm is not finite nothing
  * is written but *norm, so that the caller can drop the step.  Where the
  * factor is 1, tensors clipped in place are left alone.  max_norm > 0, finite or
- * infinite.
+ * infinite.  Return codes as topoep_grad_norm.
  */
 int topoep_clip_grads(const topoep_grad *grads, int32_t count, float scale, int32_t ord, float max_norm,
                       const float *given_norm, float *norm, void *workspace, size_t workspace_bytes, void *stream);

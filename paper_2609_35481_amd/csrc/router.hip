@@ -275,7 +275,7 @@ __device__ inline void list_candidates(const Route &a, const T *row, int sub, co
 // groups; -1: groups of any size.  Places beyond E hold masked logits of ids that no expert has: any
 // expert comes before them.
 template <class T, int LPT, int V, int K, int GL, bool Bias>
-__global__ __launch_bounds__(kThreads) void route_list_kernel(Route a) {
+__global__ __launch_bounds__(kThreads, V <= 32 ? 4 : 2) void route_list_kernel(Route a) {
   constexpr int kRows = kThreads / LPT;
   const int sub = threadIdx.x % LPT, E = a.r.E, base = sub * V;
   const int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / LPT;
@@ -292,7 +292,23 @@ __global__ __launch_bounds__(kThreads) void route_list_kernel(Route a) {
       for (int v = 0; v < V; ++v) b[v] = base + v < E ? a.bias[base + v] : 0.0f;
     }
   }
-  const auto key = [&](int v) { return Bias ? x[v] + b[Bias ? v : 0] : x[v]; };
+  // scores over every logit: their largest and the sum, before the logits become keys
+  float all = 0.0f, most = 0.0f;
+  if (!a.r.sigmoid && !a.r.renorm) {
+    most = x[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) most = fmaxf(most, x[v]);
+    most = few_max<LPT>(most);
+    const float from = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+    for (int v = 0; v < V; ++v) all += __expf(x[v] - from);
+    all = few_sum<LPT>(all);
+  }
+  if constexpr (Bias) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) x[v] += b[v];
+  }
+  const auto key = [&](int v) { return x[v]; };
   double l[K];
   uint64_t lane_open = ~0ull;   // bit v: expert base + v's group is open
   bool listed = false;          // l is made already
@@ -399,14 +415,8 @@ __global__ __launch_bounds__(kThreads) void route_list_kernel(Route a) {
 #pragma unroll
       for (int j = 0; j < K; ++j) sum += j < a.r.k && m != -INFINITY ? __expf(s[j] - m) : 0.0f;
     } else {
-      m = x[0];
-#pragma unroll
-      for (int v = 1; v < V; ++v) m = fmaxf(m, x[v]);
-      m = few_max<LPT>(m);
-      const float from = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-      for (int v = 0; v < V; ++v) sum += __expf(x[v] - from);
-      sum = few_sum<LPT>(sum);
+      m = most;
+      sum = all;
     }
     const float f = sum > 0.0f ? a.r.scale / sum : 0.0f, from = m == -INFINITY ? 0.0f : m;
 #pragma unroll

@@ -93,7 +93,7 @@ def _rows(t, name):
         raise TypeError("%s must be a CUDA tensor" % name)
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
         raise ValueError("%s must be a matrix of dense rows that do not overlap" % name)
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _dense(t, name, shape, dtype, device):
@@ -176,7 +176,8 @@ def route_backward(logits, ids, grad_weights, scoring="softmax", renorm=True, sc
 
 
 def moe_workspace_bytes(H, I, E, L, k, T, dtype=torch.bfloat16) -> int:
-    """Bytes of zero-filled workspace moe_few needs for T tokens or fewer."""
+    """Bytes of workspace moe_few needs for T tokens or fewer (and up to 255
+    more where it does not start at a multiple of 256)."""
     out = _size(0)
     m = Moe(H, I, L, _TYPES.get(dtype, -1))
     _check(_lib.topoep_moe_workspace_bytes(m, router(E, k), T, out), "topoep_moe_workspace_bytes")
@@ -189,10 +190,10 @@ def moe_few(x, gate, up, down, k, scoring="softmax", renorm=True, scale=1.0, bia
     [T, k]) of the tokens x [T, H], at most 128, through a layer with the
     router gate [E, H] and the experts up [L, 2I, H] (gate rows, then up rows)
     and down [L, H, I], bfloat16 or float16.  expert_slot [E] says where an
-    expert lies among the L here (-1: elsewhere; it adds nothing).
+    expert lies among the L here (-1: elsewhere; it adds nothing).  Forward only.
 
-    workspace: a zero-filled byte tensor kept between calls
-    (moe_workspace_bytes; any larger one serves too); None makes one for the call."""
+    workspace: a tensor of moe_workspace_bytes or more for calls on one stream to
+    share; None makes one for the call."""
     args = (x, gate, up, down, k, (scoring, renorm, scale, groups, top_groups), bias, expert_slot, workspace)
     return _few(*args) if stream is None else _on_stream(stream, _few, *args)
 
@@ -217,7 +218,7 @@ def _few(x, gate, up, down, k, rules, bias, expert_slot, workspace):
     r = router(E, k, torch.float32, *rules)
     m = Moe(H, I, L, _TYPES[dtype])
     if workspace is None:
-        workspace = torch.zeros(moe_workspace_bytes(H, I, E, L, k, T, dtype) + 256, dtype=torch.uint8, device=dev)
+        workspace = torch.empty(moe_workspace_bytes(H, I, E, L, k, T, dtype) + 255, dtype=torch.uint8, device=dev)
     elif workspace.device != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous on %s" % dev)
     ws = (workspace.data_ptr() + 255) & ~255
