@@ -1,7 +1,6 @@
 // The global gradient norm over many tensors and the clip on gfx950.
 //
-// The tensors' addresses and sizes travel as kernel arguments, kSet tensors a
-// launch, so a call copies nothing to the device and may be captured; tensors
+// The tensors' addresses and sizes travel as kernel arguments, so a call copies nothing to the device and may be captured; tensors
 // that follow each other in memory (views of one flat buffer) count as one.  A
 // launch's elements are cut into chunks of kChunk elements that do not cross
 // tensors, and each workgroup walks one contiguous range of chunks.  The norm
@@ -21,31 +20,36 @@ namespace {
 using namespace topoep_dev;
 
 constexpr int kThreads = 256;
-constexpr int kSet = 128;          // tensors a launch takes (3.6 KB of arguments)
 constexpr int64_t kChunk = 2048;
 constexpr int kBlocks = 2048;      // workgroups, and partials, a launch of the norm has at most
 constexpr int kClipBlocks = 8192;  // workgroups a launch of the clip has at most
 
 // elements a set may have (2^29 chunks: chunk numbers are 32-bit words)
 constexpr int64_t kMostElements = (int64_t)1 << 40;
+// elements of one entry at most; larger tensors are several
+constexpr int64_t kMostEntry = (int64_t)1 << 31;
 
+// The tensors of a launch, as many as 4 KB of arguments hold: 240 for the
+// norm, 160 for the clip.  An address carries its elements' type in its top byte.
+template <bool Out>
 struct Set {
+  static constexpr int kMost = Out ? 160 : 240;
   int count, chunks;
-  int first[kSet];      // chunks before tensor i
-  const void *grad[kSet];
-  void *out[kSet];
-  int64_t n[kSet];      // elements | dtype << 56 | out_dtype << 60
-  __host__ __device__ int64_t size(int i) const { return n[i] & (((int64_t)1 << 56) - 1); }
-  __host__ __device__ int type(int i) const { return (int)(n[i] >> 56) & 15; }
-  __host__ __device__ int out_type(int i) const { return (int)(n[i] >> 60) & 15; }
+  uint64_t from[kMost], to[Out ? kMost : 1];
+  uint32_t first[kMost];   // chunks before entry i
+  uint32_t n[kMost];       // its elements
+  static __host__ __device__ uint64_t tagged(const void *p, int type) { return reinterpret_cast<uint64_t>(p) | (uint64_t)type << 56; }
+  static __host__ __device__ int type(uint64_t p) { return (int)(p >> 56); }
+  static __host__ __device__ char *address(uint64_t p) { return reinterpret_cast<char *>(p & (((uint64_t)1 << 56) - 1)); }
 };
 
 // The tensor that holds a chunk (the last with first <= chunk).
-__device__ inline int tensor_of(const Set &s, int chunk) {
+template <bool Out>
+__device__ inline int tensor_of(const Set<Out> &s, int chunk) {
   int lo = 0, hi = s.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (s.first[mid] <= chunk) lo = mid; else hi = mid - 1;
+    if ((int)s.first[mid] <= chunk) lo = mid; else hi = mid - 1;
   }
   return lo;
 }
@@ -54,15 +58,15 @@ __device__ inline int tensor_of(const Set &s, int chunk) {
 // pieces, kPiece chunks each: b, b + grid, ... (Back: counted from the end), so
 // that the workgroups' accesses move through memory together.
 constexpr int kPiece = 4;
-template <bool Back, class F>
-__device__ inline void each_part(const Set &s, int b, const F &f) {
+template <bool Back, bool Out, class F>
+__device__ inline void each_part(const Set<Out> &s, int b, const F &f) {
   const int pieces = (s.chunks + kPiece - 1) / kPiece;
   for (int p = b; p < pieces; p += gridDim.x) {
     int c = (Back ? pieces - 1 - p : p) * kPiece;
     const int end = imin(c + kPiece, s.chunks);
     for (int i = tensor_of(s, c); c < end; ++i) {
-      const int stop = i + 1 < s.count ? imin(end, s.first[i + 1]) : end;
-      const int64_t at = (int64_t)(c - s.first[i]) * kChunk, to = (int64_t)(stop - s.first[i]) * kChunk, n = s.size(i);
+      const int begin = (int)s.first[i], stop = i + 1 < s.count ? imin(end, (int)s.first[i + 1]) : end;
+      const int64_t at = (int64_t)(c - begin) * kChunk, to = (int64_t)(stop - begin) * kChunk, n = s.n[i];
       f(i, at, (to < n ? to : n) - at);
       c = stop;
     }
@@ -162,14 +166,15 @@ __device__ inline void reduce_part(const T *g, int64_t n, R &r) {
 }
 
 template <class R, bool Stream>
-__global__ __launch_bounds__(kThreads) void grad_norm_kernel(Set s, double *partials) {
+__global__ __launch_bounds__(kThreads) void grad_norm_kernel(Set<false> s, double *partials) {
   __shared__ double lds[kThreads / 64];
   R r;
   each_part<false>(s, blockIdx.x, [&](int i, int64_t at, int64_t n) {
-    switch (s.type(i)) {
-      case TOPOEP_F32: reduce_part<Stream>(static_cast<const float *>(s.grad[i]) + at, n, r); break;
-      case TOPOEP_BF16: reduce_part<Stream>(static_cast<const Bf16 *>(s.grad[i]) + at, n, r); break;
-      default: reduce_part<Stream>(static_cast<const F16 *>(s.grad[i]) + at, n, r); break;
+    const char *g = s.address(s.from[i]);
+    switch (s.type(s.from[i])) {
+      case TOPOEP_F32: reduce_part<Stream>(reinterpret_cast<const float *>(g) + at, n, r); break;
+      case TOPOEP_BF16: reduce_part<Stream>(reinterpret_cast<const Bf16 *>(g) + at, n, r); break;
+      default: reduce_part<Stream>(reinterpret_cast<const F16 *>(g) + at, n, r); break;
     }
   });
   const double v = join_block(r, lds);
@@ -214,11 +219,11 @@ __device__ inline void scale_part(const T *g, O *out, int64_t n, float f) {
 }
 
 template <bool Stream, class T>
-__device__ inline void scale_part_to(const T *g, void *out, int type, int64_t at, int64_t n, float f) {
+__device__ inline void scale_part_to(const T *g, char *out, int type, int64_t at, int64_t n, float f) {
   switch (type) {
-    case TOPOEP_F32: scale_part<Stream>(g + at, static_cast<float *>(out) + at, n, f); break;
-    case TOPOEP_BF16: scale_part<Stream>(g + at, static_cast<Bf16 *>(out) + at, n, f); break;
-    default: scale_part<Stream>(g + at, static_cast<F16 *>(out) + at, n, f); break;
+    case TOPOEP_F32: scale_part<Stream>(g + at, reinterpret_cast<float *>(out) + at, n, f); break;
+    case TOPOEP_BF16: scale_part<Stream>(g + at, reinterpret_cast<Bf16 *>(out) + at, n, f); break;
+    default: scale_part<Stream>(g + at, reinterpret_cast<F16 *>(out) + at, n, f); break;
   }
 }
 
@@ -231,53 +236,66 @@ struct Clip {
 };
 
 template <class R, bool Stream>
-__global__ __launch_bounds__(kThreads) void clip_kernel(Set s, Clip c) {
+__global__ __launch_bounds__(kThreads) void clip_kernel(Set<true> s, Clip c) {
   __shared__ double lds[kThreads / 64];
   const float norm = c.given ? *c.given : norm_of<R>(c.partials, c.count, c.scale, lds);
   if (c.norm && blockIdx.x == 0 && threadIdx.x == 0) *c.norm = norm;
   if (!(norm - norm == 0.0f)) return;
   const float f = c.scale * fminf(1.0f, c.max_norm / (norm + 1e-6f));
   each_part<true>(s, blockIdx.x, [&](int i, int64_t at, int64_t n) {
-    if (f == 1.0f && s.out[i] == s.grad[i]) return;
-    const int to = s.out_type(i);
-    switch (s.type(i)) {
-      case TOPOEP_F32: scale_part_to<Stream>(static_cast<const float *>(s.grad[i]), s.out[i], to, at, n, f); break;
-      case TOPOEP_BF16: scale_part_to<Stream>(static_cast<const Bf16 *>(s.grad[i]), s.out[i], to, at, n, f); break;
-      default: scale_part_to<Stream>(static_cast<const F16 *>(s.grad[i]), s.out[i], to, at, n, f); break;
+    if (f == 1.0f && s.to[i] == s.from[i]) return;
+    const char *g = s.address(s.from[i]);
+    char *out = s.address(s.to[i]);
+    const int to = s.type(s.to[i]);
+    switch (s.type(s.from[i])) {
+      case TOPOEP_F32: scale_part_to<Stream>(reinterpret_cast<const float *>(g), out, to, at, n, f); break;
+      case TOPOEP_BF16: scale_part_to<Stream>(reinterpret_cast<const Bf16 *>(g), out, to, at, n, f); break;
+      default: scale_part_to<Stream>(reinterpret_cast<const F16 *>(g), out, to, at, n, f); break;
     }
   });
 }
 
 int bytes_of(int type) { return type == TOPOEP_F32 ? 4 : 2; }
-const char *end_of(const void *p, int64_t n, int type) { return static_cast<const char *>(p) + n * bytes_of(type); }
 
-// Walks the set in launches of kSet tensors: fills each one's arguments and
-// calls go(set, index of the launch).  `out`: outputs count too.
-template <class F>
-int each_set(const topoep_grad *grads, int count, bool out, const F &go) {
-  Set s;
+// Walks the set in launches: fills each one's arguments and calls go(set,
+// index of the launch).  Tensors that follow each other in memory (and their
+// outputs too, where Out) are one entry.
+template <bool Out, class F>
+int each_set(const topoep_grad *grads, int count, const F &go) {
+  Set<Out> s;
   int at = 0, launch = 0;
+  int64_t done = 0;   // of tensor `at`
   do {
     s.count = 0;
-    for (; at < count; ++at) {
+    while (at < count) {
       const topoep_grad &g = grads[at];
-      if (g.n == 0) continue;
-      const int last = s.count - 1;
-      if (last >= 0 && s.type(last) == g.dtype && end_of(s.grad[last], s.size(last), g.dtype) == g.grad &&
-          (!out || (s.out_type(last) == g.out_dtype && end_of(s.out[last], s.size(last), g.out_dtype) == g.out))) {
-        s.n[last] += g.n;
-        continue;
+      const int64_t left = g.n - done;
+      if (left > 0) {
+        const int width = bytes_of(g.dtype), wide = Out ? bytes_of(g.out_dtype) : 0;
+        const uint64_t from = Set<Out>::tagged(static_cast<const char *>(g.grad) + done * width, g.dtype);
+        const uint64_t to = Out ? Set<Out>::tagged(static_cast<char *>(g.out) + done * wide, g.out_dtype) : 0;
+        const int last = s.count - 1;
+        int64_t n = left < kMostEntry ? left : kMostEntry;
+        if (last >= 0 && s.from[last] + (uint64_t)s.n[last] * width == from && s.n[last] + n <= kMostEntry &&
+            (!Out || s.to[last] + (uint64_t)s.n[last] * wide == to)) {
+          s.n[last] += (uint32_t)n;
+        } else {
+          if (s.count == Set<Out>::kMost) break;
+          s.from[s.count] = from;
+          if (Out) s.to[s.count] = to;
+          s.n[s.count++] = (uint32_t)n;
+        }
+        done += n;
       }
-      if (s.count == kSet) break;
-      const int i = s.count++;
-      s.grad[i] = g.grad;
-      s.out[i] = out ? g.out : nullptr;
-      s.n[i] = g.n | (int64_t)g.dtype << 56 | (int64_t)(out ? g.out_dtype : 0) << 60;
+      if (done == g.n) {
+        ++at;
+        done = 0;
+      }
     }
     int64_t chunks = 0;
     for (int i = 0; i < s.count; ++i) {
-      s.first[i] = (int)chunks;
-      chunks += (s.size(i) + kChunk - 1) / kChunk;
+      s.first[i] = (uint32_t)chunks;
+      chunks += ((int64_t)s.n[i] + kChunk - 1) / kChunk;
     }
     s.chunks = (int)chunks;
     const int rc = go(s, launch++);
@@ -297,7 +315,8 @@ bool streams(const topoep_grad *grads, int count) {
   return bytes > kStreamBytes;
 }
 
-int grid_of(const Set &s, int most) { return imax(1, imin(most, (s.chunks + kPiece - 1) / kPiece)); }
+template <bool Out>
+int grid_of(const Set<Out> &s, int most) { return imax(1, imin(most, (s.chunks + kPiece - 1) / kPiece)); }
 
 int check_set(const topoep_grad *grads, int32_t count, bool out) {
   if (count < 0 || (count > 0 && !grads)) return TOPOEP_EINVAL;
@@ -307,17 +326,23 @@ int check_set(const topoep_grad *grads, int32_t count, bool out) {
     if (g.n < 0 || g.n > left || g.dtype < TOPOEP_F32 || g.dtype > TOPOEP_F16) return TOPOEP_EINVAL;
     left -= g.n;
     if (g.n == 0) continue;
-    if (!g.grad || (reinterpret_cast<uintptr_t>(g.grad) & (g.dtype == TOPOEP_F32 ? 3 : 1))) return TOPOEP_EINVAL;
+    if (!g.grad || (reinterpret_cast<uintptr_t>(g.grad) & (g.dtype == TOPOEP_F32 ? 3 : 1)) ||
+        reinterpret_cast<uintptr_t>(g.grad) >> 56)
+      return TOPOEP_EINVAL;
     if (!out) continue;
     if (g.out_dtype < TOPOEP_F32 || g.out_dtype > TOPOEP_F16 || !g.out) return TOPOEP_EINVAL;
-    if (reinterpret_cast<uintptr_t>(g.out) & (g.out_dtype == TOPOEP_F32 ? 3 : 1)) return TOPOEP_EINVAL;
+    if (reinterpret_cast<uintptr_t>(g.out) & (g.out_dtype == TOPOEP_F32 ? 3 : 1) || reinterpret_cast<uintptr_t>(g.out) >> 56)
+      return TOPOEP_EINVAL;
     if (g.out == g.grad && g.out_dtype != g.dtype) return TOPOEP_EINVAL;
   }
   return TOPOEP_OK;
 }
 
-// kBlocks partials a launch, and a launch per kSet tensors.
-size_t partials_bytes(int32_t count) { return ((size_t)count / kSet + 1) * kBlocks * sizeof(double); }
+// kBlocks partials a launch; the entries are the tensors and the further parts
+// of those beyond kMostEntry elements.
+size_t partials_bytes(int32_t count) {
+  return (((size_t)count + (size_t)(kMostElements / kMostEntry)) / Set<false>::kMost + 1) * kBlocks * sizeof(double);
+}
 
 int check_workspace(const void *ws, size_t bytes, int32_t count) {
   if (!ws) return TOPOEP_EINVAL;
@@ -331,7 +356,7 @@ bool finite_scale(float s) { return s >= 0.0f && s - s == 0.0f; }
 
 template <class R, bool Stream>
 int enqueue_partials(const topoep_grad *grads, int count, double *ws, hipStream_t st, int *partials) {
-  return each_set(grads, count, false, [&](const Set &s, int) {
+  return each_set<false>(grads, count, [&](const Set<false> &s, int) {
     const int grid = grid_of(s, kBlocks);
     hipLaunchKernelGGL((grad_norm_kernel<R, Stream>), dim3(grid), dim3(kThreads), 0, st, s, ws + *partials);
     *partials += grid;
@@ -357,7 +382,7 @@ int enqueue_clip(const topoep_grad *grads, int count, Clip c, double *ws, hipStr
     const int rc = enqueue_partials<R, Stream>(grads, count, ws, st, &c.count);
     if (rc != TOPOEP_OK) return rc;
   }
-  return each_set(grads, count, true, [&](const Set &s, int launch) {
+  return each_set<true>(grads, count, [&](const Set<true> &s, int launch) {
     Clip own = c;
     if (launch > 0) own.norm = nullptr;
     hipLaunchKernelGGL((clip_kernel<R, Stream>), dim3(grid_of(s, kClipBlocks)), dim3(kThreads), 0, st, s, own);

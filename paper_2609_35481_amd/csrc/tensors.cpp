@@ -7,8 +7,9 @@
 //     themselves); device: the index of the GPU that all of them are on.
 //   route(entry, router, logits, bias, stream) -> (code, ids, weights)
 //   route_backward(entry, router, logits, ids, grad_weights, stream) -> (code, grad_logits)
-//     entry: the address of topoep_route (topoep_route_backward); router: of a
-//     topoep_router whose dtype is the logits'; code: what it returned.
+//   moe_few(entry, router, x, gate, up, down, bias, expert_slot, workspace, stream) -> (code, out, ids, weights)
+//     entry: the address of topoep_route (topoep_route_backward, topoep_moe_few);
+//     router: of a topoep_router, whose dtype is the logits'; code: what it returned.
 //
 // TypeError and ValueError for what the library does not take.
 #define PY_SSIZE_T_CLEAN
@@ -16,8 +17,6 @@
 
 #include <ATen/ops/empty.h>
 #include <Python.h>
-
-#include <algorithm>
 
 #include "topoep_moe.h"
 
@@ -109,16 +108,16 @@ int64_t row_stride(const at::Tensor &t, const char *name) {
     PyErr_Format(PyExc_ValueError, "%s must be a matrix of dense rows that do not overlap", name);
     return -1;
   }
-  return t.size(0) > 1 ? t.stride(0) : std::max(t.size(1), t.stride(0));
+  return t.size(0) > 1 ? t.stride(0) : t.size(1);
 }
 
 bool dense(const at::Tensor &t, const char *name, at::ScalarType type, const at::Tensor &like, at::IntArrayRef shape) {
   if (t.scalar_type() != type || t.device() != like.device()) {
-    PyErr_Format(PyExc_TypeError, "%s must be %s on the logits' GPU", name, at::toString(type));
+    PyErr_Format(PyExc_TypeError, "%s must be %s on the same GPU", name, c10::toString(type));
     return false;
   }
   if (!t.sizes().equals(shape) || !t.is_contiguous()) {
-    PyErr_Format(PyExc_ValueError, "%s must be contiguous and of the shape that goes with the logits", name);
+    PyErr_Format(PyExc_ValueError, "%s must be contiguous and of the shape that goes with the others", name);
     return false;
   }
   return true;
@@ -184,7 +183,59 @@ PyObject *route_backward(PyObject *, PyObject *args) {
   });
 }
 
-PyMethodDef methods[] = {{"route", route, METH_VARARGS, "route(entry, router, logits, bias, stream) -> (code, ids, weights)"},
+PyObject *moe_few(PyObject *, PyObject *args) {
+  unsigned long long entry, router, stream;
+  PyObject *px, *pg, *pu, *pd, *pb, *ps, *pw;
+  if (!PyArg_ParseTuple(args, "KKOOOOOOOK", &entry, &router, &px, &pg, &pu, &pd, &pb, &ps, &pw, &stream)) return nullptr;
+  return guarded([&]() -> PyObject * {
+    const topoep_router *r = reinterpret_cast<const topoep_router *>(router);
+    const at::Tensor *x = tensor_of(px, "x"), *gate = tensor_of(pg, "gate"), *up = tensor_of(pu, "up"),
+                     *down = tensor_of(pd, "down"), *ws = tensor_of(pw, "workspace");
+    if (!x || !gate || !up || !down || !ws) return nullptr;
+    const at::Tensor *bias = pb == Py_None ? nullptr : tensor_of(pb, "bias");
+    const at::Tensor *slot = ps == Py_None ? nullptr : tensor_of(ps, "expert_slot");
+    if ((pb != Py_None && !bias) || (ps != Py_None && !slot)) return nullptr;
+    const int64_t ldx = row_stride(*x, "x");
+    if (ldx < 0) return nullptr;
+    const at::ScalarType type = x->scalar_type();
+    if (type != at::kBFloat16 && type != at::kHalf) {
+      PyErr_SetString(PyExc_TypeError, "x must be bfloat16 or float16");
+      return nullptr;
+    }
+    if (gate->dim() != 2 || up->dim() != 3 || down->dim() != 3) {
+      PyErr_SetString(PyExc_ValueError, "gate is [E, H], up [L, 2I, H], down [L, H, I]");
+      return nullptr;
+    }
+    const int64_t T = x->size(0), H = x->size(1), E = gate->size(0), L = down->size(0), I = down->size(2);
+    if (!dense(*gate, "gate", type, *x, {E, H}) || !dense(*up, "up", type, *x, {L, 2 * I, H}) ||
+        !dense(*down, "down", type, *x, {L, H, I}) || (bias && !dense(*bias, "bias", at::kFloat, *x, {E})) ||
+        (slot && !dense(*slot, "expert_slot", at::kInt, *x, {E})))
+      return nullptr;
+    if (ws->device() != x->device() || !ws->is_contiguous()) {
+      PyErr_SetString(PyExc_ValueError, "workspace must be contiguous on the same GPU");
+      return nullptr;
+    }
+    const uintptr_t from = reinterpret_cast<uintptr_t>(ws->data_ptr()), at = (from + 255) & ~(uintptr_t)255;
+    const size_t size = ws->nbytes() > at - from ? ws->nbytes() - (at - from) : 0;
+    at::Tensor out = at::empty({T, H}, x->options());
+    at::Tensor ids = at::empty({T, r->topk}, x->options().dtype(at::kInt));
+    at::Tensor weights = at::empty({T, r->topk}, x->options().dtype(at::kFloat));
+    const auto fits = [](int64_t v) { return v <= INT32_MAX; };
+    const topoep_moe m{(int32_t)H, (int32_t)I, (int32_t)L, type == at::kHalf ? TOPOEP_F16 : TOPOEP_BF16};
+    const int rc = !fits(T) || !fits(H) || !fits(I) || !fits(L)
+                       ? TOPOEP_EINVAL
+                       : reinterpret_cast<decltype(&topoep_moe_few)>(entry)(
+                             &m, r, x->data_ptr(), ldx, (int32_t)T, gate->data_ptr(), bias ? bias->data_ptr<float>() : nullptr,
+                             slot ? slot->data_ptr<int32_t>() : nullptr, up->data_ptr(), down->data_ptr(), out.data_ptr(),
+                             ids.data_ptr<int32_t>(), weights.data_ptr<float>(), reinterpret_cast<void *>(at), size,
+                             reinterpret_cast<void *>(stream));
+    return Py_BuildValue("(iNNN)", rc, THPVariable_Wrap(out), THPVariable_Wrap(ids), THPVariable_Wrap(weights));
+  });
+}
+
+PyMethodDef methods[] = {{"moe_few", moe_few, METH_VARARGS,
+                          "moe_few(entry, router, x, gate, up, down, bias, expert_slot, workspace, stream) -> (code, out, ids, weights)"},
+                         {"route", route, METH_VARARGS, "route(entry, router, logits, bias, stream) -> (code, ids, weights)"},
                          {"route_backward", route_backward, METH_VARARGS,
                           "route_backward(entry, router, logits, ids, grad_weights, stream) -> (code, grad_logits)"},
                          {"pack", pack, METH_VARARGS, "pack(grads, outs) -> (bytes, device)"}, {nullptr, nullptr, 0, nullptr}};

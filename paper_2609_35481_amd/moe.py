@@ -65,6 +65,7 @@ for _name, _args in (
     _fn.restype, _fn.argtypes = ctypes.c_int, _args
 
 _ROUTE = ctypes.cast(_lib.topoep_route, _vp).value
+_MOE_FEW = ctypes.cast(_lib.topoep_moe_few, _vp).value
 _ROUTE_BACKWARD = ctypes.cast(_lib.topoep_route_backward, _vp).value
 
 EXPORTS = ("topoep_route", "topoep_route_backward", "topoep_moe_workspace_bytes", "topoep_moe_few",
@@ -85,15 +86,6 @@ def router(E, k, dtype=torch.float32, scoring="softmax", renorm=True, scale=1.0,
 def _check(rc, name):
     if rc != OK:
         raise TopoepError(name, rc)
-
-
-def _rows(t, name):
-    """A CUDA matrix whose rows are dense."""
-    if not t.is_cuda:
-        raise TypeError("%s must be a CUDA tensor" % name)
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise ValueError("%s must be a matrix of dense rows that do not overlap" % name)
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _dense(t, name, shape, dtype, device):
@@ -199,38 +191,19 @@ def moe_few(x, gate, up, down, k, scoring="softmax", renorm=True, scale=1.0, bia
 
 
 def _few(x, gate, up, down, k, rules, bias, expert_slot, workspace):
-    ldx = _rows(x, "x")
-    dev, dtype = x.device, x.dtype
-    stream = _stream_of(dev)
-    if dtype not in (torch.bfloat16, torch.float16):
-        raise TypeError("x must be bfloat16 or float16, not %s" % dtype)
-    T, H = x.shape
-    if gate.dim() != 2 or up.dim() != 3 or down.dim() != 3:
-        raise ValueError("gate is [E, H], up [L, 2I, H], down [L, H, I]")
-    E, (L, _, I) = gate.shape[0], down.shape
-    _dense(gate, "gate", (E, H), dtype, dev)
-    _dense(up, "up", (L, 2 * I, H), dtype, dev)
-    _dense(down, "down", (L, H, I), dtype, dev)
-    if bias is not None:
-        _dense(bias, "bias", (E,), torch.float32, dev)
-    if expert_slot is not None:
-        _dense(expert_slot, "expert_slot", (E,), torch.int32, dev)
-    r = router(E, k, torch.float32, *rules)
-    m = Moe(H, I, L, _TYPES[dtype])
+    stream = _stream_of(x.device)
+    if gate.dim() != 2 or down.dim() != 3 or x.dim() != 2:
+        raise ValueError("x is [T, H], gate [E, H], up [L, 2I, H], down [L, H, I]")
+    r = router(gate.shape[0], k, torch.float32, *rules)
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("x must be bfloat16 or float16, not %s" % x.dtype)
     if workspace is None:
-        workspace = torch.empty(moe_workspace_bytes(H, I, E, L, k, T, dtype) + 255, dtype=torch.uint8, device=dev)
-    elif workspace.device != dev or not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous on %s" % dev)
-    ws = (workspace.data_ptr() + 255) & ~255
-    size = workspace.numel() * workspace.element_size() - (ws - workspace.data_ptr())
-    out = torch.empty((T, H), dtype=dtype, device=dev)
-    ids = torch.empty((T, k), dtype=torch.int32, device=dev)
-    weights = torch.empty((T, k), dtype=torch.float32, device=dev)
-    _check(_lib.topoep_moe_few(m, r, x.data_ptr(), ldx, T, gate.data_ptr(),
-                               bias.data_ptr() if bias is not None else None,
-                               expert_slot.data_ptr() if expert_slot is not None else None, up.data_ptr(),
-                               down.data_ptr(), out.data_ptr(), ids.data_ptr(), weights.data_ptr(), ws, max(size, 0),
-                               stream), "topoep_moe_few")
+        (L, H, I), dtype = down.shape, x.dtype
+        workspace = torch.empty(moe_workspace_bytes(H, I, gate.shape[0], L, k, x.shape[0], dtype) + 255,
+                                dtype=torch.uint8, device=x.device)
+    rc, out, ids, weights = _tensors.moe_few(_MOE_FEW, ctypes.addressof(r), x, gate, up, down, bias, expert_slot,
+                                             workspace, stream)
+    _check(rc, "topoep_moe_few")
     return out, ids, weights
 
 
