@@ -8,8 +8,8 @@
 //   route_backward_chosen_kernel, route_backward_kernel  the gradient where the
 //                      chosen logits alone count, and where all do
 //
-// Bound: the forward by its comparisons (847 vector instructions for 16 rows of
-// 128; 17.6 us of the 22 that 200003 x 128 take, 4.6 TB/s), few tokens by the
+// Bound: the forward by its comparisons (820 vector instructions for 16 rows of
+// 128; 200003 x 128: vector units busy 17.0 of 22.5 us, 5.1 TB/s), few tokens by the
 // chain of one row (3.0 us a launch); the gradient by memory: 200003 x 256 bf16 31
 // us for 102 MB written and 105 read, the lines that hold a chosen logit.
 #include "router.h"
@@ -267,6 +267,9 @@ __device__ inline void list_candidates(const Route &a, const T *row, int sub, co
       raw[i] = row[id[i]];
       bias[i] = Bias ? a.bias[id[i]] : 0.0f;
     }
+    // entries formed among the loads (two scalings of an id, for 16-bit logits and
+    // 32-bit biases) take 133 registers, of the 128 that four waves a SIMD have; behind them 120
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float x = clean_logit(to_float(raw[i]));
