@@ -1,18 +1,19 @@
 // The global gradient norm over many tensors and the clip on gfx950.
 //
-// The tensors' addresses and sizes travel as kernel arguments, so a call copies nothing to the device and may be captured; tensors
-// that follow each other in memory (views of one flat buffer) count as one.  A
-// launch's elements are cut into chunks of kChunk elements that do not cross
-// tensors, and each workgroup walks one contiguous range of chunks.  The norm
+// The tensors' addresses and sizes travel as kernel arguments, so a call copies
+// nothing to the device and may be captured; tensors that follow each other in
+// memory (views of one flat buffer) count as one.  A launch's elements are cut
+// into chunks of kChunk elements that do not cross tensors, and workgroup b takes
+// pieces b, b + grid, ... of kPiece chunks.  The norm
 // kernel leaves one 64-bit partial a workgroup; the reader sums them in a fixed
 // order.  Squares are formed and summed in 64 bits: the square of any 32-bit
 // number is exact there and neither overflows nor vanishes.
 //
-// Bound: memory.  The norm of 1.37 G 16-bit elements runs at 6.5 TB/s (7.0 for
+// Bound: memory.  The norm of 1.37 G 16-bit elements runs at 6.8 TB/s (7.0 for
 // reads alone on this card), the clip of 441 M of them into a 32-bit buffer
-// moves its 2.65 GB at 5.8 TB/s (6.0 for a plain copy).  Loads and stores go past
+// moves its 2.65 GB at 5.7 TB/s (6.0 for a plain copy).  Loads and stores go past
 // the caches (without: 4.6 and 4.5 TB/s).  The pieces lie in the order of the
-// workgroups: one long range a workgroup took the clip 520 us, now 458.
+// workgroups: one long range a workgroup took the clip 520 us, this order 458.
 #include "router.h"
 
 namespace {

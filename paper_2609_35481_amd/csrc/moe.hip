@@ -20,9 +20,9 @@
 // in LDS.
 //
 // Bound: memory, and for one token the chain of three kernels.  128 experts of
-// H = 2048, I = 768, top-8: one token 25 us (76 MB, 11 at the 7.0 TB/s of reads
-// alone), of which gate 3.2, up 13.9, down 7.9; 64 tokens 215 us (1.19 GB, 170),
-// up 133 (6.0 TB/s), down 72 (5.5), gate, route and combine 15, starts 5.
+// H = 2048, I = 768, top-8: one token 24 us (76 MB, 11 at the 7.0 TB/s of reads
+// alone), of which gate 3.3, up 14.7, down 8.1; 64 tokens 209 us (1.19 GB, 170),
+// up 133 (6.0 TB/s), down 72 (5.6), gate, route and combine 15, starts 5.
 #include "router.h"
 
 namespace {
