@@ -487,7 +487,8 @@ __global__ __launch_bounds__(64 * kExpertWaves, 2) void many_kernel(Layer a, int
 // One token: every wave routes it for itself, which takes the routing kernel's
 // 3.6 us and a launch off the path for 2 (one token, 128 experts of H = 2048, I =
 // 768: 26.7 us for the layer without); workgroup 0 leaves what the next kernel
-// reads.
+// reads.  Workgroup b takes tile b % tiles of the token's choices b / tiles, b /
+// tiles + gridDim / tiles, ... here: more than the places where some share one.
 template <class T, int V>
 __global__ __launch_bounds__(64 * kExpertWaves, 4) void one_up_kernel(Layer a, int tiles) {
   __shared__ uint32_t scratch[kExpertWaves][kRouteScratch];
@@ -505,15 +506,16 @@ __global__ __launch_bounds__(64 * kExpertWaves, 4) void one_up_kernel(Layer a, i
     atomicOr(&a.lists.active[mine >> 5], 1u << (mine & 31));
   }
   const uint64_t here = __ballot(slot >= 0);
-  const int n = (int)blockIdx.x / tiles;
-  if (n >= __popcll((unsigned long long)here)) return;
-  const uint64_t before = __ballot(slot >= 0 && count_below(here, 0) == n);
-  const int j = __ffsll((unsigned long long)before) - 1;
   int32_t *pair = reinterpret_cast<int32_t *>(scratch[wave]);
-  if (lane == 0) pair[0] = j;
-  wave_sync();
-  const char *w = static_cast<const char *>(a.up) + (int64_t)readlane_i32(slot, j) * 4 * a.I * a.H;
-  expert_tile<T, true, 4, 1, kExpertWaves, kOne>(a, w, pair, 1, (int)blockIdx.x % tiles, part);
+  for (int n = (int)blockIdx.x / tiles; n < __popcll((unsigned long long)here); n += (int)gridDim.x / tiles) {
+    const uint64_t before = __ballot(slot >= 0 && count_below(here, 0) == n);
+    const int j = __ffsll((unsigned long long)before) - 1;
+    wave_sync();
+    if (lane == 0) pair[0] = j;
+    wave_sync();
+    const char *w = static_cast<const char *>(a.up) + (int64_t)readlane_i32(slot, j) * 4 * a.I * a.H;
+    expert_tile<T, true, 4, 1, kExpertWaves, kOne>(a, w, pair, 1, (int)blockIdx.x % tiles, part);
+  }
 }
 
 // out_t = sum over t's choices in order, of those whose expert is here.
