@@ -285,6 +285,9 @@ constexpr int run_steps(int P, int C, int KS) { return P == 4 ? (C == 1 ? (KS > 
 // How many pairs an expert has, about; kFew serves any number.
 enum Load { kOne, kFew };   // at most 4; mostly up to 16
 
+// Columns' operands a wave's piece of LDS holds the sums of.
+template <int Kind> constexpr int kPieces = Kind == kOne ? 1 : 2;
+
 // A tile of 16 rows of one expert against 16 / P * C of its pairs.  Rows: 8
 // hidden units' gate rows and their up rows (Up), or 16 outputs.  KS = 1: the
 // tile is the wave's own; KS = kExpertWaves: the workgroup's waves share it, each
@@ -314,7 +317,9 @@ __device__ inline void expert_tile(const Layer &a, const char *weights, const in
   // this lane: rows q * 4 + 0..3 of part p, column `token` of part `of`
   const int q = (lane >> 4) % (R / 4), p = (lane >> 4) / (R / 4), token = lane % R, of = lane % kTile / R;
   constexpr int CE = C < 2 ? 1 : 2;   // columns' operands whose sums are joined at a time
-  v4f (*own)[64] = KS == 1 ? part + wave * CE : part;
+  // a wave's piece does not depend on CE: waves with tiles of their own may be at
+  // experts of other counts
+  v4f (*own)[64] = KS == 1 ? part + wave * kPieces<Kind> : part;
 #pragma unroll
   for (int c0 = 0; c0 < C; c0 += CE) {
     if (KS == 1) wave_sync(); else __syncthreads();
@@ -357,7 +362,7 @@ __device__ inline void expert_tile(const Layer &a, const char *weights, const in
 // the experts b / groups, b / groups + gridDim / groups, ... of those with pairs.
 template <class T, bool Up, int KS, int Kind>
 __global__ __launch_bounds__(64 * kExpertWaves, 4) void expert_kernel(Layer a, int groups) {
-  __shared__ v4f part[kExpertWaves * (Kind == kOne ? 1 : 2)][64];
+  __shared__ v4f part[kExpertWaves * kPieces<Kind>][64];
   constexpr int kRows = Up ? 8 : 16;
   const int tiles = ((Up ? a.I : a.H) + kRows - 1) / kRows, group = (int)blockIdx.x % groups;
   const int tile = KS == 1 ? group * kExpertWaves + uniform_i32(threadIdx.x >> 6) : group;

@@ -59,3 +59,13 @@ def test_few_tokens_with_more_experts_here_than_places(T, dtype):
         slot = shared(E, L)
         slot[::3] = -1
         check(T, 64, 32, E, L, k, slot, dtype)
+
+
+@pytest.mark.parametrize("H,I", [(64, 2048), (4096, 64)])   # a wave's own tiles of the first product, of the second
+def test_waves_at_experts_of_other_counts(H, I):
+    """More experts with tokens than places: a workgroup goes on to further
+    experts, and its waves need not be at the same one, here of 1 to 30 tokens each."""
+    for T, E, L, k in ((40, 40, 10, 8), (33, 64, 10, 6), (64, 80, 9, 4)):
+        bias = torch.linspace(-1.5, 1.5, E, device=DEV)
+        check(T, H, I, E, L, k, shared(E, L), bias=bias)
+        check(T, H, I, E, L, k, shared(E, L), torch.float16, bias=bias)
