@@ -639,13 +639,24 @@ struct Backward {
   }
 };
 
+// Every row has lanes of its own, and a grid counts its lanes in 32 bits: more
+// rows than that are several launches.
 template <class T, int LPT, int V, int K, int GL>
 int enqueue_list(const Route &a, hipStream_t st) {
+  constexpr int kMostRows = (1 << 30) / LPT;
   (void)hipGetLastError();
-  const dim3 grid((unsigned)(((int64_t)a.T * LPT + kThreads - 1) / kThreads)), block(kThreads);
-  if (a.bias) hipLaunchKernelGGL((route_list_kernel<T, LPT, V, K, GL, true>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((route_list_kernel<T, LPT, V, K, GL, false>), grid, block, 0, st, a);
-  return hipGetLastError() == hipSuccess ? TOPOEP_OK : TOPOEP_EHIP;
+  for (int64_t t0 = 0; t0 < a.T; t0 += kMostRows) {
+    Route part = a;
+    part.logits = static_cast<const T *>(a.logits) + t0 * a.ld;
+    part.ids = a.ids + t0 * a.r.k;
+    part.weights = a.weights + t0 * a.r.k;
+    part.T = a.T - t0 < kMostRows ? (int)(a.T - t0) : kMostRows;
+    const dim3 grid((unsigned)(((int64_t)part.T * LPT + kThreads - 1) / kThreads)), block(kThreads);
+    if (a.bias) hipLaunchKernelGGL((route_list_kernel<T, LPT, V, K, GL, true>), grid, block, 0, st, part);
+    else hipLaunchKernelGGL((route_list_kernel<T, LPT, V, K, GL, false>), grid, block, 0, st, part);
+    if (hipGetLastError() != hipSuccess) return TOPOEP_EHIP;
+  }
+  return TOPOEP_OK;
 }
 template <class T, int LPT>
 int enqueue_groups(const Route &a, int per_lane, hipStream_t st) {
