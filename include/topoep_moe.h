@@ -88,7 +88,8 @@ int topoep_route(const topoep_router *r, const void *logits, int64_t ld, int32_t
  *   logits, ld    as topoep_route was given them
  *   ids           device int32 [T, k]: topoep_route's (distinct in a row; one
  *                 outside [0, E) is taken for a masked expert)
- *   grad_weights  device float [T, k]
+ *   grad_weights  device float [T, k]; a masked choice's is not used, whatever
+ *                 it holds
  *   grad_logits   device out [T, E] of r->dtype, row t at t * ldg elements
  *                 (ldg >= E); every element of a row is written, columns
  *                 beyond E are not.  Masked logits get zero.

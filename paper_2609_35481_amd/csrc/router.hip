@@ -476,7 +476,8 @@ struct RouteBackward {
 
 // The chosen scores' gradients, back through the renormalisation (and the
 // sigmoid): of the logits where only chosen ones count.  KP lanes hold a row's
-// choices; `in`: this lane has one.
+// choices; `in`: this lane has one.  A score of zero gets no gradient, whatever
+// the others', so that a row's NaN stays off its masked places.
 template <int KP>
 __device__ inline float chosen_gradient(const RouterArgs &r, bool in, float xj, float g) {
   const auto sum_of = [](float v) { return KP == 64 ? row_sum<64>(v) : few_sum<KP>(v); };
@@ -486,13 +487,14 @@ __device__ inline float chosen_gradient(const RouterArgs &r, bool in, float xj, 
       const float sum = sum_of(s), mean = sum_of(g * s);
       g = sum > 0.0f ? (g - mean / sum) / sum : 0.0f;
     }
-    return g * s * sigmoid(-xj);
+    return s > 0.0f ? g * s * sigmoid(-xj) : 0.0f;
   }
   const float m = KP == 64 ? row_maxf<64>(xj) : few_max<KP>(xj);
   const float e = m == -INFINITY ? 0.0f : __expf(xj - m);
   const float sum = sum_of(e);
   const float q = sum > 0.0f ? e / sum : 0.0f;
-  return q * (g - sum_of(g * q));
+  const float mean = sum_of(g * q);
+  return q > 0.0f ? q * (g - mean) : 0.0f;
 }
 
 // Where only the chosen logits count, a wave takes `rows` rows at once: KP
@@ -518,9 +520,10 @@ __global__ __launch_bounds__(kThreads) void route_backward_chosen_kernel(RouteBa
     const bool mine = slot < live && sub < a.r.k;
     const int64_t t = t0 + (mine ? slot : 0);
     const int id = mine ? a.ids[t * a.r.k + sub] : -1;
-    const float g = mine ? a.r.scale * a.grad[t * a.r.k + sub] : 0.0f;
+    const float dw = mine ? a.r.scale * a.grad[t * a.r.k + sub] : 0.0f;
     const bool in = (unsigned)id < (unsigned)E;
     const float xj = in ? clean_logit(to_float(static_cast<const T *>(a.logits)[t * a.ld + id])) : -INFINITY;
+    const float g = xj > -INFINITY ? dw : 0.0f;   // a masked choice's weight is a constant zero
     const float d = chosen_gradient<KP>(a.r, in, xj, g);
     if (in) image[slot * E + id] = from_float<T>(d);
     wave_sync();
@@ -559,9 +562,9 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward 
     const T *row = static_cast<const T *>(a.logits) + (live ? t : t0) * a.ld;
     const bool mine = live && sub < a.r.k;
     const int id = mine ? a.ids[t * a.r.k + sub] : -1;
-    const bool in = (unsigned)id < (unsigned)a.r.E;
-    const float g = mine ? a.r.scale * a.grad[t * a.r.k + sub] : 0.0f;
-    const float xj = in ? clean_logit(to_float(row[id])) : -INFINITY;   // masked: score 0
+    const float xj = (unsigned)id < (unsigned)a.r.E ? clean_logit(to_float(row[id])) : -INFINITY;
+    const bool in = xj > -INFINITY;   // a masked choice's weight is a constant zero
+    const float g = in ? a.r.scale * a.grad[t * a.r.k + sub] : 0.0f;
     float p[V];
     load_logits<T, V>(row, sub * V, a.r.E, p);
     float m = p[0];
@@ -576,13 +579,13 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward 
     }
     sum = row_sum<LPT>(sum);
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    const float back = row_sum<LPT>(in && m != -INFINITY ? g * (__expf(xj - m) * inv) : 0.0f);
+    const float back = row_sum<LPT>(in ? g * (__expf(xj - m) * inv) : 0.0f);
     if (in) d[id] = g;
     wave_sync();
     T out[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      out[v] = from_float<T>(p[v] * inv * (d[sub * V + v] - back));
+      out[v] = from_float<T>(p[v] > 0.0f ? p[v] * inv * (d[sub * V + v] - back) : 0.0f);
     }
     wave_sync();
     if (in) d[id] = 0.0f;
