@@ -135,8 +135,9 @@ int topoep_moe_workspace_bytes(const topoep_moe *m, const topoep_router *r, int3
  *                in it is kept between calls or has to be cleared.  Calls that
  *                share one are ordered on one stream.
  *
- * Products are accumulated in 32 bits; h is rounded to the weights' type
- * (f16: saturated at its largest finite value).  TOPOEP_EINVAL: null
+ * Products are accumulated in 32 bits; h is held in two words of the weights'
+ * type: to 2^-16 of it (bf16), 2^-22 (f16, at least 2^-25; saturated at 2^27).
+ * Outputs are rounded once.  TOPOEP_EINVAL: null
  * pointers, sizes outside their ranges, misaligned buffers; TOPOEP_ELIMIT:
  * T above TOPOEP_MOE_MAX_TOKENS or the router's limits;
  * TOPOEP_EWORKSPACE: workspace too small or misaligned.

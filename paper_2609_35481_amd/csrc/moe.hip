@@ -11,7 +11,8 @@
 //   route   one wave a token: joins the partial sums in order, ids, weights,
 //           and appends the token to its experts' lists
 //   up      16 rows (8 hidden units' gate and up rows) of one expert a wave,
-//           or a workgroup where there are few: h = silu(gate) * up
+//           or a workgroup where there are few: h = silu(gate) * up, kept in two
+//           words of the weights' type
 //   down    the same over h, 16 outputs; every pair's result to the workspace
 //   combine the weighted sum of a token's pairs in the order of its choices
 //
@@ -47,12 +48,32 @@ template <> __device__ inline v4f mfma<F16>(v4i a, v4i b, v4f d) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), d, 0, 0, 0);
 }
 
-// 16 bytes at base + at, zero where not ok.  The base is the workgroup's, the
-// place the lane's own 32-bit one, so that an address costs no arithmetic.
-__device__ inline v4i load16(const char *base, uint32_t at, bool ok) {
-  v4i v = {0, 0, 0, 0};
-  if (ok) v = *reinterpret_cast<const v4i *>(base + at);
-  return v;
+// A hidden value between the two products: two words of the weights' type, so
+// that it keeps 16 bits (bf16) and 22 (f16), below what rounding an output costs,
+// for no byte of weights, only a second matrix instruction an operand.  One word alone put
+// outputs up to 2^-8 (bf16) of their terms away.  f16's first word counts 2^11-fold, so
+// that values up to 2^27 are held, not 65504 alone; its products have sums of their own.
+template <class T> struct Hidden;
+template <> struct Hidden<Bf16> {
+  static constexpr int kSums = 1;
+  static constexpr float kFirst = 1.0f, kMost = INFINITY;
+};
+template <> struct Hidden<F16> {
+  static constexpr int kSums = 2;
+  static constexpr float kFirst = 2048.0f, kMost = 65504.0f;
+};
+// Column operands' words and sums of the first product (Up) and the second.
+template <class T, bool Up> constexpr int kWords = Up ? 1 : 2;
+template <class T, bool Up> constexpr int kSums = Up ? 1 : Hidden<T>::kSums;
+
+__device__ inline float clamp(float f, float most) { return f > most ? most : f < -most ? -most : f; }   // NaN stays
+
+template <class T>
+__device__ inline void split(float h, T &first, T &second) {
+  first = from_float<T>(clamp(h * (1.0f / Hidden<T>::kFirst), Hidden<T>::kMost));
+  const float rest = h - to_float(first) * Hidden<T>::kFirst;
+  // (an infinity's own difference is none)
+  second = from_float<T>(clamp(rest == rest ? rest : 0.0f, Hidden<T>::kMost));
 }
 
 // The pairs (token, choice) by expert, in the workspace.  Waves append to
@@ -78,7 +99,7 @@ struct Layer {
   int32_t *ids;
   float *weights;
   float *logits;        // [kSplits, T, E]
-  void *hidden;         // [T * k, I]
+  void *hidden;         // [T * k, 2, I] first and second words
   float *each;          // [T * k, H] what each pair's expert gives
   Lists lists;
 };
@@ -92,13 +113,33 @@ struct Layer {
 // columns; of D only the products of equal parts are kept.  Memory gives 16
 // rows of 64 bytes 5.0 to 6.2 TB/s, 4 rows of 256 bytes, read past the caches,
 // 7.0 (768 MB, rows of 4 to 28 KB), which the dropped products are cheap for:
-// a tile of 16 rows takes P A operands, so P times the instructions.
+// a tile of 16 rows takes P A operands, so P times the instructions.  The P parts
+// of a row or column are P lanes side by side, and a part is every P-th 16 bytes
+// of it, so that neighbouring lanes read neighbouring bytes: a load then looks up as
+// many lines as it has rows, not one a lane (64 tokens, 128 experts of H = 2048, I =
+// 768, top-8: 211 us, 239 with a lane's neighbours in other rows).
 template <int P>
 struct Parts {
   static constexpr int kCols = kTile / P;    // rows of an A operand, columns of a B operand
   static constexpr int kStep = 32 * P;       // elements of the inner axis
-  // This lane's place in its row of a step.
-  static __device__ int place() { return lane_id() % kTile / kCols * 32 + (lane_id() >> 4) * 8; }
+  // This lane's row (column) of an operand, and its place in a step of it.
+  static __device__ int index() { return lane_id() % kTile / P; }
+  static __device__ int place() { return ((lane_id() >> 4) * P + lane_id() % P) * 8; }
+  // Of an operand's products d the rows (lane / 16) * 4 / P + 0 .. 4 / P - 1 of column
+  // index(), all parts joined, the same in each of the P lanes side by side.
+  static __device__ void join(const v4f &d, float (&s)[4 / P]) {
+    static_assert(P == 2 || P == 4, "");
+    const int part = lane_id() % P;
+#pragma unroll
+    for (int j = 0; j < 4 / P; ++j) {
+      float v = d[j * P];
+#pragma unroll
+      for (int i = 1; i < P; ++i) v = part == i ? d[j * P + i] : v;
+      v += dpp_movf<0xB1>(v);
+      if (P == 4) v += dpp_movf<0x4E>(v);
+      s[j] = v;
+    }
+  }
 };
 
 // The inner axis is streamed in runs of S steps, all of whose loads are in flight
@@ -106,10 +147,11 @@ struct Parts {
 // (two runs a wave in registers: fewer waves, and slower).  Rows and columns
 // that do not exist read an existing one instead (their products are dropped),
 // so that no load of a full run depends on a condition.
-template <class T, int P, int NA, int C, int S>
+template <class T, int P, int NA, int C, int S, int W, int A>
 struct Run {
-  v4i a[S][NA], b[S][C];
-  __device__ void load(const char *rows, const uint32_t (&row)[NA], const char *cols, const uint32_t (&col)[C]) {
+  v4i a[S][NA], b[W][S][C];
+  __device__ void load(const char *rows, const uint32_t (&row)[NA], const char *cols, const uint32_t (&col)[C],
+                       uint32_t word) {
 #pragma unroll
     for (int i = 0; i < NA; ++i)
 #pragma unroll
@@ -118,17 +160,22 @@ struct Run {
         a[s][i] = P > 1 ? __builtin_nontemporal_load(p) : *p;
       }
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int s = 0; s < S; ++s) b[s][c] = *reinterpret_cast<const v4i *>(cols + col[c] + Parts<P>::kStep * 2 * s);
-  }
-  __device__ void multiply(v4f (&d)[NA][C]) const {
-#pragma unroll
-    for (int s = 0; s < S; ++s)
+    for (int w = 0; w < W; ++w)
 #pragma unroll
       for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < NA; ++i) d[i][c] = mfma<T>(a[s][i], b[s][c], d[i][c]);
+        for (int s = 0; s < S; ++s)
+          b[w][s][c] = *reinterpret_cast<const v4i *>(cols + w * word + col[c] + Parts<P>::kStep * 2 * s);
+  }
+  __device__ void multiply(v4f (&d)[A][NA][C]) const {
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int i = 0; i < NA; ++i) d[w % A][i][c] = mfma<T>(a[s][i], b[w][s][c], d[w % A][i][c]);
   }
 };
 
@@ -136,10 +183,11 @@ struct Run {
 // this wave, from the `turn`-th of them on and round (tiles that run side by side
 // then read different places of their rows), and its share of the steps behind
 // the last run.  row, col: bytes from rows and cols to the lane's own place
-// (Parts::place()) of k = 0.
-template <class T, int P, int S, int NA, int C>
+// (Parts::place()) of k = 0; columns are W words of n elements, one behind the
+// other, whose products go to A sums.
+template <class T, int P, int S, int W, int NA, int C, int A>
 __device__ inline void stream(const char *rows, const uint32_t (&row)[NA], const char *cols, const uint32_t (&col)[C],
-                              int n, int first, int every, uint32_t turn, v4f (&d)[NA][C]) {
+                              int n, uint32_t word, int first, int every, uint32_t turn, v4f (&d)[A][NA][C]) {
   constexpr int kRun = Parts<P>::kStep * S;
   const int full = n / kRun;
   if (first < full) {
@@ -147,8 +195,8 @@ __device__ inline void stream(const char *rows, const uint32_t (&row)[NA], const
     int k = (first + (int)(turn % (uint32_t)mine) * every) * kRun;
 #pragma unroll 1
     for (int i = 0; i < mine; ++i) {
-      Run<T, P, NA, C, S> x;
-      x.load(rows + k * 2, row, cols + k * 2, col);
+      Run<T, P, NA, C, S, W, A> x;
+      x.load(rows + k * 2, row, cols + k * 2, col, word);
       k += step;
       if (k >= end) k = first * kRun;
       x.multiply(d);
@@ -161,16 +209,27 @@ __device__ inline void stream(const char *rows, const uint32_t (&row)[NA], const
     const bool in = k + place < n;
     const uint32_t at = in ? (uint32_t)k * 2u : 0u - (uint32_t)place * 2u;
     const v4i zero = {0, 0, 0, 0};
-    v4i w[NA], b[C];
+    v4i a[NA], b[W][C];
+    __builtin_amdgcn_sched_barrier(0);   // (addresses formed before the loop: 16 bytes of scratch for f16)
 #pragma unroll
-    for (int i = 0; i < NA; ++i) w[i] = *reinterpret_cast<const v4i *>(rows + (row[i] + at));
+    for (int i = 0; i < NA; ++i) a[i] = *reinterpret_cast<const v4i *>(rows + (row[i] + at));
 #pragma unroll
-    for (int c = 0; c < C; ++c) b[c] = *reinterpret_cast<const v4i *>(cols + (col[c] + at));
+    for (int w = 0; w < W; ++w)
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+      for (int c = 0; c < C; ++c) b[w][c] = *reinterpret_cast<const v4i *>(cols + (col[c] + w * word + at));
 #pragma unroll
-      for (int i = 0; i < NA; ++i) d[i][c] = mfma<T>(in ? w[i] : zero, in ? b[c] : zero, d[i][c]);
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < NA; ++i) d[w % A][i][c] = mfma<T>(in ? a[i] : zero, in ? b[w][c] : zero, d[w % A][i][c]);
   }
+}
+
+// The sums of a product's words, as one.
+template <class T, int A>
+__device__ inline v4f join_sums(const v4f &first, const v4f &second) {
+  return A == 1 ? first : Hidden<T>::kFirst * first + second;
 }
 
 // ---------------------------------------------------------------- logits
@@ -191,12 +250,13 @@ __global__ __launch_bounds__(64 * kGateWaves) void gate_kernel(Layer a) {
   uint32_t src[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) src[c] = ((uint32_t)imin(c * kTile + col, a.T - 1) * (uint32_t)a.ldx + inner) * 2u;
-  v4f d[1][C] = {};
-  stream<T, 1, 2>(static_cast<const char *>(a.gate), row, static_cast<const char *>(a.x), src, a.H, blockIdx.y * kGateWaves + wave, kSplits * kGateWaves, 0, d);
+  v4f d[1][1][C] = {};
+  stream<T, 1, 2, 1>(static_cast<const char *>(a.gate), row, static_cast<const char *>(a.x), src, a.H, 0,
+                     blockIdx.y * kGateWaves + wave, kSplits * kGateWaves, 0, d);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     if (c > 0) __syncthreads();
-    part[wave][lane] = d[0][c];
+    part[wave][lane] = d[0][0][c];
     __syncthreads();
     const int l = threadIdx.x, t = c * kTile + (l & 15), e = blockIdx.x * kTile + (l >> 4) * 4;
     if (l < 64 && t < a.T) {
@@ -273,20 +333,21 @@ __device__ inline int nth_active(const Layer &a, int n) {
 
 // ---------------------------------------------------------------- experts
 
-template <class T> __device__ inline float saturate(float f) { return f; }
-template <> __device__ inline float saturate<F16>(float f) { return f > 65504.0f ? 65504.0f : f < -65504.0f ? -65504.0f : f; }
-
 constexpr int kExpertWaves = 4;
 
 // Steps of a run by P and C; with few tokens and shared tiles every load of a row
 // of 2048 elements is in flight at once.
-constexpr int run_steps(int P, int C, int KS) { return P == 4 ? (C == 1 ? (KS > 1 ? 4 : 2) : 1) : C <= 4 ? 2 : 1; }
+constexpr int run_steps(int P, int C, int KS, int W) {
+  return P == 4 ? (C == 1 ? (KS > 1 ? (W > 1 ? 3 : 4) : 2) : 1) : 2;
+}
 
 // How many pairs an expert has, about; kFew serves any number.
 enum Load { kOne, kFew };   // at most 4; mostly up to 16
 
-// Columns' operands a wave's piece of LDS holds the sums of.
+// Columns' operands a wave's piece of LDS holds the sums of, and the quads of rows
+// of one of them.
 template <int Kind> constexpr int kPieces = Kind == kOne ? 1 : 2;
+constexpr int kPiece = 32;
 
 // A tile of 16 rows of one expert against 16 / P * C of its pairs.  Rows: 8
 // hidden units' gate rows and their up rows (Up), or 16 outputs.  KS = 1: the
@@ -294,48 +355,57 @@ template <int Kind> constexpr int kPieces = Kind == kOne ? 1 : 2;
 // with its part of the runs.
 template <class T, bool Up, int P, int C, int KS, int Kind>
 __device__ inline void expert_tile(const Layer &a, const char *weights, const int32_t *pairs, int count, int tile,
-                                   v4f (*part)[64]) {
+                                   v4f (*part)[kPiece]) {
   constexpr int R = Parts<P>::kCols, kRows = Up ? 8 : 16;
-  const int lane = lane_id(), wave = uniform_i32(threadIdx.x >> 6), place = Parts<P>::place(), at0 = tile * kRows;
+  const int lane = lane_id(), index = Parts<P>::index(), wave = uniform_i32(threadIdx.x >> 6), place = Parts<P>::place(), at0 = tile * kRows;
   const int n = Up ? a.H : a.I;
   uint32_t row[P], src[C];
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    const int r = i * R + lane % R;
+    const int r = i * R + index;
     row[i] = ((uint32_t)(Up ? (r >> 3) * a.I + imin(at0 + (r & 7), a.I - 1) : imin(at0 + r, a.H - 1)) * n + place) * 2u;
   }
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int at = c * R + lane % R;
+    const int at = c * R + index;
     const int p = pairs[at < count ? at : 0];
-    src[c] = ((Up ? (uint32_t)(p / a.r.k) * (uint32_t)a.ldx : (uint32_t)p * (uint32_t)a.I) + place) * 2u;
+    src[c] = ((Up ? (uint32_t)(p / a.r.k) * (uint32_t)a.ldx : (uint32_t)p * 2u * (uint32_t)a.I) + place) * 2u;
   }
   const char *cols = static_cast<const char *>(Up ? a.x : a.hidden);
-  v4f d[P][C] = {};
+  constexpr int W = kWords<T, Up>, A = kSums<T, Up>;
+  v4f d[A][P][C] = {};
   // eight tiles side by side run on eight XCDs
-  stream<T, P, run_steps(P, C, Kind == kOne ? KS : 1)>(weights, row, cols, src, n, KS == 1 ? 0 : wave, KS, tile >> 3, d);
-  // this lane: rows q * 4 + 0..3 of part p, column `token` of part `of`
-  const int q = (lane >> 4) % (R / 4), p = (lane >> 4) / (R / 4), token = lane % R, of = lane % kTile / R;
+  stream<T, P, run_steps(P, C, Kind == kOne ? KS : 1, W), W>(weights, row, cols, src, n, (uint32_t)n * 2u,
+                                                             KS == 1 ? 0 : wave, KS, tile >> 3, d);
   constexpr int CE = C < 2 ? 1 : 2;   // columns' operands whose sums are joined at a time
   // a wave's piece does not depend on CE: waves with tiles of their own may be at
   // experts of other counts
-  v4f (*own)[64] = KS == 1 ? part + wave * kPieces<Kind> : part;
+  v4f (*own)[kPiece] = KS == 1 ? part + wave * kPieces<Kind> : part;
 #pragma unroll
   for (int c0 = 0; c0 < C; c0 += CE) {
     if (KS == 1) wave_sync(); else __syncthreads();
-    if (p == of) {
 #pragma unroll
-      for (int c = 0; c < CE; ++c)
+    for (int c = 0; c < CE; ++c) {
+      float s[P][4 / P];
 #pragma unroll
-        for (int i = 0; i < P; ++i)
-          own[(KS == 1 ? 0 : wave * CE) + c][((i * P + p) * (R / 4) + q) * R + token] = d[i][c0 + c];
+      for (int i = 0; i < P; ++i)
+        Parts<P>::join(join_sums<T, A>(d[0][i][c0 + c], d[A - 1][i][c0 + c]), s[i]);
+      // of the lanes side by side the i-th leaves operand i's
+      const int i = lane % P, row = i * R + (lane >> 4) * (4 / P);
+      float *to = reinterpret_cast<float *>(&own[(KS == 1 ? 0 : wave * CE) + c][row / 4 * R + index]) + row % 4;
+#pragma unroll
+      for (int j = 0; j < 4 / P; ++j) {
+        float v = s[0][j];
+#pragma unroll
+        for (int o = 1; o < P; ++o) v = i == o ? s[o][j] : v;
+        to[j] = v;
+      }
     }
     if (KS == 1) wave_sync(); else __syncthreads();
     const auto sum = [&](int c, int quad, int t) {   // rows quad * 4 + 0..3 of the tile
-      const v4f *from = &own[c][((quad * 4 / R * P) * (R / 4) + quad % (R / 4)) * R + t];
-      v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-      for (int i = 0; i < KS * P; ++i) s += from[i / P * CE * 64 + i % P * (R / 4) * R];
+      v4f s = own[c][quad * R + t];
+#pragma unroll
+      for (int w = 1; w < KS; ++w) s += own[w * CE + c][quad * R + t];
       return s;
     };
     constexpr int kQuads = Up ? 2 : 4;
@@ -347,10 +417,12 @@ __device__ inline void expert_tile(const Layer &a, const char *weights, const in
       const v4f g = sum(c, quad, t);
       if (Up) {
         const v4f u = sum(c, quad + 2, t);
-        T h[4];
+        T h[2][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) h[j] = from_float<T>(saturate<T>(g[j] * sigmoid(g[j]) * u[j]));
-        __builtin_memcpy(static_cast<T *>(a.hidden) + pair * a.I + at, h, sizeof(h));
+        for (int j = 0; j < 4; ++j) split(g[j] * sigmoid(g[j]) * u[j], h[0][j], h[1][j]);
+        T *to = static_cast<T *>(a.hidden) + pair * 2 * a.I + at;
+        __builtin_memcpy(to, h[0], sizeof(h[0]));
+        __builtin_memcpy(to + a.I, h[1], sizeof(h[1]));
       } else {
         *reinterpret_cast<v4f *>(a.each + pair * a.H + at) = g;
       }
@@ -362,7 +434,7 @@ __device__ inline void expert_tile(const Layer &a, const char *weights, const in
 // the experts b / groups, b / groups + gridDim / groups, ... of those with pairs.
 template <class T, bool Up, int KS, int Kind>
 __global__ __launch_bounds__(64 * kExpertWaves, 4) void expert_kernel(Layer a, int groups) {
-  __shared__ v4f part[kExpertWaves * kPieces<Kind>][64];
+  __shared__ v4f part[kExpertWaves * kPieces<Kind>][kPiece];
   constexpr int kRows = Up ? 8 : 16;
   const int tiles = ((Up ? a.I : a.H) + kRows - 1) / kRows, group = (int)blockIdx.x % groups;
   const int tile = KS == 1 ? group * kExpertWaves + uniform_i32(threadIdx.x >> 6) : group;
@@ -386,17 +458,18 @@ __global__ __launch_bounds__(64 * kExpertWaves, 4) void expert_kernel(Layer a, i
 }
 
 // Many pairs an expert: the columns' operands would cost more of the caches than
-// the rows' of memory, so a workgroup's waves share them.  A stage is 64 or 128 of
+// the rows' of memory, so a workgroup's waves share them.  A stage is 32 to 128 of
 // the inner axis of all of the expert's columns in LDS (chunks of 16 bytes, their
 // places turned by the column so that no bank is met twice), double-buffered;
 // each wave has 32 rows of its own (16 hidden units' gate and up rows, or 32
 // outputs) straight from memory, one stage ahead.
 template <class T, bool Up, int kStage>
-__global__ __launch_bounds__(64 * kExpertWaves, 2) void many_kernel(Layer a, int tiles) {
-  constexpr int kChunks = kStage / 8, kSteps = kStage / 32;
+__global__ __launch_bounds__(64 * kExpertWaves, (kStage * (Up ? 1 : 2) > 128 ? 1 : 2)) void many_kernel(Layer a, int tiles) {
+  constexpr int kChunks = kStage / 8, kSteps = kStage / 32, W = kWords<T, Up>, A = kSums<T, Up>;
   constexpr int kCols = TOPOEP_MOE_MAX_TOKENS / kTile, kEach = 64 * kExpertWaves / kChunks,
                 kUnits = TOPOEP_MOE_MAX_TOKENS / kEach;   // columns a pass of the workgroup stages, and passes
-  __shared__ v4i stage[2][TOPOEP_MOE_MAX_TOKENS][kChunks];
+  __shared__ v4i stage[2][W][TOPOEP_MOE_MAX_TOKENS][kChunks];
+  const auto turned = [](int c) { return kChunks < 8 ? c >> 2 & 3 : c & 7; };
   const int lane = lane_id(), wave = uniform_i32(threadIdx.x >> 6), r = lane & 15, place = (lane >> 4) * 8;
   const int n = Up ? a.H : a.I, rows = Up ? a.I : a.H, stages = (n + kStage - 1) / kStage;
   const int first = ((int)blockIdx.x % tiles * kExpertWaves + wave) * (Up ? 16 : 32);   // of this wave's units or outputs
@@ -415,10 +488,10 @@ __global__ __launch_bounds__(64 * kExpertWaves, 2) void many_kernel(Layer a, int
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {   // this thread's columns and chunk of a stage
       const int c = (int)threadIdx.x / kChunks + kEach * u, p = pairs[c < count ? c : 0];
-      src[u] = ((Up ? (uint32_t)(p / a.r.k) * (uint32_t)a.ldx : (uint32_t)p * (uint32_t)a.I) + threadIdx.x % kChunks * 8) * 2u;
+      src[u] = ((Up ? (uint32_t)(p / a.r.k) * (uint32_t)a.ldx : (uint32_t)p * 2u * (uint32_t)a.I) + threadIdx.x % kChunks * 8) * 2u;
     }
-    v4i x[2][kSteps], b[kUnits];
-    v4f d[2][kCols] = {};
+    v4i x[2][kSteps], b[W][kUnits];
+    v4f d[A][2][kCols] = {};
     const v4i zero = {0, 0, 0, 0};
     // what lies behind the axis reads its start and counts as zero
     const auto load = [&](int k) {
@@ -435,8 +508,11 @@ __global__ __launch_bounds__(64 * kExpertWaves, 2) void many_kernel(Layer a, int
 #pragma unroll
       for (int u = 0; u < kUnits; ++u)
         if (kEach * u < count) {
-          const v4i v = *reinterpret_cast<const v4i *>(from + (src[u] + (in ? (uint32_t)k * 2u : 0u - mine * 2u)));
-          b[u] = in ? v : zero;
+#pragma unroll
+          for (int m = 0; m < W; ++m) {
+            const v4i v = *reinterpret_cast<const v4i *>(from + (src[u] + m * (uint32_t)n * 2u + (in ? (uint32_t)k * 2u : 0u - mine * 2u)));
+            b[m][u] = in ? v : zero;
+          }
         }
     };
     // tiles that run side by side start at different places of their rows
@@ -447,7 +523,8 @@ __global__ __launch_bounds__(64 * kExpertWaves, 2) void many_kernel(Layer a, int
       for (int u = 0; u < kUnits; ++u)
         if (kEach * u < count) {
           const int c = (int)threadIdx.x / kChunks + kEach * u;
-          stage[g & 1][c][threadIdx.x % kChunks ^ (c & 7)] = b[u];
+#pragma unroll
+          for (int m = 0; m < W; ++m) stage[g & 1][m][c][threadIdx.x % kChunks ^ turned(c)] = b[m][u];
         }
       v4i now[2][kSteps];
 #pragma unroll
@@ -463,9 +540,12 @@ __global__ __launch_bounds__(64 * kExpertWaves, 2) void many_kernel(Layer a, int
 #pragma unroll
           for (int s = 0; s < kSteps; ++s) {
             const int at = c * kTile + r;
-            const v4i col = stage[g & 1][at][(s * 4 + (lane >> 4)) ^ (at & 7)];
 #pragma unroll
-            for (int q = 0; q < 2; ++q) d[q][c] = mfma<T>(now[q][s], col, d[q][c]);
+            for (int m = 0; m < W; ++m) {
+              const v4i col = stage[g & 1][m][at][(s * 4 + (lane >> 4)) ^ turned(at)];
+#pragma unroll
+              for (int q = 0; q < 2; ++q) d[m % A][q][c] = mfma<T>(now[q][s], col, d[m % A][q][c]);
+            }
           }
         }
     }
@@ -475,14 +555,19 @@ __global__ __launch_bounds__(64 * kExpertWaves, 2) void many_kernel(Layer a, int
       if (c * kTile + r >= count) continue;
       const int64_t pair = pairs[c * kTile + r];
       if (Up) {
-        T h[4];
+        const v4f g = d[0][0][c], up = d[0][1][c];
+        T h[2][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) h[j] = from_float<T>(saturate<T>(d[0][c][j] * sigmoid(d[0][c][j]) * d[1][c][j]));
-        if (at < rows) __builtin_memcpy(static_cast<T *>(a.hidden) + pair * a.I + at, h, sizeof(h));
+        for (int j = 0; j < 4; ++j) split(g[j] * sigmoid(g[j]) * up[j], h[0][j], h[1][j]);
+        T *to = static_cast<T *>(a.hidden) + pair * 2 * a.I + at;
+        if (at < rows) {
+          __builtin_memcpy(to, h[0], sizeof(h[0]));
+          __builtin_memcpy(to + a.I, h[1], sizeof(h[1]));
+        }
       } else {
         float *to = a.each + pair * a.H + at;
-        if (at < rows) *reinterpret_cast<v4f *>(to) = d[0][c];
-        if (at + 16 < rows) *reinterpret_cast<v4f *>(to + 16) = d[1][c];
+        if (at < rows) *reinterpret_cast<v4f *>(to) = join_sums<T, A>(d[0][0][c], d[A - 1][0][c]);
+        if (at + 16 < rows) *reinterpret_cast<v4f *>(to + 16) = join_sums<T, A>(d[0][1][c], d[A - 1][1][c]);
       }
     }
     __syncthreads();   // before the next expert's stages
@@ -497,7 +582,7 @@ __global__ __launch_bounds__(64 * kExpertWaves, 2) void many_kernel(Layer a, int
 template <class T, int V>
 __global__ __launch_bounds__(64 * kExpertWaves, 4) void one_up_kernel(Layer a, int tiles) {
   __shared__ uint32_t scratch[kExpertWaves][kRouteScratch];
-  __shared__ v4f part[kExpertWaves][64];
+  __shared__ v4f part[kExpertWaves][kPiece];
   const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id();
   const bool writes = blockIdx.x == 0 && wave == 0;
   float x[V], b[V];
@@ -563,34 +648,39 @@ constexpr int kDownWaves = 8;
 template <class T, int NA, int C>
 __device__ inline void down_unit(const Layer &a, const char *weights, int o0, const int32_t *pairs, int count, int lo,
                                  int len, v4f *mine) {
-  const int lane = lane_id(), place = Parts<4>::place();
+  const int lane = lane_id(), index = Parts<4>::index(), place = Parts<4>::place();
   uint32_t row[NA], src[C];
   int pair[C];
 #pragma unroll
-  for (int i = 0; i < NA; ++i) row[i] = ((uint32_t)imin(o0 + 4 * i + lane % 4, a.H - 1) * a.I + place) * 2u;
+  for (int i = 0; i < NA; ++i) row[i] = ((uint32_t)imin(o0 + 4 * i + index, a.H - 1) * a.I + place) * 2u;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int at = c * 4 + lane % 4;
+    const int at = c * 4 + index;
     pair[c] = pairs[at < count ? at : 0];
-    src[c] = ((uint32_t)pair[c] * (uint32_t)a.I + place) * 2u;
+    src[c] = ((uint32_t)pair[c] * 2u * (uint32_t)a.I + place) * 2u;
     if (at >= count) pair[c] = -1;
   }
   const char *cols = static_cast<const char *>(a.hidden);
-  v4f d[NA][C] = {};
+  constexpr int W = kWords<T, false>, A = kSums<T, false>;
+  const uint32_t word = (uint32_t)a.I * 2u;
+  v4f d[A][NA][C] = {};
   // four steps (512 elements) in flight, then two, then one
   constexpr int kLong = 4 * Parts<4>::kStep;
   const int most = len / kLong * kLong;
-  if (C == 1) stream<T, 4, 4>(weights + lo * 2, row, cols + lo * 2, src, most, 0, 1, blockIdx.x / 8, d);
+  if (C == 1) stream<T, 4, 4, W>(weights + lo * 2, row, cols + lo * 2, src, most, word, 0, 1, blockIdx.x / 8, d);
   const int done = C == 1 ? most : 0;
-  stream<T, 4, 2>(weights + (lo + done) * 2, row, cols + (lo + done) * 2, src, len - done, 0, 1, 0, d);
-  // part p's sums of outputs 4 i + 0..3 and column `token`
-  const int p = lane >> 4, of = lane % kTile / 4;
+  stream<T, 4, 2, W>(weights + (lo + done) * 2, row, cols + (lo + done) * 2, src, len - done, word, 0, 1, 0, d);
+  // output 4 i + lane / 16 of this lane's column, left by the i-th of the lanes side by side
 #pragma unroll
   for (int c = 0; c < C; ++c)
-    if (p == of && pair[c] >= 0) {
-      v4f *to = mine + (pair[c] / a.r.k * 4 + p) * NA;
 #pragma unroll
-      for (int i = 0; i < NA; ++i) to[i] = to[i] + a.weights[pair[c]] * d[i][c];
+    for (int i = 0; i < NA; ++i) {
+      float s[1];
+      Parts<4>::join(join_sums<T, A>(d[0][i][c], d[A - 1][i][c]), s);
+      if (lane % 4 == i && pair[c] >= 0) {
+        float *to = reinterpret_cast<float *>(mine + pair[c] / a.r.k * NA + i) + (lane >> 4);
+        *to = *to + a.weights[pair[c]] * s[0];
+      }
     }
 }
 
@@ -599,8 +689,8 @@ __device__ inline void down_unit(const Layer &a, const char *weights, int o0, co
 // expert, a part of the inner axis) in turn, each into LDS sums of its own.
 template <class T, int NA>
 __global__ __launch_bounds__(64 * kDownWaves, 3) void down_kernel(Layer a) {
-  extern __shared__ v4f sums[];   // [kDownWaves][T][4 parts][NA]
-  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), size = a.T * 4 * NA;
+  extern __shared__ v4f sums[];   // [kDownWaves][T][NA]
+  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), size = a.T * NA;
   const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int i = threadIdx.x; i < kDownWaves * size; i += 64 * kDownWaves) sums[i] = zero;
   __syncthreads();
@@ -628,9 +718,7 @@ __global__ __launch_bounds__(64 * kDownWaves, 3) void down_kernel(Layer a) {
     const int t = i / NA, at = i % NA, row = (blockIdx.x * NA + at) * 4;
     v4f s = zero;
 #pragma unroll
-    for (int w = 0; w < kDownWaves; ++w)
-#pragma unroll
-      for (int p = 0; p < 4; ++p) s += sums[w * size + (t * 4 + p) * NA + at];
+    for (int w = 0; w < kDownWaves; ++w) s += sums[w * size + t * NA + at];
     if (row >= a.H) continue;
     T out[4];
 #pragma unroll
@@ -660,7 +748,7 @@ Places places_of(const topoep_moe *m, const topoep_router *r, int T) {
   p.logits = at;
   at += align256(kSplits * T * E * sizeof(float));
   p.hidden = at;
-  at += align256(pairs * m->inter * 2);
+  at += align256(pairs * m->inter * 4);
   p.each = at;
   at += align256(pairs * m->hidden * sizeof(float));
   p.total = at;
@@ -703,28 +791,41 @@ int enqueue_experts(const Layer &a, int experts, hipStream_t st) {
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
+template <class T, bool Up, int kStage>
+int enqueue_many(const Layer &a, int blocks, int tiles, hipStream_t st) {
+  hipLaunchKernelGGL((many_kernel<T, Up, kStage>), dim3((unsigned)blocks), dim3(64 * kExpertWaves), 0, st, a, tiles);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
 template <class T, bool Up>
 int enqueue_experts(const Layer &a, hipStream_t st) {
   const int experts = imin(imin(a.T * a.r.k, a.r.E), a.L);   // with pairs, about
   if (a.T <= 4) return enqueue_experts<T, Up, kOne>(a, experts, st);
   const int rows = kExpertWaves * (Up ? 16 : 32), tiles = ((Up ? a.I : a.H) + rows - 1) / rows;
-  // more than 12 pairs an expert (64 experts, 128 tokens, top-8: 163 us shared, 255
-  // not; 64 tokens: 154 either way)
+  // more than 12 pairs an expert (64 experts of H = 2048, I = 768, top-8: 128 tokens 178 us
+  // shared, 219 not; 96 tokens, 12 pairs: 171 and 178; 64 tokens: 166 and 141)
   if (a.T * a.r.k <= 12 * a.r.E) return enqueue_experts<T, Up, kFew>(a, experts, st);
-  // Stages of 128 read rows in longer pieces (8 experts of I = 14336: 672 us, 769
-  // with 64) but two workgroups fit a CU, not three: taken where the chip's rounds
-  // leave it no more than a seventh emptier (20 experts of I = 2048: 328 and 250 us)
+  // Longer stages read rows in longer pieces, but fewer workgroups fit a CU: of the
+  // first product three with stages of 64 and two with 128, of the second (two words)
+  // three with 32, two with 64, one with 128.  The longer one where the chip's rounds leave
+  // it no more than a seventh emptier (second product, 8 experts of I = 14336, 256 workgroups:
+  // layer 820, 799 and 751 us; 20 experts of I = 2048, 640 workgroups: 289, 314, 348).
   const int blocks = experts * tiles, rounds2 = (blocks + 511) / 512, rounds3 = (blocks + 767) / 768;
-  const dim3 grid((unsigned)blocks), block(64 * kExpertWaves);
-  if (rounds2 * 512 * 6 <= rounds3 * 768 * 7) hipLaunchKernelGGL((many_kernel<T, Up, 128>), grid, block, 0, st, a, tiles);
-  else hipLaunchKernelGGL((many_kernel<T, Up, 64>), grid, block, 0, st, a, tiles);
-  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+  const bool longer = rounds2 * 512 * 6 <= rounds3 * 768 * 7;
+  if constexpr (Up) {
+    return longer ? enqueue_many<T, true, 128>(a, blocks, tiles, st) : enqueue_many<T, true, 64>(a, blocks, tiles, st);
+  } else {
+    if (blocks <= 256) return enqueue_many<T, false, 128>(a, blocks, tiles, st);
+    if constexpr (kSums<T, false> == 1)   // (f16: its sums' registers let two workgroups run at most)
+      if (!longer) return enqueue_many<T, false, 32>(a, blocks, tiles, st);
+    return enqueue_many<T, false, 64>(a, blocks, tiles, st);
+  }
 }
 
 template <class T, int NA>
 int enqueue_down_rows(const Layer &a, hipStream_t st) {
   hipLaunchKernelGGL((down_kernel<T, NA>), dim3((a.H + 4 * NA - 1) / (4 * NA)), dim3(64 * kDownWaves),
-                     kDownWaves * a.T * 4 * NA * sizeof(v4f), st, a);
+                     kDownWaves * a.T * NA * sizeof(v4f), st, a);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
