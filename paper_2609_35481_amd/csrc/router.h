@@ -79,12 +79,15 @@ __device__ inline uint32_t row_max(uint32_t v) {
 }
 template <int C>
 __device__ inline float dpp_movf(float v) { return __uint_as_float(dpp_mov<C>(__float_as_uint(v))); }
+// Sums go over a row's places as one binary tree of neighbours, first inside a
+// lane, then over the lanes, whatever their number: a row's sum has the same
+// bits in every form (places that hold nothing add zero).
 template <int LPT>
 __device__ inline float row_sum(float v) {
-  v += dpp_movf<0x128>(v);
-  v += dpp_movf<0x124>(v);
-  v += dpp_movf<0x122>(v);
-  v += dpp_movf<0x121>(v);
+  if (LPT > 1) v += dpp_movf<0xB1>(v);
+  if (LPT > 2) v += dpp_movf<0x4E>(v);
+  if (LPT > 4) v += dpp_movf<0x141>(v);
+  if (LPT > 8) v += dpp_movf<0x140>(v);
   if (LPT == 64) {
     const int u = (int)__float_as_uint(v);
     v = (__uint_as_float((uint32_t)__builtin_amdgcn_readlane(u, 0)) +
@@ -94,12 +97,23 @@ __device__ inline float row_sum(float v) {
   }
   return v;
 }
+template <int V>
+__device__ inline float lane_sum(const float (&v)[V]) {
+  float s[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) s[i] = v[i];
+#pragma unroll
+  for (int d = 1; d < V; d *= 2)
+#pragma unroll
+    for (int i = 0; i < V; i += 2 * d) s[i] += s[i + d];
+  return s[0];
+}
 template <int LPT>
 __device__ inline float row_maxf(float v) {
-  v = fmaxf(v, dpp_movf<0x128>(v));
-  v = fmaxf(v, dpp_movf<0x124>(v));
-  v = fmaxf(v, dpp_movf<0x122>(v));
-  v = fmaxf(v, dpp_movf<0x121>(v));
+  if (LPT > 1) v = fmaxf(v, dpp_movf<0xB1>(v));
+  if (LPT > 2) v = fmaxf(v, dpp_movf<0x4E>(v));
+  if (LPT > 4) v = fmaxf(v, dpp_movf<0x141>(v));
+  if (LPT > 8) v = fmaxf(v, dpp_movf<0x140>(v));
   if (LPT == 64) {
     const int u = (int)__float_as_uint(v);
     v = fmaxf(fmaxf(__uint_as_float((uint32_t)__builtin_amdgcn_readlane(u, 0)),
@@ -129,6 +143,32 @@ __device__ inline void load_logits(const T *row, int base, int E, float (&x)[V])
 constexpr int kRouteScratch = 2 * TOPOEP_ROUTER_MAX_TOPK + 64;
 
 __device__ inline float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }
+
+// exp(x - from), x <= from, to 1.5 x 2^-23 of it.  In 32 bits the difference and its
+// product with log2 e are off by |x - from| 2^-24 each, which the exponential makes
+// relative; both are formed in 64, and what 32 bits of them leave comes in as a factor.
+__device__ inline float exp_from(float x, float from) {
+  constexpr double kLog2e = 0x1.71547652b82fep+0;
+  constexpr float kLn2 = 0x1.62e430p-1f;
+  const double t = fmax(((double)x - (double)from) * kLog2e, -200.0);   // 0 from -150 on
+  const float near = (float)t, rest = (float)(t - (double)near);
+  const float e = __builtin_amdgcn_exp2f(near);
+  return fmaf(e, rest * kLn2, e);
+}
+// A term of a sum of exp(d) next to one of 1: roundings of d and of its product move it
+// by |d| exp(d) 2^-23 < 0.8 x 2^-24 of the sum.
+__device__ inline float exp_term(float d) { return __expf(d); }
+
+// A chosen logit's sigmoid score: exp(min(x, 0)) / (1 + exp(-|x|)).
+__device__ inline float sigmoid_score(float x) {
+  const float e = exp_from(-fabsf(x), 0.0f), y = 1.0f + e;
+  float r = __builtin_amdgcn_rcpf(y);
+  r = fmaf(fmaf(-y, r, 1.0f), r, r);   // 1 <= y <= 2: a step takes the reciprocal's error out
+  return (x < 0.0f ? e : 1.0f) * r;
+}
+
+// The factor of a row's scores: the scale, over their sum where they have one.
+__device__ inline float over(float scale, float sum) { return sum > 0.0f ? scale / sum : 0.0f; }
 
 // Chooses a row's k experts and their weights.  x: the cleaned logits of
 // experts sub * V .. + V - 1 (sub = this lane's place in the row), b: their
@@ -186,32 +226,29 @@ __device__ inline void route_row(const RouterArgs &r, const float (&x)[V], const
   const int id = mine ? (int)scratch[2 * sub] : 0;
   const float xj = mine ? __uint_as_float(scratch[2 * sub + 1]) : -INFINITY;
   wave_sync();
-  float s;
+  float s, f = r.scale;
   if (r.sigmoid) {
-    s = mine ? sigmoid(xj) : 0.0f;
-    if (r.renorm) {
-      const float sum = row_sum<LPT>(s);
-      s = sum > 0.0f ? s / sum : 0.0f;
-    }
+    s = mine ? sigmoid_score(xj) : 0.0f;
+    if (r.renorm) f = over(r.scale, row_sum<LPT>(s));
   } else if (r.renorm) {
     const float m = row_maxf<LPT>(xj);
-    s = m == -INFINITY ? 0.0f : __expf(xj - m);
-    const float sum = row_sum<LPT>(s);
-    s = sum > 0.0f ? s / sum : 0.0f;
+    s = exp_from(xj, m == -INFINITY ? 0.0f : m);
+    f = over(r.scale, row_sum<LPT>(s));
   } else {
     float m = x[0];
 #pragma unroll
     for (int v = 1; v < V; ++v) m = fmaxf(m, x[v]);
     m = row_maxf<LPT>(m);
-    float sum = 0.0f;
+    const float from = m == -INFINITY ? 0.0f : m;
+    float e[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) sum += m == -INFINITY ? 0.0f : __expf(x[v] - m);
-    sum = row_sum<LPT>(sum);
-    s = sum > 0.0f ? __expf(xj - m) / sum : 0.0f;
+    for (int v = 0; v < V; ++v) e[v] = exp_term(x[v] - from);
+    f = over(r.scale, row_sum<LPT>(lane_sum(e)));
+    s = exp_from(xj, from);
   }
   if (live && mine) {
     ids[sub] = id;
-    weights[sub] = r.scale * s;
+    weights[sub] = s * f;
   }
 }
 

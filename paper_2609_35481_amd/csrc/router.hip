@@ -162,23 +162,6 @@ __device__ inline void merge_row(double (&l)[K]) {
   if (LPT > 4) merge_over<K, 0x141>(l);
   if (LPT > 8) merge_over<K, 0x140>(l);
 }
-template <int LPT>
-__device__ inline float few_max(float v) {
-  if (LPT > 1) v = fmaxf(v, dpp_movf<0xB1>(v));
-  if (LPT > 2) v = fmaxf(v, dpp_movf<0x4E>(v));
-  if (LPT > 4) v = fmaxf(v, dpp_movf<0x141>(v));
-  if (LPT > 8) v = fmaxf(v, dpp_movf<0x140>(v));
-  return v;
-}
-template <int LPT>
-__device__ inline float few_sum(float v) {
-  if (LPT > 1) v += dpp_movf<0xB1>(v);
-  if (LPT > 2) v += dpp_movf<0x4E>(v);
-  if (LPT > 4) v += dpp_movf<0x141>(v);
-  if (LPT > 8) v += dpp_movf<0x140>(v);
-  return v;
-}
-
 // The groups' largest keys in LDS (`best`, a word a group), where groups and
 // lanes need not fit.
 template <int LPT, int V, class Key>
@@ -313,11 +296,12 @@ __global__ __launch_bounds__(kThreads, V <= 32 ? 4 : 2) void route_list_kernel(R
     most = x[0];
 #pragma unroll
     for (int v = 1; v < V; ++v) most = fmaxf(most, x[v]);
-    most = few_max<LPT>(most);
+    most = row_maxf<LPT>(most);
     const float from = most == -INFINITY ? 0.0f : most;
+    float e[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) all += __expf(x[v] - from);
-    all = few_sum<LPT>(all);
+    for (int v = 0; v < V; ++v) e[v] = exp_term(x[v] - from);
+    all = row_sum<LPT>(lane_sum(e));
   }
   if constexpr (Bias) {
 #pragma unroll
@@ -411,32 +395,22 @@ __global__ __launch_bounds__(kThreads, V <= 32 ? 4 : 2) void route_list_kernel(R
 #pragma unroll
     for (int j = 0; j < K; ++j) s[j] = j < a.r.k ? clean_logit(to_float(row[entry_id(l[j])])) : -INFINITY;
   }
+  float f = a.r.scale, m = s[0];   // m: the largest chosen logit, or of all
+#pragma unroll
+  for (int j = 1; j < K; ++j) m = j < a.r.k ? fmaxf(m, s[j]) : m;
   if (a.r.sigmoid) {
-    float sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < K; ++j) {
-      s[j] = j < a.r.k ? __builtin_amdgcn_rcpf(1.0f + __expf(-s[j])) : 0.0f;
-      sum += s[j];
-    }
-    const float f = a.r.renorm ? (sum > 0.0f ? a.r.scale / sum : 0.0f) : a.r.scale;
-#pragma unroll
-    for (int j = 0; j < K; ++j) s[j] *= f;
+    for (int j = 0; j < K; ++j) s[j] = j < a.r.k ? sigmoid_score(s[j]) : 0.0f;
+    if (a.r.renorm) f = over(a.r.scale, lane_sum(s));
   } else {
-    float m, sum = 0.0f;
-    if (a.r.renorm) {
-      m = s[0];
+    if (!a.r.renorm) m = most;
+    const float from = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-      for (int j = 1; j < K; ++j) m = j < a.r.k ? fmaxf(m, s[j]) : m;
-#pragma unroll
-      for (int j = 0; j < K; ++j) sum += j < a.r.k && m != -INFINITY ? __expf(s[j] - m) : 0.0f;
-    } else {
-      m = most;
-      sum = all;
-    }
-    const float f = sum > 0.0f ? a.r.scale / sum : 0.0f, from = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-    for (int j = 0; j < K; ++j) s[j] = __expf(s[j] - from) * f;
+    for (int j = 0; j < K; ++j) s[j] = j < a.r.k ? exp_from(s[j], from) : 0.0f;
+    f = over(a.r.scale, a.r.renorm ? lane_sum(s) : all);
   }
+#pragma unroll
+  for (int j = 0; j < K; ++j) s[j] *= f;
   if (!live) return;
   int32_t *ids = a.ids + t * a.r.k;
   float *weights = a.weights + t * a.r.k;
@@ -480,20 +454,18 @@ struct RouteBackward {
 // the others', so that a row's NaN stays off its masked places.
 template <int KP>
 __device__ inline float chosen_gradient(const RouterArgs &r, bool in, float xj, float g) {
-  const auto sum_of = [](float v) { return KP == 64 ? row_sum<64>(v) : few_sum<KP>(v); };
+  const float m = r.renorm ? row_maxf<KP>(xj) : 0.0f;
   if (r.sigmoid) {
-    const float s = in ? sigmoid(xj) : 0.0f;
+    float s = in ? sigmoid_score(xj) : 0.0f;
     if (r.renorm) {
-      const float sum = sum_of(s), mean = sum_of(g * s);
-      g = sum > 0.0f ? (g - mean / sum) / sum : 0.0f;
+      s *= over(1.0f, row_sum<KP>(s));
+      g -= row_sum<KP>(g * s);
     }
-    return s > 0.0f ? g * s * sigmoid(-xj) : 0.0f;
+    return s > 0.0f ? g * s * sigmoid_score(-xj) : 0.0f;
   }
-  const float m = KP == 64 ? row_maxf<64>(xj) : few_max<KP>(xj);
-  const float e = m == -INFINITY ? 0.0f : __expf(xj - m);
-  const float sum = sum_of(e);
-  const float q = sum > 0.0f ? e / sum : 0.0f;
-  const float mean = sum_of(g * q);
+  const float e = exp_from(xj, m == -INFINITY ? 0.0f : m);
+  const float q = e * over(1.0f, row_sum<KP>(e));
+  const float mean = row_sum<KP>(g * q);
   return q > 0.0f ? q * (g - mean) : 0.0f;
 }
 
@@ -571,15 +543,11 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(RouteBackward 
 #pragma unroll
     for (int v = 1; v < V; ++v) m = fmaxf(m, p[v]);
     m = row_maxf<LPT>(m);
-    float sum = 0.0f;
+    const float from = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      p[v] = m == -INFINITY ? 0.0f : __expf(p[v] - m);
-      sum += p[v];
-    }
-    sum = row_sum<LPT>(sum);
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    const float back = row_sum<LPT>(in ? g * (__expf(xj - m) * inv) : 0.0f);
+    for (int v = 0; v < V; ++v) p[v] = exp_term(p[v] - from);
+    const float inv = over(1.0f, row_sum<LPT>(lane_sum(p)));
+    const float back = row_sum<LPT>(in ? g * (exp_term(xj - from) * inv) : 0.0f);
     if (in) d[id] = g;
     wave_sync();
     T out[V];

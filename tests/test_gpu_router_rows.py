@@ -53,3 +53,52 @@ def test_weights_gradients_of_masked_choices_are_not_used(scoring, renorm, E, k,
         got = moe.route_backward(x, ids, grad, scoring=scoring, renorm=renorm)
         torch.cuda.synchronize()
         assert not bool(got[torch.isinf(x)].any()) and torch.equal(got[1::2], want[1::2])
+
+
+SCORES = [("softmax", True), ("softmax", False), ("sigmoid", True), ("sigmoid", False)]
+
+
+def draw(T, E, std, dtype=torch.float32, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed + 31 * T + E)
+    return torch.randn((T, E), generator=g, device=DEV).mul_(std).to(dtype)
+
+
+def in_64_bits(x, ids, scoring, renorm):
+    x, at = x.double(), ids.long()
+    if scoring == "sigmoid":
+        s = torch.sigmoid(x.gather(1, at))
+        return s / s.sum(1, keepdim=True) if renorm else s
+    return torch.softmax(x.gather(1, at), 1) if renorm else torch.softmax(x, 1).gather(1, at)
+
+
+@pytest.mark.parametrize("scoring,renorm", SCORES)
+@pytest.mark.parametrize("E,k", [(16, 2), (37, 5), (64, 8), (100, 12), (128, 8), (200, 16), (256, 4), (512, 8), (1000, 20)])
+def test_a_row_has_the_same_bits_in_any_batch(E, k, scoring, renorm):
+    """One token, some, many: other kernels, the same ids and weights."""
+    for dtype in (torch.float32, torch.bfloat16):
+        x = draw(20000, E, 2.0, dtype)
+        x[7, 2:] = float("-inf")
+        x[9] = float("-inf")
+        print("batches", E, k, scoring, renorm, dtype, flush=True)
+        for kw in (dict(), dict(groups=4, top_groups=2, bias=draw(1, E, 0.3)[0]) if E % 8 == 0 and k <= E // 2 else dict()):
+            ids, w = moe.route(x, k, scoring=scoring, renorm=renorm, scale=2.5, **kw)
+            for n in (1, 11, 500, 5000):
+                i, v = moe.route(x[:n], k, scoring=scoring, renorm=renorm, scale=2.5, **kw)
+                assert torch.equal(i, ids[:n]) and torch.equal(v, w[:n]), n
+
+
+@pytest.mark.parametrize("scoring,renorm", SCORES)
+@pytest.mark.parametrize("E,k", [(16, 4), (128, 8), (130, 12), (512, 8)])
+@pytest.mark.parametrize("T", [5, 9000])
+def test_weights_to_32_bits(T, E, k, scoring, renorm):
+    """Logits far apart.  An exponential is off by 1.5 x 2^-23 relative, a sum of them by
+    that, by its terms' |d| exp(d) 2^-23 < 0.8 x 2^-24, and by half a unit for each of
+    log2 E levels; reciprocal, quotient and product add four half units: (12 +
+    log2 E) 2^-24.  Scores below 2^-126 vanish (1.2e-38, times the scale)."""
+    x = draw(T, E, 12.0)
+    print("weights", T, E, k, scoring, renorm, flush=True)
+    ids, w = moe.route(x, k, scoring=scoring, renorm=renorm, scale=2.5)
+    want = 2.5 * in_64_bits(x, ids, scoring, renorm)
+    bound = (12 + (E - 1).bit_length()) * 2.0 ** -24
+    off = (w.double() - want).abs()
+    assert bool((off <= bound * want + 1e-37).all()), float(((off - 1e-37) / want).max() / 2.0 ** -24)
