@@ -71,8 +71,9 @@ typedef struct topoep_router {
  *            topoep_plan takes them.
  *   weights  device float out [T, k]: c times the score.  Softmax scores are
  *            over all E logits, or with renorm over the chosen ones; sigmoid
- *            scores with renorm are divided by the chosen scores' sum.  Where
- *            a sum is zero (every logit masked) the weights are zero.
+ *            scores with renorm are divided by the chosen scores' sum (where the
+ *            largest is below e^-709, which ends 64 bits, it counts as zero).
+ *            Where a sum is zero (every logit masked) the weights are zero.
  *
  * T = 0 enqueues nothing.  TOPOEP_EINVAL: null pointers (bias excepted),
  * sizes outside the ranges of topoep_router, T < 0 or T * k > INT32_MAX, ld <

@@ -159,13 +159,18 @@ __device__ inline float exp_from(float x, float from) {
 // by |d| exp(d) 2^-23 < 0.8 x 2^-24 of the sum.
 __device__ inline float exp_term(float d) { return __expf(d); }
 
-// A chosen logit's sigmoid score: exp(min(x, 0)) / (1 + exp(-|x|)).
-__device__ inline float sigmoid_score(float x) {
+// A chosen logit's sigmoid score times exp(-top), where top (0, or the largest
+// chosen logit below it, when only the scores' ratios count) keeps it from
+// vanishing: exp(min(x, 0) - top) / (1 + exp(-|x|)).
+__device__ inline float sigmoid_score(float x, float top) {
   const float e = exp_from(-fabsf(x), 0.0f), y = 1.0f + e;
   float r = __builtin_amdgcn_rcpf(y);
   r = fmaf(fmaf(-y, r, 1.0f), r, r);   // 1 <= y <= 2: a step takes the reciprocal's error out
-  return (x < 0.0f ? e : 1.0f) * r;
+  return (top < 0.0f ? exp_from(fminf(x, 0.0f), top) : x < 0.0f ? e : 1.0f) * r;
 }
+// `top` for renormalised scores with largest chosen logit m.  Scores below
+// e^-709, where one in 64 bits ends, are zero.
+__device__ inline float sigmoid_top(float m) { return m >= -709.0f ? fminf(m, 0.0f) : 0.0f; }
 
 // The factor of a row's scores: the scale, over their sum where they have one.
 __device__ inline float over(float scale, float sum) { return sum > 0.0f ? scale / sum : 0.0f; }
@@ -228,7 +233,8 @@ __device__ inline void route_row(const RouterArgs &r, const float (&x)[V], const
   wave_sync();
   float s, f = r.scale;
   if (r.sigmoid) {
-    s = mine ? sigmoid_score(xj) : 0.0f;
+    const float top = r.renorm ? sigmoid_top(row_maxf<LPT>(xj)) : 0.0f;
+    s = mine ? sigmoid_score(xj, top) : 0.0f;
     if (r.renorm) f = over(r.scale, row_sum<LPT>(s));
   } else if (r.renorm) {
     const float m = row_maxf<LPT>(xj);

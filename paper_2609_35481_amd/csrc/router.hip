@@ -399,8 +399,9 @@ __global__ __launch_bounds__(kThreads, V <= 32 ? 4 : 2) void route_list_kernel(R
 #pragma unroll
   for (int j = 1; j < K; ++j) m = j < a.r.k ? fmaxf(m, s[j]) : m;
   if (a.r.sigmoid) {
+    const float top = a.r.renorm ? sigmoid_top(m) : 0.0f;
 #pragma unroll
-    for (int j = 0; j < K; ++j) s[j] = j < a.r.k ? sigmoid_score(s[j]) : 0.0f;
+    for (int j = 0; j < K; ++j) s[j] = j < a.r.k ? sigmoid_score(s[j], top) : 0.0f;
     if (a.r.renorm) f = over(a.r.scale, lane_sum(s));
   } else {
     if (!a.r.renorm) m = most;
@@ -456,12 +457,12 @@ template <int KP>
 __device__ inline float chosen_gradient(const RouterArgs &r, bool in, float xj, float g) {
   const float m = r.renorm ? row_maxf<KP>(xj) : 0.0f;
   if (r.sigmoid) {
-    float s = in ? sigmoid_score(xj) : 0.0f;
+    float s = in ? sigmoid_score(xj, r.renorm ? sigmoid_top(m) : 0.0f) : 0.0f;
     if (r.renorm) {
       s *= over(1.0f, row_sum<KP>(s));
       g -= row_sum<KP>(g * s);
     }
-    return s > 0.0f ? g * s * sigmoid_score(-xj) : 0.0f;
+    return s > 0.0f ? g * s * sigmoid_score(-xj, 0.0f) : 0.0f;
   }
   const float e = exp_from(xj, m == -INFINITY ? 0.0f : m);
   const float q = e * over(1.0f, row_sum<KP>(e));

@@ -102,3 +102,21 @@ def test_weights_to_32_bits(T, E, k, scoring, renorm):
     bound = (12 + (E - 1).bit_length()) * 2.0 ** -24
     off = (w.double() - want).abs()
     assert bool((off <= bound * want + 1e-37).all()), float(((off - 1e-37) / want).max() / 2.0 ** -24)
+
+
+@pytest.mark.parametrize("E,k", [(24, 4), (128, 8), (200, 12)])
+@pytest.mark.parametrize("level", [-80.0, -100.0, -300.0, -680.0])
+def test_renormalised_sigmoid_scores_far_below_zero(E, k, level):
+    """Scores that vanish in 32 bits still have ratios."""
+    for T in (3, 9000):
+        x = level + draw(T, E, 2.0)
+        print("far below", T, E, k, level, flush=True)
+        ids, w = moe.route(x, k, scoring="sigmoid", scale=2.5)
+        want = 2.5 * in_64_bits(x, ids, "sigmoid", True)
+        assert bool(((w.double() - want).abs() <= (12 + 8) * 2.0 ** -24 * want).all())
+        g = torch.randn((T, k), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)
+        got = moe.route_backward(x, ids, g, scoring="sigmoid", scale=2.5)
+        r, dw = want / 2.5, g.double()
+        ref = torch.zeros(x.shape, dtype=torch.float64, device=DEV).scatter(
+            1, ids.long(), 2.5 * r * (dw - (r * dw).sum(1, keepdim=True)))   # 1 - score is 1
+        assert bool(((got.double() - ref).abs() <= 2e-6 * 2.5 * float(g.abs().max())).all())
