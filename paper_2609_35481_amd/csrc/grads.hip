@@ -6,7 +6,8 @@
 // into chunks of kChunk elements that do not cross tensors, and workgroup b takes
 // pieces b, b + grid, ... of kPiece chunks.  The norm
 // kernel leaves one 64-bit partial a workgroup; the reader sums them in a fixed
-// order.  Squares are formed and summed in 64 bits: the square of any 32-bit
+// order: every workgroup of the clip for itself, or, where there are more than one
+// launch leaves, a kernel of its own once.  Squares are formed and summed in 64 bits: the square of any 32-bit
 // number is exact there and neither overflows nor vanishes.
 //
 // Bound: memory.  The norm of 1.37 G 16-bit elements runs at 6.8 TB/s (7.0 for
@@ -345,6 +346,9 @@ size_t partials_bytes(int32_t count) {
   return (((size_t)count + (size_t)(kMostElements / kMostEntry)) / Set<false>::kMost + 1) * kBlocks * sizeof(double);
 }
 
+// The partials and, behind them, the clip's norm.
+size_t workspace_bytes_of(int32_t count) { return (partials_bytes(count) + sizeof(float) + 255) & ~(size_t)255; }
+
 int check_workspace(const void *ws, size_t bytes, int32_t count) {
   if (!ws) return TOPOEP_EINVAL;
   size_t need = 0;
@@ -382,6 +386,15 @@ int enqueue_clip(const topoep_grad *grads, int count, Clip c, double *ws, hipStr
   if (!c.given) {
     const int rc = enqueue_partials<R, Stream>(grads, count, ws, st, &c.count);
     if (rc != TOPOEP_OK) return rc;
+    // Summed by every workgroup of every launch, the partials of many launches cost
+    // more than the tensors (12 000 tensors of 65 536 elements: 8.6 ms, 2.4 so)
+    if (c.count > kBlocks) {
+      float *norm = c.norm ? c.norm : reinterpret_cast<float *>(reinterpret_cast<char *>(ws) + partials_bytes(count));
+      hipLaunchKernelGGL((grad_finish_kernel<R>), dim3(1), dim3(kThreads), 0, st, ws, c.count, c.scale, norm);
+      if (hipGetLastError() != hipSuccess) return TOPOEP_EHIP;
+      c.given = norm;
+      c.norm = nullptr;
+    }
   }
   return each_set<true>(grads, count, [&](const Set<true> &s, int launch) {
     Clip own = c;
@@ -397,7 +410,7 @@ extern "C" {
 
 int topoep_grads_workspace_bytes(int32_t count, size_t *bytes_out) {
   if (count < 0 || !bytes_out) return TOPOEP_EINVAL;
-  *bytes_out = (partials_bytes(count) + 255) & ~(size_t)255;
+  *bytes_out = workspace_bytes_of(count);
   return TOPOEP_OK;
 }
 

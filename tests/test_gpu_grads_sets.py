@@ -1,0 +1,56 @@
+"""Gradient sets as training loops hand them over: thousands of separate
+tensors, tensors that share memory, tensors that autograd watches."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+from paper_2609_35481_amd import moe, topoep  # noqa: E402
+
+DEV = torch.device("cuda:0")
+
+
+def separate(count, n, dtype=torch.bfloat16, gap=8):
+    """`count` tensors of n elements, none next to another, and the buffer they lie in."""
+    g = torch.Generator(device=DEV).manual_seed(count)
+    flat = torch.randn((count, n + gap), generator=g, device=DEV, dtype=dtype)
+    flat[:, n:] = 0
+    return [row[:n] for row in flat], flat
+
+
+@pytest.mark.parametrize("ord", [2, "inf"])
+@pytest.mark.parametrize("count,n", [(300, 20000), (2000, 30000), (4001, 50)])
+def test_thousands_of_separate_tensors(count, n, ord):
+    grads, flat = separate(count, n)
+    print("separate", count, n, ord, flush=True)
+    want = flat.double().abs().max() if ord == "inf" else flat.double().square().sum().sqrt()
+    before = flat.clone()
+    norm = moe.grad_norm(grads, ord=ord)
+    clipped = moe.clip_grads(grads, 1.0, scale=0.5, ord=ord)
+    torch.cuda.synchronize()
+    assert abs(float(norm) - float(want)) <= 2.0 ** -23 * float(want) and float(clipped) == 0.5 * float(norm)
+    f = 0.5 * min(1.0, 1.0 / (0.5 * float(want) + 1e-6))
+    assert bool(((flat.double() - before.double() * f).abs() <= (2.0 ** -8 + 2.0 ** -21) * before.double().abs() * f + 1e-38).all())
+
+
+def test_many_launches_partials_are_summed_once():
+    """The clip of 12 000 separate tensors against that of one buffer of their size:
+    a hundred launches more, some of the tensors' time again and not a multiple of it."""
+    grads, flat = separate(12000, 65536)
+
+    def ms(call):
+        call()
+        torch.cuda.synchronize()
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        call()
+        b.record()
+        torch.cuda.synchronize()
+        return a.elapsed_time(b)
+
+    one, many = ms(lambda: moe.clip_grads([flat], 1.0, scale=0.5)), ms(lambda: moe.clip_grads(grads, 1.0, scale=0.5))
+    print("clip of one buffer %.2f ms, of 12000 tensors %.2f ms" % (one, many), flush=True)
+    assert many < 8 * one + 1.0
