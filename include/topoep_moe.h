@@ -151,8 +151,9 @@ int topoep_moe_few(const topoep_moe *m, const topoep_router *r, const void *x, i
 typedef struct topoep_grad {
   const void *grad;  /* device, n elements of dtype, any alignment of their size     */
   void *out;         /* device, n elements of out_dtype: where the clipped gradient  */
-                     /* goes.  May be grad itself (dtype == out_dtype), else the two */
-                     /* do not overlap.  Not read by topoep_grad_norm                */
+                     /* goes.  May be grad itself (dtype == out_dtype); otherwise no */
+                     /* out overlaps another out or any grad of the set.  Not read   */
+                     /* by topoep_grad_norm                                          */
   int64_t n;         /* >= 0; a set has at most 2^40 elements                        */
   int32_t dtype;
   int32_t out_dtype;
@@ -181,7 +182,9 @@ int topoep_grad_norm(const topoep_grad *grads, int32_t count, float scale, int32
  * also written to *norm (may be NULL).  Where the norm is not finite nothing
  * is written but *norm, so that the caller can drop the step.  Where the
  * factor is 1, tensors clipped in place are left alone.  max_norm > 0, finite or
- * infinite.  Return codes as topoep_grad_norm.
+ * infinite.  Return codes as topoep_grad_norm; TOPOEP_EINVAL also for outputs
+ * that overlap (a tensor clipped in place that is in the set twice, say),
+ * TOPOEP_ELIMIT where the host has no memory to look.
  */
 int topoep_clip_grads(const topoep_grad *grads, int32_t count, float scale, int32_t ord, float max_norm,
                       const float *given_norm, float *norm, void *workspace, size_t workspace_bytes, void *stream);

@@ -244,7 +244,8 @@ def grad_norm(grads, scale=1.0, ord=2, stream=None):
 def clip_grads(grads, max_norm, scale=1.0, ord=2, outs=None, norm=None, stream=None):
     """Enqueue topoep_clip_grads: every gradient times scale * min(1, max_norm /
     (norm + 1e-6)), in place or into `outs` (same shapes and strides, any
-    of the three types); returns the norm.  norm: a given one (float32 scalar tensor,
+    of the three types), none of which overlaps another tensor of the set but
+    its own gradient; returns the norm.  norm: a given one (float32 scalar tensor,
     already scaled), say of a whole group of ranks; None takes this set's.  A norm that
     is not finite leaves every tensor as it is."""
     if stream is not None:

@@ -54,3 +54,18 @@ def test_many_launches_partials_are_summed_once():
     one, many = ms(lambda: moe.clip_grads([flat], 1.0, scale=0.5)), ms(lambda: moe.clip_grads(grads, 1.0, scale=0.5))
     print("clip of one buffer %.2f ms, of 12000 tensors %.2f ms" % (one, many), flush=True)
     assert many < 8 * one + 1.0
+
+
+def test_a_tensor_twice_in_place_is_refused():
+    g = torch.full((1000,), 2.0, device=DEV)
+    h = torch.ones(10, device=DEV)
+    for grads in ([g, h, g], [g, g[:10]], [g[:600], g[500:]]):
+        with pytest.raises(topoep.TopoepError):
+            moe.clip_grads(grads, 1.0)
+    torch.cuda.synchronize()
+    assert bool((g == 2.0).all())
+    # read twice, written once each
+    outs = [torch.empty_like(g), torch.empty_like(g)]
+    norm = moe.clip_grads([g, g], 1.0, outs=outs)
+    torch.cuda.synchronize()
+    assert abs(float(norm) - 8000.0 ** 0.5) <= 1e-4 and torch.equal(outs[0], outs[1])
