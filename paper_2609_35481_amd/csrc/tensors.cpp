@@ -5,6 +5,8 @@
 //   pack(grads, outs) -> (table, device)
 //     table: bytes, a topoep_grad for each tensor (outs None: the gradients
 //     themselves); device: the index of the GPU that all of them are on.
+//   written(tensors): raises their version counters, so that autograd refuses a
+//     backward pass that saved one of them before.
 //   route(entry, router, logits, bias, stream) -> (code, ids, weights)
 //   route_backward(entry, router, logits, ids, grad_weights, stream) -> (code, grad_logits)
 //   moe_few(entry, router, x, gate, up, down, bias, expert_slot, workspace, stream) -> (code, out, ids, weights)
@@ -95,6 +97,17 @@ PyObject *pack(PyObject *, PyObject *args) {
   Py_DECREF(fg);
   Py_XDECREF(fo);
   return result;
+}
+
+PyObject *written(PyObject *, PyObject *tensors) {
+  PyObject *fast = PySequence_Fast(tensors, "a list of tensors");
+  if (!fast) return nullptr;
+  for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(fast); ++i) {
+    const at::Tensor &t = THPVariable_Unpack(PySequence_Fast_GET_ITEM(fast, i));   // pack() took it
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  }
+  Py_DECREF(fast);
+  Py_RETURN_NONE;
 }
 
 // Row stride of a matrix of dense rows that do not overlap; -1 (and an error)
@@ -238,7 +251,8 @@ PyMethodDef methods[] = {{"moe_few", moe_few, METH_VARARGS,
                          {"route", route, METH_VARARGS, "route(entry, router, logits, bias, stream) -> (code, ids, weights)"},
                          {"route_backward", route_backward, METH_VARARGS,
                           "route_backward(entry, router, logits, ids, grad_weights, stream) -> (code, grad_logits)"},
-                         {"pack", pack, METH_VARARGS, "pack(grads, outs) -> (bytes, device)"}, {nullptr, nullptr, 0, nullptr}};
+                         {"pack", pack, METH_VARARGS, "pack(grads, outs) -> (bytes, device)"},
+                         {"written", written, METH_O, "written(tensors)"}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -259,4 +259,5 @@ def clip_grads(grads, max_norm, scale=1.0, ord=2, outs=None, norm=None, stream=N
                                   total.data_ptr() if norm is not None else None,
                                   total.data_ptr() if norm is None else None, ws.data_ptr(), ws.numel(), queue),
            "topoep_clip_grads")
+    _tensors.written(grads if outs is None else outs)
     return total

@@ -69,3 +69,25 @@ def test_a_tensor_twice_in_place_is_refused():
     norm = moe.clip_grads([g, g], 1.0, outs=outs)
     torch.cuda.synchronize()
     assert abs(float(norm) - 8000.0 ** 0.5) <= 1e-4 and torch.equal(outs[0], outs[1])
+
+
+def test_autograd_sees_what_the_clip_writes():
+    """A tensor that a backward pass still needs: as torch's own in-place
+    operations, the clip makes that pass fail instead of using the new values."""
+    w = torch.ones(100, device=DEV, requires_grad=True)
+    g, out = torch.full((100,), 5.0, device=DEV), torch.empty(100, device=DEV)
+    loss = (w * g).sum() + (w * out).sum()
+    moe.grad_norm([g])
+    versions = g._version, out._version
+    moe.clip_grads([g], 1.0, outs=[out])
+    assert (g._version, out._version) == (versions[0], versions[1] + 1)
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+    loss = (w * g).sum()
+    moe.clip_grads([g[:50], g[50:]], 1.0)   # views share their base's
+    assert g._version == versions[0] + 2
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+    with torch.inference_mode():
+        t = torch.full((10,), 5.0, device=DEV)
+    assert abs(float(moe.clip_grads([t], 1.0)) - 250.0 ** 0.5) < 1e-5
