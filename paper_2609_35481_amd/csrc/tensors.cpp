@@ -13,7 +13,8 @@
 //     entry: the address of topoep_route (topoep_route_backward, topoep_moe_few);
 //     router: of a topoep_router, whose dtype is the logits'; code: what it returned.
 //
-// TypeError and ValueError for what the library does not take.
+// TypeError and ValueError for what the library does not take, RuntimeError for
+// tensors of forward-mode differentiation, whose tangents would be lost.
 #define PY_SSIZE_T_CLEAN
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -38,6 +39,8 @@ PyObject *refuse(PyObject *kind, const char *what, Py_ssize_t i) {
   return nullptr;
 }
 
+bool has_tangent(const at::Tensor &t) { return t._fw_grad(0).defined(); }
+
 PyObject *fill(PyObject *grads, PyObject *outs) {
   const Py_ssize_t n = PySequence_Fast_GET_SIZE(grads);
   if (outs && PySequence_Fast_GET_SIZE(outs) != n) {
@@ -56,6 +59,7 @@ PyObject *fill(PyObject *grads, PyObject *outs) {
     PyObject *pg = PySequence_Fast_GET_ITEM(grads, i), *po = outs ? PySequence_Fast_GET_ITEM(outs, i) : pg;
     if (!THPVariable_Check(pg) || !THPVariable_Check(po)) return drop(PyExc_TypeError, "not a tensor", i);
     const at::Tensor &g = THPVariable_Unpack(pg), &o = THPVariable_Unpack(po);
+    if (has_tangent(g) || has_tangent(o)) return drop(PyExc_RuntimeError, "carries a tangent, which is not passed on", i);
     if (!g.is_cuda() || !o.is_cuda()) return drop(PyExc_ValueError, "not on a GPU", i);
     if (g.layout() != at::kStrided || o.layout() != at::kStrided) return drop(PyExc_TypeError, "not a strided tensor", i);
     if (device < 0) device = g.get_device();
@@ -137,8 +141,13 @@ bool dense(const at::Tensor &t, const char *name, at::ScalarType type, const at:
 }
 
 const at::Tensor *tensor_of(PyObject *o, const char *name) {
-  if (THPVariable_Check(o)) return &THPVariable_Unpack(o);
-  PyErr_Format(PyExc_TypeError, "%s is not a tensor", name);
+  if (!THPVariable_Check(o)) {
+    PyErr_Format(PyExc_TypeError, "%s is not a tensor", name);
+    return nullptr;
+  }
+  const at::Tensor &t = THPVariable_Unpack(o);
+  if (!has_tangent(t)) return &t;
+  PyErr_Format(PyExc_RuntimeError, "%s carries a tangent, which is not passed on", name);
   return nullptr;
 }
 

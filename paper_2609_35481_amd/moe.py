@@ -144,6 +144,37 @@ class _Route(torch.autograd.Function):
         return _backward(ctx.router, logits, ids, grad_weights.contiguous()), None, None
 
 
+class _RouteBackward(torch.autograd.Function):
+    """A direct call's result under autograd: a gradient through it is an
+    error, not nothing."""
+    @staticmethod
+    def forward(ctx, logits, ids, grad_weights, r):
+        return _backward(r, logits, ids, grad_weights)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("route_backward has no gradient of its own")
+
+
+class _Few(torch.autograd.Function):
+    """The layer under autograd: a backward pass through it is an error, not
+    one that leaves its weights out."""
+    @staticmethod
+    def forward(ctx, x, gate, up, down, bias, k, rules, expert_slot, workspace):
+        out, ids, weights = _few(x, gate, up, down, k, rules, bias, expert_slot, workspace)
+        ctx.mark_non_differentiable(ids)
+        return out, ids, weights
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("moe_few is forward only: its inputs get no gradient")
+
+
+def _watched(*tensors):
+    """Whether autograd would record an operation on them."""
+    return torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors)
+
+
 def route(logits, k, scoring="softmax", renorm=True, scale=1.0, bias=None, groups=1, top_groups=1, stream=None):
     """Enqueue topoep_route: (ids int32 [T, k], weights float32 [T, k]) of the
     logits [T, E].  The ids are what a planner takes; the weights carry a
@@ -163,7 +194,9 @@ def route_backward(logits, ids, grad_weights, scoring="softmax", renorm=True, sc
     r = router(logits.shape[1] if logits.dim() == 2 else 0, ids.shape[1] if ids.dim() == 2 else 0, logits.dtype,
                scoring, renorm, scale)
     if stream is not None:
-        return _on_stream(stream, _backward, r, logits, ids, grad_weights)
+        return _on_stream(stream, route_backward, logits, ids, grad_weights, scoring, renorm, scale)
+    if _watched(logits, grad_weights):
+        return _RouteBackward.apply(logits, ids, grad_weights, r)
     return _backward(r, logits, ids, grad_weights)
 
 
@@ -182,12 +215,17 @@ def moe_few(x, gate, up, down, k, scoring="softmax", renorm=True, scale=1.0, bia
     [T, k]) of the tokens x [T, H], at most 128, through a layer with the
     router gate [E, H] and the experts up [L, 2I, H] (gate rows, then up rows)
     and down [L, H, I], bfloat16 or float16.  expert_slot [E] says where an
-    expert lies among the L here (-1: elsewhere; it adds nothing).  Forward only.
+    expert lies among the L here (-1: elsewhere; it adds nothing).  Forward
+    only: a backward pass through the outputs is an error.
 
     workspace: a tensor of moe_workspace_bytes or more for calls on one stream to
     share; None makes one for the call."""
-    args = (x, gate, up, down, k, (scoring, renorm, scale, groups, top_groups), bias, expert_slot, workspace)
-    return _few(*args) if stream is None else _on_stream(stream, _few, *args)
+    rules = (scoring, renorm, scale, groups, top_groups)
+    if stream is not None:
+        return _on_stream(stream, moe_few, x, gate, up, down, k, *rules[:3], bias, *rules[3:], expert_slot, workspace)
+    if _watched(x, gate, up, down, bias):
+        return _Few.apply(x, gate, up, down, bias, k, rules, expert_slot, workspace)
+    return _few(x, gate, up, down, k, rules, bias, expert_slot, workspace)
 
 
 def _few(x, gate, up, down, k, rules, bias, expert_slot, workspace):

@@ -1,0 +1,78 @@
+"""Derivatives that the operators do not carry are errors, not lost: the layer
+for a few tokens has no backward pass, the router's gradient none of its own,
+and no operator passes tangents of forward-mode differentiation on."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import torch.autograd.forward_ad as forward_ad  # noqa: E402
+
+from paper_2609_35481_amd import moe  # noqa: E402
+
+DEV = torch.device("cuda:0")
+
+
+def layer():
+    g = torch.Generator(device=DEV).manual_seed(1)
+    return [torch.randn(s, generator=g, device=DEV).mul_(0.1).bfloat16() for s in ((3, 64), (8, 64), (8, 64, 64), (8, 64, 32))]
+
+
+@pytest.mark.parametrize("which", [0, 1, 2, 3, 4])
+def test_a_backward_pass_through_the_layer_is_an_error(which):
+    args, bias = layer(), torch.zeros(8, device=DEV)
+    want = moe.moe_few(*args, 2, bias=bias)
+    assert not any(t.requires_grad for t in want)
+    if which == 4:
+        bias.requires_grad_()
+    else:
+        args[which].requires_grad_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (None, side):
+        out, ids, weights = moe.moe_few(*args, 2, bias=bias, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(ids, want[1]) and torch.equal(weights, want[2])
+        for t in (out, weights):
+            assert t.requires_grad
+            with pytest.raises(RuntimeError, match="forward only"):
+                t.float().sum().backward()
+    with torch.no_grad():
+        out, _, weights = moe.moe_few(*args, 2, bias=bias)
+        assert not out.requires_grad and not weights.requires_grad
+
+
+def test_the_routers_gradient_has_none_of_its_own():
+    x = torch.randn(5, 16, device=DEV, requires_grad=True)
+    ids, w = moe.route(x, 4)
+    dw = torch.ones(5, 4, device=DEV, requires_grad=True)
+    for logits, grad in ((x, dw.detach()), (x.detach(), dw)):
+        d = moe.route_backward(logits, ids, grad)
+        assert torch.equal(d, moe.route_backward(x.detach(), ids, dw.detach()))
+        with pytest.raises(RuntimeError, match="no gradient"):
+            d.sum().backward()
+    (d,) = torch.autograd.grad(w.square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        d.sum().backward()
+
+
+def test_tangents_are_not_dropped():
+    x = torch.randn(5, 16, device=DEV)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, torch.ones_like(x))
+        with pytest.raises(RuntimeError, match="tangent"):
+            moe.route(dual, 4)
+        with pytest.raises(RuntimeError):
+            moe.route(forward_ad.make_dual(x.clone().requires_grad_(), torch.ones_like(x)), 4)
+        ids, w = moe.route(x, 4)
+        with pytest.raises(RuntimeError, match="tangent"):
+            moe.route_backward(x, ids, forward_ad.make_dual(w, torch.ones_like(w)))
+        args = layer()
+        with pytest.raises(RuntimeError, match="tangent"):
+            moe.moe_few(forward_ad.make_dual(args[0], torch.ones_like(args[0])), *args[1:], 2)
+        with pytest.raises(RuntimeError, match="tangent"):
+            moe.grad_norm([dual])
+        assert moe.route(x, 4)[0].shape == (5, 4)
