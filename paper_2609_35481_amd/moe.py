@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import numbers
 
 import torch
 
@@ -72,15 +73,30 @@ EXPORTS = ("topoep_route", "topoep_route_backward", "topoep_moe_workspace_bytes"
            "topoep_grads_workspace_bytes", "topoep_grad_norm", "topoep_clip_grads")
 
 
+def _int32(name, value):
+    """A size as the library's 32 bits take it, which ctypes would cut it to."""
+    if not isinstance(value, numbers.Integral):
+        raise TypeError("%s must be an integer, not %s" % (name, type(value).__name__))
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError("%s is %d, beyond 32 bits" % (name, value))
+    return int(value)
+
+
 @functools.lru_cache(maxsize=256)
 def router(E, k, dtype=torch.float32, scoring="softmax", renorm=True, scale=1.0, groups=1, top_groups=1) -> Router:
-    """The sizes and rules of a router (plain values, so one struct serves
-    every call that names the same)."""
+    """The sizes and rules of a router.  Plain values alone, so that one struct
+    serves every call that names the same: a tensor, whose value may change, is
+    refused."""
+    if not isinstance(scale, numbers.Real):
+        raise TypeError("scale must be a number, not %s" % type(scale).__name__)
+    if isinstance(renorm, torch.Tensor):
+        raise TypeError("renorm must be true or false, not a tensor")
     if dtype not in _TYPES:
         raise TypeError("logits must be float32, bfloat16 or float16, not %s" % dtype)
     if scoring not in _SCORES:
         raise ValueError("scoring is 'softmax' or 'sigmoid', not %r" % (scoring,))
-    return Router(E, k, groups, top_groups, _SCORES[scoring], int(bool(renorm)), _TYPES[dtype], scale)
+    return Router(_int32("E", E), _int32("k", k), _int32("groups", groups), _int32("top_groups", top_groups),
+                  _SCORES[scoring], int(bool(renorm)), _TYPES[dtype], float(scale))
 
 
 def _check(rc, name):
@@ -204,8 +220,8 @@ def moe_workspace_bytes(H, I, E, L, k, T, dtype=torch.bfloat16) -> int:
     """Bytes of workspace moe_few needs for T tokens or fewer (and up to 255
     more where it does not start at a multiple of 256)."""
     out = _size(0)
-    m = Moe(H, I, L, _TYPES.get(dtype, -1))
-    _check(_lib.topoep_moe_workspace_bytes(m, router(E, k), T, out), "topoep_moe_workspace_bytes")
+    m = Moe(_int32("H", H), _int32("I", I), _int32("L", L), _TYPES.get(dtype, -1))
+    _check(_lib.topoep_moe_workspace_bytes(m, router(E, k), _int32("T", T), out), "topoep_moe_workspace_bytes")
     return out.value
 
 
