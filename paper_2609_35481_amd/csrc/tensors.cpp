@@ -14,9 +14,13 @@
 //     router: of a topoep_router, whose dtype is the logits'; code: what it returned.
 //
 // TypeError and ValueError for what the library does not take, RuntimeError for
-// tensors of forward-mode differentiation, whose tangents would be lost.
+// tensors of forward-mode differentiation, whose tangents would be lost.  C++
+// exceptions become what torch raises for them (memory that does not suffice:
+// torch.OutOfMemoryError).
 #define PY_SSIZE_T_CLEAN
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/utils/object_ptr.h>
 
 #include <ATen/ops/empty.h>
 #include <Python.h>
@@ -47,60 +51,54 @@ PyObject *fill(PyObject *grads, PyObject *outs) {
     PyErr_Format(PyExc_ValueError, "%zd outs for %zd grads", PySequence_Fast_GET_SIZE(outs), n);
     return nullptr;
   }
-  PyObject *table = PyBytes_FromStringAndSize(nullptr, n * (Py_ssize_t)sizeof(topoep_grad));
+  THPObjectPtr table(PyBytes_FromStringAndSize(nullptr, n * (Py_ssize_t)sizeof(topoep_grad)));
   if (!table) return nullptr;
-  topoep_grad *to = reinterpret_cast<topoep_grad *>(PyBytes_AS_STRING(table));
+  topoep_grad *to = reinterpret_cast<topoep_grad *>(PyBytes_AS_STRING(table.get()));
   int device = -1;
-  const auto drop = [&](PyObject *kind, const char *what, Py_ssize_t i) {
-    Py_DECREF(table);
-    return refuse(kind, what, i);
-  };
   for (Py_ssize_t i = 0; i < n; ++i) {
     PyObject *pg = PySequence_Fast_GET_ITEM(grads, i), *po = outs ? PySequence_Fast_GET_ITEM(outs, i) : pg;
-    if (!THPVariable_Check(pg) || !THPVariable_Check(po)) return drop(PyExc_TypeError, "not a tensor", i);
+    if (!THPVariable_Check(pg) || !THPVariable_Check(po)) return refuse(PyExc_TypeError, "not a tensor", i);
     const at::Tensor &g = THPVariable_Unpack(pg), &o = THPVariable_Unpack(po);
-    if (has_tangent(g) || has_tangent(o)) return drop(PyExc_RuntimeError, "carries a tangent, which is not passed on", i);
-    if (!g.is_cuda() || !o.is_cuda()) return drop(PyExc_ValueError, "not on a GPU", i);
-    if (g.layout() != at::kStrided || o.layout() != at::kStrided) return drop(PyExc_TypeError, "not a strided tensor", i);
+    if (has_tangent(g) || has_tangent(o)) return refuse(PyExc_RuntimeError, "carries a tangent, which is not passed on", i);
+    if (!g.is_cuda() || !o.is_cuda()) return refuse(PyExc_ValueError, "not on a GPU", i);
+    if (g.layout() != at::kStrided || o.layout() != at::kStrided) return refuse(PyExc_TypeError, "not a strided tensor", i);
     if (device < 0) device = g.get_device();
-    if (g.get_device() != device || o.get_device() != device) return drop(PyExc_ValueError, "on another GPU than the first", i);
+    if (g.get_device() != device || o.get_device() != device) return refuse(PyExc_ValueError, "on another GPU than the first", i);
     const int from = dtype_of(g), into = dtype_of(o);
-    if (from < 0 || into < 0) return drop(PyExc_TypeError, "not float32, bfloat16 or float16", i);
-    if (po != pg && !g.sizes().equals(o.sizes())) return drop(PyExc_ValueError, "its output has another shape", i);
+    if (from < 0 || into < 0) return refuse(PyExc_TypeError, "not float32, bfloat16 or float16", i);
+    if (po != pg && !g.sizes().equals(o.sizes())) return refuse(PyExc_ValueError, "its output has another shape", i);
     if (!(g.is_contiguous() && o.is_contiguous()) &&
         !(g.is_non_overlapping_and_dense() && g.strides().equals(o.strides())))
-      return drop(PyExc_ValueError, "not dense, or its output has other strides", i);
+      return refuse(PyExc_ValueError, "not dense, or its output has other strides", i);
     to[i].grad = g.data_ptr();
     to[i].out = o.data_ptr();
     to[i].n = g.numel();
     to[i].dtype = from;
     to[i].out_dtype = into;
   }
-  return Py_BuildValue("(Ni)", table, device);
+  return Py_BuildValue("(Ni)", table.release(), device);
+}
+
+template <class F>
+PyObject *guarded(const F &f) {
+  try {
+    return f();
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());
+    return nullptr;
+  }
 }
 
 PyObject *pack(PyObject *, PyObject *args) {
   PyObject *grads = nullptr, *outs = nullptr;
   if (!PyArg_ParseTuple(args, "OO", &grads, &outs)) return nullptr;
-  PyObject *fg = PySequence_Fast(grads, "grads is a list of tensors");
+  THPObjectPtr fg(PySequence_Fast(grads, "grads is a list of tensors")), fo;
   if (!fg) return nullptr;
-  PyObject *fo = nullptr;
   if (outs != Py_None) {
     fo = PySequence_Fast(outs, "outs is a list of tensors");
-    if (!fo) {
-      Py_DECREF(fg);
-      return nullptr;
-    }
+    if (!fo) return nullptr;
   }
-  PyObject *result = nullptr;
-  try {
-    result = fill(fg, fo);
-  } catch (const std::exception &e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-  }
-  Py_DECREF(fg);
-  Py_XDECREF(fo);
-  return result;
+  return guarded([&] { return fill(fg.get(), fo.get()); });
 }
 
 PyObject *written(PyObject *, PyObject *tensors) {
@@ -149,16 +147,6 @@ const at::Tensor *tensor_of(PyObject *o, const char *name) {
   if (!has_tangent(t)) return &t;
   PyErr_Format(PyExc_RuntimeError, "%s carries a tangent, which is not passed on", name);
   return nullptr;
-}
-
-template <class F>
-PyObject *guarded(const F &f) {
-  try {
-    return f();
-  } catch (const std::exception &e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-    return nullptr;
-  }
 }
 
 PyObject *route(PyObject *, PyObject *args) {

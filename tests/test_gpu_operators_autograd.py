@@ -76,3 +76,18 @@ def test_tangents_are_not_dropped():
         with pytest.raises(RuntimeError, match="tangent"):
             moe.grad_norm([dual])
         assert moe.route(x, 4)[0].shape == (5, 4)
+
+
+def test_memory_that_does_not_suffice_is_torchs_error():
+    """Callers that shrink a batch on torch.OutOfMemoryError see it from these calls too."""
+    x = torch.zeros((1 << 25, 1), device=DEV)   # outputs of 128 MB each
+    total = torch.cuda.get_device_properties(DEV).total_memory
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    try:
+        torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + (16 << 20)) / total)
+        with pytest.raises(torch.OutOfMemoryError):
+            moe.route(x, 1)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert moe.route(x, 1)[0].shape == (1 << 25, 1)
