@@ -829,6 +829,8 @@ int enqueue_down_rows(const Layer &a, hipStream_t st) {
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
+// Four outputs a workgroup where eight would leave too few of them (one token, I = 512, H = 1024:
+// layer 20.5 against 20.9 us; two tokens, I = 1024: 37.9 and 41.6; H = 1536: 22.1 and 21.2, 48.4 and 46.9).
 template <class T>
 int enqueue_down(const Layer &a, hipStream_t st) {
   return a.H <= 1024 ? enqueue_down_rows<T, 1>(a, st) : enqueue_down_rows<T, 2>(a, st);
@@ -845,7 +847,11 @@ int enqueue(const Layer &a, hipStream_t st) {
   else hipLaunchKernelGGL((gate_kernel<T, 8>), gg, gb, 0, st, a);
   if (!launched()) return TOPOEP_EHIP;
   const int experts = imin(imin(a.T * a.r.k, E), a.L), tiles = (a.I + 7) / 8;
-  if (a.T == 1 && E <= 256 && (int64_t)experts * tiles < 2048 && (int64_t)experts * a.H * a.I <= 1 << 25 && a.r.k <= 16) {
+  // One token, three kernels or five (H = 2048, I = 768, 8 of 128 experts: 29.5 against 33.7 us;
+  // H = 4096, I = 14336, 1 of 8: 69 and 77): where a workgroup has a tile (the rule of
+  // enqueue_experts), and for up to 16 choices, behind which neither is always the faster
+  // (H = 2048, I = 256, 24 choices: 34.7 and 37.3; H = 1024, I = 512, 32: 45.1 and 42.8).
+  if (a.T == 1 && E <= 256 && (int64_t)experts * tiles < 2048 && a.r.k <= 16) {
     const dim3 grid((unsigned)experts * tiles), block(64 * kExpertWaves);
     if (E <= 64) hipLaunchKernelGGL((one_up_kernel<T, 1>), grid, block, 0, st, a, tiles);
     else if (E <= 128) hipLaunchKernelGGL((one_up_kernel<T, 2>), grid, block, 0, st, a, tiles);
@@ -862,6 +868,9 @@ int enqueue(const Layer &a, hipStream_t st) {
   if (!launched()) return TOPOEP_EHIP;
   int rc = enqueue_experts<T, true>(a, st);
   if (rc != TOPOEP_OK) return rc;
+  // The second product and the sum in one, or two kernels, few pairs of small experts (H = 512,
+  // I = 256: 16 pairs 24.4 against 25.2 us, 32 pairs 27.7 and 27.0; two tokens, H = 4096, I = 2048,
+  // 4 experts: 49.6 and 52.0; from 2^26 weights on the one is from 2 % faster to 2 % slower).
   if (a.T * a.r.k <= 16 && (int64_t)experts * a.H * a.I <= 1 << 25) return enqueue_down<T>(a, st);
   rc = enqueue_experts<T, false>(a, st);
   if (rc != TOPOEP_OK) return rc;
