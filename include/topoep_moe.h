@@ -61,19 +61,21 @@ typedef struct topoep_router {
  *            (ld >= E, any alignment of the element's size).  NaN and -inf
  *            are masked: chosen last, score 0.  +inf counts as the largest
  *            finite number.
- *   bias     device float [E] or NULL: added to the logits where experts are
- *            chosen, not in their weights.
+ *   bias     device float [E] or NULL: added to the LOGITS where experts are
+ *            chosen, not in their weights.  A bias that was trained to be added
+ *            to sigmoid scores is another rule and chooses other experts.
  *   ids      device int32 out [T, k]: the experts of the k largest keys,
  *            key = logit + bias rounded to 32 bits (a NaN key is -inf),
  *            descending, equal keys by the lower id.  With groups, only the
  *            experts of the g groups of the largest maximum key (equal ones
- *            by the lower group).  Always k distinct valid ids, as
+ *            by the lower group; not of the largest sum of two keys).  Always k distinct valid ids, as
  *            topoep_plan takes them.
  *   weights  device float out [T, k]: c times the score.  Softmax scores are
  *            over all E logits, or with renorm over the chosen ones; sigmoid
  *            scores with renorm are divided by the chosen scores' sum (where the
  *            largest is below e^-709, which ends 64 bits, it counts as zero).
  *            Where a sum is zero (every logit masked) the weights are zero.
+ *            A row's ids and weights do not depend on the rows beside it.
  *
  * T = 0 enqueues nothing.  TOPOEP_EINVAL: null pointers (bias excepted),
  * sizes outside the ranges of topoep_router, T < 0 or T * k > INT32_MAX, ld <

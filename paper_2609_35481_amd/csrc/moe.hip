@@ -21,9 +21,10 @@
 // in LDS.
 //
 // Bound: memory, and for one token the chain of three kernels.  128 experts of
-// H = 2048, I = 768, top-8: one token 24 us (76 MB, 11 at the 7.0 TB/s of reads
-// alone), of which gate 3.3, up 14.7, down 8.1; 64 tokens 209 us (1.19 GB, 170),
-// up 133 (6.0 TB/s), down 72 (5.6), gate, route and combine 15, starts 5.
+// H = 2048, I = 768, top-8: one token 23.3 us (76 MB, 11 at the 7.0 TB/s of reads
+// alone), 64 tokens 209 us (1.19 GB, 170).  In a traced run, whose passes take
+// 32 and 217 us: one token gate 3.1, up 13.4, down 7.9; 64 tokens up 125 (6.4
+// TB/s), down 74 (5.4), gate, route and combine 16.
 #include "router.h"
 
 namespace {
@@ -574,10 +575,9 @@ __global__ __launch_bounds__(64 * kExpertWaves, (kStage * (Up ? 1 : 2) > 128 ? 1
   }
 }
 
-// One token: every wave routes it for itself, which takes the routing kernel's
-// 3.6 us and a launch off the path for 2 (one token, 128 experts of H = 2048, I =
-// 768: 26.7 us for the layer without); workgroup 0 leaves what the next kernel
-// reads.  Workgroup b takes tile b % tiles of the token's choices b / tiles, b /
+// One token: every wave routes it for itself, which takes the routing kernel and
+// a launch off the path (one token, 128 experts of H = 2048, I = 768, from a graph:
+// 29.5 us, 33.7 with five kernels); workgroup 0 leaves what the next kernel reads.  Workgroup b takes tile b % tiles of the token's choices b / tiles, b /
 // tiles + gridDim / tiles, ... here: more than the places where some share one.
 template <class T, int V>
 __global__ __launch_bounds__(64 * kExpertWaves, 4) void one_up_kernel(Layer a, int tiles) {
@@ -778,9 +778,9 @@ int enqueue_experts(const Layer &a, int experts, hipStream_t st) {
   const int rows = Up ? 8 : 16, tiles = ((Up ? a.I : a.H) + rows - 1) / rows;
   const dim3 block(64 * kExpertWaves);
   // A wave to a tile where there are tiles for all of the chip's 4096 places, or
-  // for half of them and rows are short (62 against 66 us for 32 experts, H = 2048,
-  // I = 768); else the workgroup to a tile (two experts, H = 4096, I = 14336: 130
-  // against 169 us)
+  // for half of them and rows are short (64 against 67 us for 32 experts, H = 2048,
+  // I = 768); else the workgroup to a tile (two experts, H = 4096, I = 14336: 127
+  // against 164 us)
   const int64_t all = (int64_t)experts * tiles;
   if (all < 2048 || (all < 4096 && (Up ? a.H : a.I) > 2048)) {
     hipLaunchKernelGGL((expert_kernel<T, Up, kExpertWaves, Kind>), dim3((unsigned)experts * tiles), block, 0, st, a, tiles);

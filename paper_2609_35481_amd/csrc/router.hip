@@ -8,10 +8,12 @@
 //   route_backward_chosen_kernel, route_backward_kernel  the gradient where the
 //                      chosen logits alone count, and where all do
 //
-// Bound: the forward by its comparisons (820 vector instructions for 16 rows of
-// 128; 200003 x 128: vector units busy 17.0 of 22.5 us, 5.1 TB/s), few tokens by the
-// chain of one row (3.0 us a launch); the gradient by memory: 200003 x 256 bf16 31
-// us for 102 MB written and 105 read, the lines that hold a chosen logit.
+// Bound: the forward by its comparisons (846 vector instructions for 16 rows of
+// 128; 200003 x 128: vector units busy 17.4 of 23.3 us, 4.9 TB/s; 200003 x 128 of 16 bits
+// 23.1; 16384 x 512 with groups and a bias 1326 instructions, 9.1 of 13 us; beyond eight
+// choices a maximum each: 200003 x 256, top-16, 143 us), few tokens by the chain of
+// one row (3.0 us a launch); the gradient by memory: 200003 x 256 bf16 31 us for
+// 102 MB written and 105 read, the lines that hold a chosen logit.
 #include "router.h"
 
 namespace {
@@ -659,8 +661,8 @@ template <class T>
 int enqueue_route(const Route &a, hipStream_t st) {
   const RouterArgs &r = a.r;
   // Few tokens are a chain of dependent steps, shorter with a wave a token (one
-  // token, 128 experts: 3.0 us a launch, lists 3.9; 512 tokens 3.3 and 4.3; 4096 tokens
-  // 4.4 both); up to 64 experts without groups, or beyond 256, the lists' is no longer.
+  // token, 128 experts: 3.0 us a launch, lists 3.8; 512 tokens 3.2 and 4.2; 4096 tokens
+  // 4.3 both); up to 64 experts without groups, or beyond 256, the lists' is no longer.
   if (a.T <= 1024 && r.E <= 256 && (r.groups > 1 || r.E > 64)) return launch_rows<T, Forward>(r.E, r.k, true, a, a.T, st);
   if (r.k <= 8 && r.groups == 1) return r.k <= 4 ? enqueue_lists<T, 4, 0>(a, st) : enqueue_lists<T, 8, 0>(a, st);
   const int per_lane = groups_of_lane(r);

@@ -194,7 +194,9 @@ def _watched(*tensors):
 def route(logits, k, scoring="softmax", renorm=True, scale=1.0, bias=None, groups=1, top_groups=1, stream=None):
     """Enqueue topoep_route: (ids int32 [T, k], weights float32 [T, k]) of the
     logits [T, E].  The ids are what a planner takes; the weights carry a
-    gradient to logits that require one (a bias gets none)."""
+    gradient to logits that require one (a bias gets none).  A bias is added to
+    the logits where experts are chosen (a bias trained on sigmoid scores is
+    another rule), and a group counts by its largest such sum."""
     r = router(logits.shape[1] if logits.dim() == 2 else 0, k, logits.dtype, scoring, renorm, scale, groups,
                top_groups)
     if stream is not None:
