@@ -9,7 +9,7 @@ the same library's ``include/topoep_moe.h``, bound by
 """
 import importlib
 
-__all__ = ["topoep", "moe", "build"]
+__all__ = ["topoep", "moe", "ffn", "build"]
 
 
 def __getattr__(name):

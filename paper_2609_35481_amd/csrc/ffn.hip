@@ -1,0 +1,503 @@
+// The gated feed-forward block and its gradients on gfx950, dense or for the rows of
+// every expert of a routed layer.
+//
+//   up       h = w silu(g) u, (g, u) = up x: a tile's P holds gate and up rows of the same
+//            units side by side, so that both of a unit end in one lane, and the
+//            activation is the product's epilogue
+//   down     y = down h, to out where dense, else by row in 32 bits
+//   combine  out_t = the sum of a token's rows in the order of its choices
+//
+//   hidden   dh = down^T dout, whose epilogue makes da (and each row's part of
+//            the weights' gradient)
+//   input    dx = up^T da, by row, then combine
+//   weights  dup = da^T x and ddown = dout^T h, an expert's rows being the inner axis
+//
+// A routed layer's tokens are never copied into the order of their experts: an
+// operand's rows are read where they are, through the pairs (a row's address is a
+// lane's own anyway).
+//
+// Which tiles there are depends on the experts' rows, which the host does not know:
+// every workgroup counts them from the offsets and takes tiles by its number.
+#include "fastdiv.h"
+#include "spans.h"
+#include "tile.h"
+#include "topoep_ffn.h"
+
+namespace {
+
+using namespace topoep_dev;
+
+struct Ffn {
+  int T, H, I, L, rows;       // rows: at most
+  const void *x;
+  int64_t ldx;
+  const int32_t *offsets, *pairs, *places;   // NULL: dense
+  const float *weights;
+  int k;
+  FastDiv per_token;
+  const void *up, *down;
+  void *out;
+  float *gu;                  // [rows, 2, I]
+  void *h;                    // [rows, I]
+  float *y;                   // [rows, H]
+  const void *dout;           // [T, H]
+  void *da;                   // [rows, 2I]
+  float *part;                // [tiles of I, rows]
+  void *dx;
+  float *dw;
+  void *dup, *ddown;
+};
+
+__device__ inline int token_of(const Ffn &a, int row) {
+  return a.pairs ? (int)fdiv((uint32_t)a.pairs[row], a.per_token) : row;
+}
+__device__ inline float weight_of(const Ffn &a, int row) { return a.pairs ? a.weights[a.pairs[row]] : 1.0f; }
+
+// ---------------------------------------------------------------- forward
+
+// BP rows of P are BP / 2 units: a wave's first half gate rows, its second half up rows.
+template <class S, bool Save>
+__global__ __launch_bounds__(S::kThreads, 2) void up_kernel(Ffn a) {
+  typedef typename S::T T;
+  TOPOEP_STAGES(S);
+  constexpr int kUnits = S::BP / 2, kWaveUnits = S::TP * 8, kHalf = S::TP / 2;
+  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), np = (a.I + kUnits - 1) / kUnits;
+  Span s;
+  const int nq = spans<S::BQ>(a.offsets, a.rows, a.L, -1, s);
+  for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
+    int tq, tp;
+    place_of(t, nq, np, tq, tp);
+    spans<S::BQ>(a.offsets, a.rows, a.L, tq, s);
+    const int unit0 = tp * kUnits;
+    Operand<T, S::BP, S::kWaves, false> p;
+    Operand<T, S::BQ, S::kWaves, false> q;
+    const char *w = static_cast<const char *>(a.up) + (int64_t)s.group * 4 * a.I * a.H;
+    by_rows<S>(p, wave, [&](int r) {
+      const int in = r % (S::TP * 16), half = in / (kHalf * 16), unit = unit0 + r / (S::TP * 16) * kWaveUnits + in % (kHalf * 16);
+      return w + (int64_t)(half * a.I + imin(unit, a.I - 1)) * a.H * 2;
+    });
+    by_rows<S>(q, wave, [&](int r) {
+      return static_cast<const char *>(a.x) + token_of(a, imin(s.first + r, s.end - 1)) * a.ldx * 2;
+    });
+    typename S::Sum d[S::TP][S::TQ] = {};
+    __syncthreads();
+    multiply<S>(p, q, wave, a.H, p0, p1, q0, q1, d);
+#pragma unroll
+    for (int j = 0; j < S::TQ; ++j) {
+      const int m = s.first + (wave / S::NP * S::TQ + j) * 16 + (lane & 15);
+      if (m >= s.end) continue;
+      const float weight = weight_of(a, m);
+#pragma unroll
+      for (int i = 0; i < kHalf; ++i) {
+        const int unit = unit0 + wave % S::NP * kWaveUnits + i * 16 + (lane >> 4) * 4;
+        if (unit >= a.I) continue;
+        const v4f g = d[i][j], u = d[i + kHalf][j];
+        v4f h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = weight * (g[e] * sigmoid(g[e]) * u[e]);
+        store4<T>(a.h, (int64_t)m * a.I + unit, h);
+        if (Save) {
+          float *to = a.gu + (int64_t)m * 2 * a.I + unit;
+          *reinterpret_cast<v4f *>(to) = g;
+          *reinterpret_cast<v4f *>(to + a.I) = u;
+        }
+      }
+    }
+  }
+}
+
+// y = down h (Back false), dx = up^T da (Back true): to `to`, of T where dense, else 32 bits.
+template <class S, bool Back>
+__global__ __launch_bounds__(S::kThreads, 2) void out_kernel(Ffn a, void *to) {
+  typedef typename S::T T;
+  TOPOEP_STAGES(S);
+  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), np = (a.H + S::BP - 1) / S::BP;
+  const int n = Back ? 2 * a.I : a.I;
+  Span s;
+  const int nq = spans<S::BQ>(a.offsets, a.rows, a.L, -1, s);
+  for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
+    int tq, tp;
+    place_of(t, nq, np, tq, tp);
+    spans<S::BQ>(a.offsets, a.rows, a.L, tq, s);
+    Operand<T, S::BP, S::kWaves, S::PA> p;
+    Operand<T, S::BQ, S::kWaves, false> q;
+    const char *w = static_cast<const char *>(Back ? a.up : a.down) + (int64_t)s.group * n * a.H * 2;
+    if constexpr (Back) across<S>(p, wave, w, a.H, tp * S::BP, a.H);
+    else by_rows<S>(p, wave, [&](int r) { return w + (int64_t)imin(tp * S::BP + r, a.H - 1) * n * 2; });
+    by_rows<S>(q, wave, [&](int r) {
+      return static_cast<const char *>(Back ? a.da : a.h) + (int64_t)imin(s.first + r, s.end - 1) * n * 2;
+    });
+    typename S::Sum d[S::TP][S::TQ] = {};
+    __syncthreads();
+    multiply<S>(p, q, wave, n, p0, p1, q0, q1, d);
+#pragma unroll
+    for (int j = 0; j < S::TQ; ++j) {
+      const int m = s.first + (wave / S::NP * S::TQ + j) * 16 + (lane & 15);
+      if (m >= s.end) continue;
+#pragma unroll
+      for (int i = 0; i < S::TP; ++i) {
+        const int c = tp * S::BP + (wave % S::NP * S::TP + i) * 16 + (lane >> 4) * 4;
+        if (c >= a.H) continue;
+        if (a.pairs) *reinterpret_cast<v4f *>(static_cast<float *>(to) + (int64_t)m * a.H + c) = d[i][j];
+        else store4<T>(to, (int64_t)m * a.H + c, d[i][j]);
+      }
+    }
+  }
+}
+
+// out_t = the sum of its rows of `from`, in the order of its choices.
+template <class T>
+__global__ __launch_bounds__(256) void combine_kernel(Ffn a, const float *from, void *to) {
+  const int groups = a.H / 4;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)a.T * groups; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = i / groups;
+    const int c = (int)(i - t * groups) * 4;
+    v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < a.k; ++j) {
+      const int m = a.places[t * a.k + j];
+      if ((unsigned)m < (unsigned)a.rows) s += *reinterpret_cast<const v4f *>(from + (int64_t)m * a.H + c);
+    }
+    store4<T>(to, t * a.H + c, s);
+  }
+}
+
+// ---------------------------------------------------------------- backward
+
+template <class S>
+__global__ __launch_bounds__(S::kThreads, 2) void hidden_kernel(Ffn a) {
+  typedef typename S::T T;
+  TOPOEP_STAGES(S);
+  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), np = (a.I + S::BP - 1) / S::BP;
+  Span s;
+  const int nq = spans<S::BQ>(a.offsets, a.rows, a.L, -1, s);
+  for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
+    int tq, tp;
+    place_of(t, nq, np, tq, tp);
+    spans<S::BQ>(a.offsets, a.rows, a.L, tq, s);
+    Operand<T, S::BP, S::kWaves, true> p;
+    Operand<T, S::BQ, S::kWaves, false> q;
+    across<S>(p, wave, static_cast<const char *>(a.down) + (int64_t)s.group * 2 * a.I * a.H, a.I, tp * S::BP, a.I);
+    by_rows<S>(q, wave, [&](int r) {
+      return static_cast<const char *>(a.dout) + (int64_t)token_of(a, imin(s.first + r, s.end - 1)) * a.H * 2;
+    });
+    typename S::Sum d[S::TP][S::TQ] = {};
+    __syncthreads();
+    multiply<S>(p, q, wave, a.H, p0, p1, q0, q1, d);
+    __syncthreads();   // the stages are read: sums go where they were
+    __attribute__((address_space(3))) float *sums = (__attribute__((address_space(3))) float *)p0;   // [NP, BQ]
+#pragma unroll
+    for (int j = 0; j < S::TQ; ++j) {
+      const int col = (wave / S::NP * S::TQ + j) * 16 + (lane & 15), m = s.first + col;
+      float sum = 0.0f;
+      if (m < s.end) {
+        const float weight = weight_of(a, m);
+#pragma unroll
+        for (int i = 0; i < S::TP; ++i) {
+          const int unit = tp * S::BP + (wave % S::NP * S::TP + i) * 16 + (lane >> 4) * 4;
+          if (unit >= a.I) continue;
+          const float *from = a.gu + (int64_t)m * 2 * a.I + unit;
+          const v4f g = *reinterpret_cast<const v4f *>(from), u = *reinterpret_cast<const v4f *>(from + a.I);
+          v4f dg, du;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float sg = sigmoid(g[e]), act = g[e] * sg, dh = d[i][j][e];
+            sum += dh * (act * u[e]);
+            dg[e] = weight * (dh * u[e] * (sg + act * (1.0f - sg)));
+            du[e] = weight * (dh * act);
+          }
+          const int64_t at = (int64_t)m * 2 * a.I + unit;
+          store4<T>(a.da, at, dg);
+          store4<T>(a.da, at + a.I, du);
+        }
+      }
+      if (a.dw) {
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 16) sums[wave % S::NP * S::BQ + col] = sum;
+      }
+    }
+    if (a.dw) {
+      __syncthreads();
+      for (int c = threadIdx.x; c < S::BQ && s.first + c < s.end; c += S::kThreads) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < S::NP; ++w) sum += sums[w * S::BQ + c];
+        a.part[(int64_t)tp * a.rows + s.first + c] = sum;
+      }
+    }
+  }
+}
+
+// A row's parts, in order, as its pair's gradient.
+__global__ __launch_bounds__(256) void weights_kernel(Ffn a, int parts) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (int64_t)a.T * a.k) return;
+  const int m = a.places[i];
+  float s = 0.0f;
+  if ((unsigned)m < (unsigned)a.rows)
+    for (int p = 0; p < parts; ++p) s += a.part[(int64_t)p * a.rows + m];
+  a.dw[i] = s;
+}
+
+// An operand across whose rows of the inner axis are tokens', through the pairs.
+template <class T, int B, int W>
+struct Tokens {
+  typedef Operand<T, B, W, true> Place;
+  static constexpr int kLoads = Place::kLoads;
+  const Ffn *a;
+  const char *base;
+  int64_t ld;                       // bytes
+  int first, column[kLoads], token[kLoads];
+  __device__ void start(const Ffn &of, int wave, const void *from, int64_t stride, int row, int c0, int n, int len) {
+    a = &of, base = static_cast<const char *>(from), ld = stride * 2, first = row;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int c = c0 + Place::piece_of(i, wave) * 8;
+      column[i] = (c < n ? c : 0) * 2;
+      token[i] = Place::row_of(i, wave) < len ? token_of(of, row + Place::row_of(i, wave)) : 0;
+    }
+  }
+  __device__ void load(Lds *to, int wave, int k, int n) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = Place::row_of(i, wave);
+      const char *p = base + token[i] * ld + column[i];
+      to_lds(at < n - k ? p : reinterpret_cast<const char *>(&kZeros), to + Place::load_of(i, wave) * 1024);
+    }
+    // the next stage's
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = k + kAcross + Place::row_of(i, wave);
+      if (at < n) token[i] = token_of(*a, first + at);
+    }
+  }
+};
+
+// dup[g][r][c] = sum over the group's rows of da[m][r] x[token][c] (Down false), ddown[g][r][c] of
+// dout[token][r] h[m][c] (Down true).
+template <class S, bool Down>
+__global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a) {
+  typedef typename S::T T;
+  TOPOEP_STAGES(S);
+  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id();
+  const int cols = Down ? a.I : a.H, rows = Down ? a.H : 2 * a.I;
+  const int np = (cols + S::BP - 1) / S::BP, nq = (rows + S::BQ - 1) / S::BQ;
+  const int g = blockIdx.x / (np * nq);
+  int tq, tp, first, end;
+  place_of(blockIdx.x % (np * nq), nq, np, tq, tp);
+  rows_of(a.offsets, a.rows, g, first, end);
+  const int n = end - first;
+  typename S::Sum d[S::TP][S::TQ] = {};
+  const auto run = [&](auto &p, auto &q) { multiply<S>(p, q, wave, n, p0, p1, q0, q1, d); };
+  if constexpr (Down) {
+    Operand<T, S::BP, S::kWaves, true> p;
+    Tokens<T, S::BQ, S::kWaves> q;
+    across<S>(p, wave, static_cast<const T *>(a.h) + (int64_t)first * a.I, a.I, tp * S::BP, a.I);
+    q.start(a, wave, a.dout, a.H, first, tq * S::BQ, a.H, n);
+    run(p, q);
+  } else {
+    Tokens<T, S::BP, S::kWaves> p;
+    Operand<T, S::BQ, S::kWaves, true> q;
+    p.start(a, wave, a.x, a.ldx, first, tp * S::BP, a.H, n);
+    across<S>(q, wave, static_cast<const T *>(a.da) + (int64_t)first * 2 * a.I, 2 * a.I, tq * S::BQ, 2 * a.I);
+    run(p, q);
+  }
+#pragma unroll
+  for (int j = 0; j < S::TQ; ++j) {
+    const int r = tq * S::BQ + (wave / S::NP * S::TQ + j) * 16 + (lane & 15);
+    if (r >= rows) continue;
+#pragma unroll
+    for (int i = 0; i < S::TP; ++i) {
+      const int c = tp * S::BP + (wave % S::NP * S::TP + i) * 16 + (lane >> 4) * 4;
+      if (c < cols) store4<T>(Down ? a.ddown : a.dup, ((int64_t)g * rows + r) * cols + c, d[i][j]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool launched() { return hipGetLastError() == hipSuccess; }
+
+constexpr int kPartUnits = 128;   // units of a part of the weights' gradient: the hidden kernel's BP
+
+struct Sizes {
+  int64_t rows;
+  size_t gu, h, y, da, part, saved, forward, backward;
+};
+
+Sizes sizes_of(const topoep_ffn *f, int32_t T, int topk) {
+  Sizes s;
+  s.rows = (int64_t)T * (topk ? topk : 1);
+  const size_t n = (size_t)s.rows, H = (size_t)f->hidden, I = (size_t)f->inter;
+  s.gu = align256(n * 2 * I * sizeof(float));
+  s.h = align256(n * I * 2);
+  s.y = topk ? align256(n * H * sizeof(float)) : 0;
+  s.da = align256(n * 2 * I * 2);
+  s.part = topk ? align256((I + kPartUnits - 1) / kPartUnits * n * sizeof(float)) : 0;
+  s.saved = s.gu + s.h;
+  s.forward = s.h + s.y;   // (h where nothing is saved)
+  s.backward = s.da + s.y + s.part;
+  return s;
+}
+
+int check(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *rows) {
+  if (!f || T < 0) return TOPOEP_EINVAL;
+  if (f->hidden < 8 || (f->hidden & 7) || f->inter < 8 || (f->inter & 7) || f->experts < 1) return TOPOEP_EINVAL;
+  if (f->hidden > 1 << 17 || f->inter > 1 << 17 || (int64_t)f->hidden * f->inter > 1 << 30) return TOPOEP_EINVAL;
+  if (f->dtype != TOPOEP_BF16 && f->dtype != TOPOEP_F16) return TOPOEP_EINVAL;
+  if (!rows && f->experts != 1) return TOPOEP_EINVAL;
+  if (rows && (rows->topk < 1 || (int64_t)T * rows->topk > INT32_MAX)) return TOPOEP_EINVAL;
+  if (f->experts > TOPOEP_FFN_MAX_EXPERTS || (rows && rows->topk > TOPOEP_ROUTER_MAX_TOPK)) return TOPOEP_ELIMIT;
+  return TOPOEP_OK;
+}
+
+Ffn args_of(const topoep_ffn *f, const void *x, int64_t ldx, int32_t T, const topoep_ffn_rows *rows, const void *up,
+            const void *down) {
+  Ffn a = {};
+  a.T = T, a.H = f->hidden, a.I = f->inter, a.L = f->experts;
+  a.x = x, a.ldx = ldx, a.up = up, a.down = down;
+  a.k = rows ? rows->topk : 1;
+  a.rows = T * a.k;
+  a.per_token = make_fastdiv((uint32_t)a.k);
+  if (rows) a.offsets = rows->offsets, a.pairs = rows->pairs, a.places = rows->places, a.weights = rows->weights;
+  return a;
+}
+
+template <class S, bool Save>
+int enqueue_up(const Ffn &a, hipStream_t st) {
+  const int64_t tiles = most_spans<S::BQ>(a.offsets, a.rows, a.L) * ((a.I + S::BP / 2 - 1) / (S::BP / 2));
+  hipLaunchKernelGGL((up_kernel<S, Save>), dim3(grid_of(tiles)), dim3(S::kThreads), 0, st, a);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
+template <class S, bool Back>
+int enqueue_out(const Ffn &a, void *to, hipStream_t st) {
+  const int64_t tiles = most_spans<S::BQ>(a.offsets, a.rows, a.L) * ((a.H + S::BP - 1) / S::BP);
+  hipLaunchKernelGGL((out_kernel<S, Back>), dim3(grid_of(tiles)), dim3(S::kThreads), 0, st, a, to);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
+template <class T>
+int enqueue_combine(const Ffn &a, void *to, hipStream_t st) {
+  const int64_t blocks = ((int64_t)a.T * (a.H / 4) + 255) / 256;
+  hipLaunchKernelGGL((combine_kernel<T>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, st, a, a.y, to);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
+template <class S, bool Down>
+int enqueue_grad(const Ffn &a, hipStream_t st) {
+  const int cols = Down ? a.I : a.H, rows = Down ? a.H : 2 * a.I;
+  const int64_t tiles = (int64_t)a.L * ((cols + S::BP - 1) / S::BP) * ((rows + S::BQ - 1) / S::BQ);
+  hipLaunchKernelGGL((grad_kernel<S, Down>), dim3((unsigned)tiles), dim3(S::kThreads), 0, st, a);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
+template <class T>
+int forward(const Ffn &a, hipStream_t st) {
+  typedef Shape<T, 128, 128, 2, 2> S;
+  int rc = a.gu ? enqueue_up<S, true>(a, st) : enqueue_up<S, false>(a, st);
+  if (rc != TOPOEP_OK) return rc;
+  rc = enqueue_out<S, false>(a, a.pairs ? static_cast<void *>(a.y) : a.out, st);
+  if (rc != TOPOEP_OK || !a.pairs) return rc;
+  return enqueue_combine<T>(a, a.out, st);
+}
+
+template <class T>
+int backward(const Ffn &a, hipStream_t st) {
+  typedef Shape<T, kPartUnits, 128, 2, 2, true, false> A;
+  typedef Shape<T, 128, 128, 2, 2, true, true> B;
+  int rc = TOPOEP_OK;
+  if (a.rows > 0 && (a.dx || a.dw || a.dup)) {
+    const int parts = (a.I + A::BP - 1) / A::BP;
+    const int64_t tiles = most_spans<A::BQ>(a.offsets, a.rows, a.L) * parts;
+    hipLaunchKernelGGL((hidden_kernel<A>), dim3(grid_of(tiles)), dim3(A::kThreads), 0, st, a);
+    if (!launched()) return TOPOEP_EHIP;
+    if (a.dw) {
+      hipLaunchKernelGGL(weights_kernel, dim3((unsigned)((a.rows + (int64_t)255) / 256)), dim3(256), 0, st, a, parts);
+      if (!launched()) return TOPOEP_EHIP;
+    }
+  }
+  if (a.rows > 0 && a.dx) {
+    rc = enqueue_out<A, true>(a, a.pairs ? static_cast<void *>(a.y) : a.dx, st);
+    if (rc == TOPOEP_OK && a.pairs) rc = enqueue_combine<T>(a, a.dx, st);
+    if (rc != TOPOEP_OK) return rc;
+  }
+  if (a.dup) rc = enqueue_grad<B, false>(a, st);
+  if (rc == TOPOEP_OK && a.ddown) rc = enqueue_grad<B, true>(a, st);
+  return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+int topoep_ffn_bytes(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *rows, size_t *forward, size_t *saved,
+                     size_t *backward) {
+  const int rc = check(f, T, rows);
+  if (rc != TOPOEP_OK) return rc;
+  const Sizes s = sizes_of(f, T, rows ? rows->topk : 0);
+  if (forward) *forward = s.forward;
+  if (saved) *saved = s.saved;
+  if (backward) *backward = s.backward;
+  return TOPOEP_OK;
+}
+
+int topoep_ffn_forward(const topoep_ffn *f, const void *x, int64_t ldx, int32_t T, const topoep_ffn_rows *rows,
+                       const void *up, const void *down, void *out, void *saved, void *workspace,
+                       size_t workspace_bytes, void *stream) {
+  const int rc = check(f, T, rows);
+  if (rc != TOPOEP_OK) return rc;
+  if (T == 0) return TOPOEP_OK;
+  if (!x || !up || !down || !out || !workspace) return TOPOEP_EINVAL;
+  if (rows && (!rows->offsets || !rows->pairs || !rows->places || !rows->weights)) return TOPOEP_EINVAL;
+  if (ldx < f->hidden || (ldx & 7) || ldx > (int64_t)1 << 40) return TOPOEP_EINVAL;
+  if (!aligned16(x) || !aligned16(up) || !aligned16(down) || !aligned16(out) || !aligned16(saved)) return TOPOEP_EINVAL;
+  const Sizes s = sizes_of(f, T, rows ? rows->topk : 0);
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < s.forward) return TOPOEP_EWORKSPACE;
+  Ffn a = args_of(f, x, ldx, T, rows, up, down);
+  a.out = out;
+  a.h = saved ? static_cast<char *>(saved) + s.gu : workspace;
+  a.gu = static_cast<float *>(saved);
+  a.y = reinterpret_cast<float *>(static_cast<char *>(workspace) + s.h);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  return f->dtype == TOPOEP_BF16 ? forward<Bf16>(a, st) : forward<F16>(a, st);
+}
+
+int topoep_ffn_backward(const topoep_ffn *f, const void *x, int64_t ldx, int32_t T, const topoep_ffn_rows *rows,
+                        const void *up, const void *down, const void *saved, const void *grad_out, void *grad_x,
+                        float *grad_weights, void *grad_up, void *grad_down, void *workspace, size_t workspace_bytes,
+                        void *stream) {
+  const int rc = check(f, T, rows);
+  if (rc != TOPOEP_OK) return rc;
+  if (T > 0) {
+    if (!x || !up || !down || !saved || !grad_out || !workspace) return TOPOEP_EINVAL;
+    if (rows && (!rows->offsets || !rows->pairs || !rows->places || !rows->weights)) return TOPOEP_EINVAL;
+    if (ldx < f->hidden || (ldx & 7) || ldx > (int64_t)1 << 40) return TOPOEP_EINVAL;
+  }
+  if (!aligned16(x) || !aligned16(up) || !aligned16(down) || !aligned16(saved) || !aligned16(grad_out) ||
+      !aligned16(grad_x) || !aligned16(grad_up) || !aligned16(grad_down))
+    return TOPOEP_EINVAL;
+  const Sizes s = sizes_of(f, T, rows ? rows->topk : 0);
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < s.backward) return TOPOEP_EWORKSPACE;
+  Ffn a = args_of(f, x, ldx, T, rows, up, down);
+  if (T == 0) a.offsets = nullptr;   // no rows, whatever they say
+  char *const kept = static_cast<char *>(const_cast<void *>(saved)), *const ws = static_cast<char *>(workspace);
+  a.gu = reinterpret_cast<float *>(kept);
+  a.h = kept ? kept + s.gu : nullptr;
+  a.da = ws;
+  a.y = reinterpret_cast<float *>(ws + s.da);
+  a.part = reinterpret_cast<float *>(ws + s.da + s.y);
+  a.dout = grad_out;
+  a.dx = grad_x;
+  a.dw = rows ? grad_weights : nullptr;
+  a.dup = grad_up;
+  a.ddown = grad_down;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  return f->dtype == TOPOEP_BF16 ? backward<Bf16>(a, st) : backward<F16>(a, st);
+}
+
+}  // extern "C"

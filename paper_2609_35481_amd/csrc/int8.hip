@@ -1,0 +1,292 @@
+// Products in 8-bit integers on gfx950: rows quantised with a scale each, and their
+// products with weights that have a scale for each channel, for all rows or the
+// rows of every expert.
+//
+// The sums are whole numbers, exact in 32 bits; scales (and the activation of a gated
+// block) are the epilogue, in 32 bits, rounded once.
+#include "tile.h"
+#include "topoep_ffn.h"
+#include "spans.h"
+
+namespace {
+
+using namespace topoep_dev;
+
+// ---------------------------------------------------------------- quantisation
+
+struct Quant {
+  const void *x;
+  int64_t ldx;
+  int M, K;
+  int8_t *q;
+  float *scale;
+  bool wide;   // rows of x at multiples of 16 bytes, K a multiple of 8
+};
+
+// x / s to the nearest integer, ties to even, at most 127 in magnitude.  The quotient rounded to 32 bits
+// can lie on the border of two integers where the quotient itself does not: then the sign of the
+// remainder, which fma keeps, tells on which side it is.
+__device__ inline int nearest(float x, float s) {
+  const float t = x / s;
+  float r = rintf(t);
+  if (fabsf(t - r) == 0.5f) {
+    const float rest = fmaf(-t, s, x);
+    r = rest > 0.0f ? t + 0.5f : rest < 0.0f ? t - 0.5f : r;
+  }
+  return (int)fminf(fmaxf(r, -127.0f), 127.0f);
+}
+
+constexpr int kEach = 8;   // elements of a load
+
+template <class T>
+__device__ inline void load8(const T *row, int k, int K, bool wide, float (&v)[kEach]) {
+  if (wide) {
+    T e[kEach];
+    __builtin_memcpy(e, __builtin_assume_aligned(row + k, 16), sizeof(e));
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) v[i] = to_float(e[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) v[i] = k + i < K ? to_float(row[k + i]) : 0.0f;
+  }
+}
+
+// Of magnitudes as unsigned words the largest: NaN's lie above infinity's.
+__device__ inline uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// W waves a row, 256 / (64 W) rows a workgroup; a thread keeps V loads of the row in registers, and reads
+// what is behind them again.
+template <class T, int W, int V>
+__global__ __launch_bounds__(256) void quantize_kernel(Quant a) {
+  __shared__ uint32_t most[4];
+  const int wave = uniform_i32(threadIdx.x >> 6), lane = threadIdx.x % (64 * W);
+  const int m = blockIdx.x * (4 / W) + wave / W;
+  const bool live = m < a.M;
+  const T *row = static_cast<const T *>(a.x) + (live ? m : 0) * a.ldx;
+  const int K = live ? a.K : 0;
+  float v[V][kEach];
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int k = (i * 64 * W + lane) * kEach;
+    if (k < K) {
+      load8(row, k, K, a.wide, v[i]);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) top = max(top, magnitude(v[i][e]));
+    }
+  }
+  for (int k = (V * 64 * W + lane) * kEach; k < K; k += 64 * W * kEach) {
+    float u[kEach];
+    load8(row, k, K, a.wide, u);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) top = max(top, magnitude(u[e]));
+  }
+  top = row_max<64>(top);
+  if (W > 1) {
+    most[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = max(top, most[w]);
+  }
+  const float scale = __uint_as_float(top) / 127.0f;
+  const bool plain = scale > 0.0f && top < 0x7F800000u;
+  if (live && lane == 0) a.scale[m] = scale;
+  // (both times 2^64 where a remainder could be too small for 32 bits)
+  const float lift = scale < 0x1p-100f ? 0x1p64f : 1.0f, step = scale * lift;
+  const auto store = [&](int k, const float (&u)[kEach]) {
+    int8_t q[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) q[e] = plain ? (int8_t)nearest(u[e] * lift, step) : (int8_t)0;
+    int8_t *to = a.q + (int64_t)m * a.K + k;
+    if (a.wide) {
+      __builtin_memcpy(to, q, kEach);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (k + e < K) to[e] = q[e];
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int k = (i * 64 * W + lane) * kEach;
+    if (k < K) store(k, v[i]);
+  }
+  for (int k = (V * 64 * W + lane) * kEach; k < K; k += 64 * W * kEach) {
+    float u[kEach];
+    load8(row, k, K, a.wide, u);
+    store(k, u);
+  }
+}
+
+// ---------------------------------------------------------------- product
+
+struct Int8 {
+  int M, N, K, G, No;         // No: columns of out
+  const int8_t *q, *w;
+  int64_t ldq;
+  const float *scale, *ws;
+  const int32_t *offsets;
+  void *out;
+  int type;
+  bool keep;
+};
+
+__device__ inline void store1(void *out, int type, int64_t at, float v) {
+  if (type == TOPOEP_F32) static_cast<float *>(out)[at] = v;
+  else if (type == TOPOEP_BF16) static_cast<Bf16 *>(out)[at] = from_float<Bf16>(v);
+  else static_cast<F16 *>(out)[at] = from_float<F16>(v);
+}
+
+// Four neighbours of a row of `n`, from column c on.
+__device__ inline void store_row(void *out, int type, int64_t row, int n, int c, v4f v) {
+  const int64_t at = row * n + c;
+  if ((n & 3) == 0) {
+    if (type == TOPOEP_F32) store4<float>(out, at, v);
+    else if (type == TOPOEP_BF16) store4<Bf16>(out, at, v);
+    else store4<F16>(out, at, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < n) store1(out, type, at + e, v[e]);
+  }
+}
+
+// Rows behind the groups' last are zeros.
+__device__ inline void clear_rest(const Int8 &a) {
+  if (!a.offsets || a.keep) return;
+  const int64_t from = (int64_t)imin(imax(a.offsets[a.G], 0), a.M) * a.No;
+  for (int64_t i = from + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < (int64_t)a.M * a.No;
+       i += (int64_t)gridDim.x * blockDim.x)
+    store1(a.out, a.type, i, 0.0f);
+}
+
+template <class S, bool Gated>
+__global__ __launch_bounds__(S::kThreads, 2) void int8_kernel(Int8 a) {
+  TOPOEP_STAGES(S);
+  constexpr int kCols = Gated ? S::BP / 2 : S::BP, kTiles = Gated ? S::TP / 2 : S::TP;   // columns of out, a wave's tiles of them
+  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), np = (a.No + kCols - 1) / kCols;
+  clear_rest(a);
+  Span s;
+  const int nq = spans<S::BQ>(a.offsets, a.M, a.G, -1, s);
+  for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
+    int tq, tp;
+    place_of(t, nq, np, tq, tp);
+    spans<S::BQ>(a.offsets, a.M, a.G, tq, s);
+    Operand<I8, S::BP, S::kWaves, false> p;
+    Operand<I8, S::BQ, S::kWaves, false> q;
+    const char *w = reinterpret_cast<const char *>(a.w) + (int64_t)s.group * a.N * a.K;
+    by_rows<S>(p, wave, [&](int r) {
+      const int in = r % (S::TP * 16), half = Gated ? in / (kTiles * 16) : 0;
+      const int c = tp * kCols + r / (S::TP * 16) * (kTiles * 16) + in % (kTiles * 16);
+      return w + (int64_t)(half * a.No + imin(c, a.No - 1)) * a.K;
+    });
+    by_rows<S>(q, wave, [&](int r) { return reinterpret_cast<const char *>(a.q) + imin(s.first + r, s.end - 1) * a.ldq; });
+    typename S::Sum d[S::TP][S::TQ] = {};
+    __syncthreads();
+    multiply<S>(p, q, wave, a.K, p0, p1, q0, q1, d);
+    const float *ws = a.ws + (int64_t)s.group * a.N;
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      const int c = tp * kCols + (wave % S::NP * kTiles + i) * 16 + (lane >> 4) * 4;
+      if (c >= a.No) continue;
+      float w0[4], w1[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w0[e] = ws[imin(c + e, a.No - 1)];
+        if (Gated) w1[e] = ws[a.No + imin(c + e, a.No - 1)];
+      }
+#pragma unroll
+      for (int j = 0; j < S::TQ; ++j) {
+        const int m = s.first + (wave / S::NP * S::TQ + j) * 16 + (lane & 15);
+        if (m >= s.end) continue;
+        const float scale = a.scale[m];
+        v4f v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = (float)d[i][j][e] * scale * w0[e];
+          if (Gated) {
+            const float u = (float)d[i + kTiles * (Gated ? 1 : 0)][j][e] * scale * w1[e];
+            v[e] = v[e] * sigmoid(v[e]) * u;
+          }
+        }
+        store_row(a.out, a.type, m, a.No, c, v);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+bool launched() { return hipGetLastError() == hipSuccess; }
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+int check(const topoep_int8 *p, int32_t M) {
+  if (!p || M < 0) return TOPOEP_EINVAL;
+  if (p->n < 1 || p->n > 1 << 20 || p->k < 16 || (p->k & 15) || p->k > 1 << 17 || p->groups < 1) return TOPOEP_EINVAL;
+  if (p->gated && (p->n & 1)) return TOPOEP_EINVAL;
+  if (p->out_dtype < TOPOEP_F32 || p->out_dtype > TOPOEP_F16) return TOPOEP_EINVAL;
+  return p->groups > TOPOEP_FFN_MAX_EXPERTS ? TOPOEP_ELIMIT : TOPOEP_OK;
+}
+
+template <class S, bool Gated>
+int enqueue(const Int8 &a, hipStream_t st) {
+  const int cols = Gated ? S::BP / 2 : S::BP;
+  const int64_t tiles = most_spans<S::BQ>(a.offsets, a.M, a.G) * ((a.No + cols - 1) / cols);
+  hipLaunchKernelGGL((int8_kernel<S, Gated>), dim3(grid_of(tiles)), dim3(S::kThreads), 0, st, a);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
+template <class T>
+int enqueue_quantize(const Quant &a, hipStream_t st) {
+  // a wave a row where that keeps the row in registers
+  if (a.K <= 64 * kEach * 4 && a.M > 1) hipLaunchKernelGGL((quantize_kernel<T, 1, 4>), dim3((a.M + 3) / 4), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((quantize_kernel<T, 4, 4>), dim3(a.M), dim3(256), 0, st, a);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+int topoep_quantize(const void *x, int32_t dtype, int64_t ldx, int32_t M, int32_t K, int8_t *q, float *scale,
+                    void *stream) {
+  if (M < 0 || K < 1 || ldx < K || ldx > (int64_t)1 << 40 || dtype < TOPOEP_F32 || dtype > TOPOEP_F16) return TOPOEP_EINVAL;
+  if (M == 0) return TOPOEP_OK;
+  const int size = dtype == TOPOEP_F32 ? 4 : 2;
+  if (!x || !q || !scale || reinterpret_cast<uintptr_t>(x) % size || reinterpret_cast<uintptr_t>(scale) % 4) return TOPOEP_EINVAL;
+  Quant a{x, ldx, M, K, q, scale, false};
+  a.wide = aligned16(x) && ldx * size % 16 == 0 && K % kEach == 0 && reinterpret_cast<uintptr_t>(q) % kEach == 0;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (dtype == TOPOEP_F32) return enqueue_quantize<float>(a, st);
+  return dtype == TOPOEP_BF16 ? enqueue_quantize<Bf16>(a, st) : enqueue_quantize<F16>(a, st);
+}
+
+int topoep_matmul_int8_workspace_bytes(const topoep_int8 *p, int32_t M, size_t *bytes_out) {
+  const int rc = check(p, M);
+  if (rc != TOPOEP_OK) return rc;
+  if (!bytes_out) return TOPOEP_EINVAL;
+  *bytes_out = 0;
+  return TOPOEP_OK;
+}
+
+int topoep_matmul_int8(const topoep_int8 *p, const int8_t *q, int64_t ldq, const float *scale, int32_t M,
+                       const int32_t *offsets, int32_t keep_rest, const int8_t *w, const float *w_scale, void *out,
+                       void *workspace, size_t workspace_bytes, void *stream) {
+  const int rc = check(p, M);
+  if (rc != TOPOEP_OK) return rc;
+  if (M == 0) return TOPOEP_OK;
+  if (!q || !scale || !w || !w_scale || !out || (!offsets && p->groups != 1)) return TOPOEP_EINVAL;
+  if (ldq < p->k || (ldq & 15) || ldq > (int64_t)1 << 40 || !aligned16(q) || !aligned16(w) || !aligned16(out)) return TOPOEP_EINVAL;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255) return TOPOEP_EWORKSPACE;
+  Int8 a = {};
+  a.M = M, a.N = p->n, a.K = p->k, a.G = p->groups, a.No = p->gated ? p->n / 2 : p->n;
+  a.q = q, a.w = w, a.ldq = ldq, a.scale = scale, a.ws = w_scale, a.offsets = offsets;
+  a.out = out, a.type = p->out_dtype, a.keep = keep_rest != 0;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  typedef Shape<I8, 128, 128, 2, 2> S;
+  return p->gated ? enqueue<S, true>(a, st) : enqueue<S, false>(a, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,236 @@
+"""The gated feed-forward block, dense and for the experts of a routed layer, with
+its gradients, against the same in 64 bits; the bounds of every element
+are derived in ffnmodel.py from the roundings the header names."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import ffnmodel  # noqa: E402
+from paper_2609_35481_amd import ffn, moe  # noqa: E402
+
+DEV = torch.device("cuda:0")
+BF16, F16 = torch.bfloat16, torch.float16
+
+
+def normal(seed, *shape, dtype=torch.float32, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std).to(dtype)
+
+
+def case(T, H, I, E, L, k, dtype, seed=0, hot=None):
+    x, up = normal(seed, T, H, dtype=dtype), normal(seed + 1, L, 2 * I, H, dtype=dtype, std=H ** -0.5)
+    down, dout = normal(seed + 2, L, H, I, dtype=dtype, std=I ** -0.5), normal(seed + 3, T, H, dtype=dtype)
+    logits = normal(seed + 4, T, E) + normal(seed + 5, E)
+    if hot is not None:
+        logits[:, hot] += 20.0
+    top = torch.topk(logits, k, dim=1)
+    weights = torch.softmax(top.values, 1)
+    slot = torch.full((E,), -1, dtype=torch.int32)
+    slot[torch.randperm(E, generator=torch.Generator().manual_seed(seed + 6))[:L]] = torch.arange(L, dtype=torch.int32)
+    return x, top.indices.to(torch.int32), weights, up, down, slot, dout
+
+
+def gradients(out, dout, **leaves):
+    return dict(zip(leaves, torch.autograd.grad(out, list(leaves.values()), dout)))
+
+
+def run_experts(x, ids, weights, up, down, slot, dout):
+    t = {n: v.to(DEV).requires_grad_() for n, v in (("x", x), ("weights", weights), ("up", up), ("down", down))}
+    out = ffn.experts(t["x"], ids.to(DEV), t["weights"], t["up"], t["down"],
+                      expert_slot=None if slot is None else slot.to(DEV))
+    return {"out": out, **gradients(out, dout.to(DEV), **t)}
+
+
+def check(got, want):
+    assert set(got) == set(want)
+    for name in want:
+        ffnmodel.within(got[name], *want[name], name)
+
+
+DENSE = [(1, 64, 32, BF16), (1, 8, 8, F16), (2, 520, 248, BF16), (15, 128, 128, F16), (16, 72, 136, BF16),
+         (17, 256, 64, BF16), (127, 136, 72, BF16), (128, 128, 256, F16), (129, 264, 104, BF16), (300, 64, 520, F16),
+         (515, 392, 200, BF16)]
+
+
+@pytest.mark.parametrize("T,H,I,dtype", DENSE)
+def test_dense_block_and_gradients(T, H, I, dtype):
+    x, up, down, dout = (normal(T, T, H, dtype=dtype), normal(1, 2 * I, H, dtype=dtype, std=H ** -0.5),
+                         normal(2, H, I, dtype=dtype, std=I ** -0.5), normal(3, T, H, dtype=dtype))
+    want = ffnmodel.dense(x, up, down, dout)
+    t = {n: v.to(DEV).requires_grad_() for n, v in (("x", x), ("up", up), ("down", down))}
+    out = ffn.feed_forward(t["x"], t["up"], t["down"])
+    check({"out": out, **gradients(out, dout.to(DEV), **t)}, want)
+    with torch.no_grad():
+        ffnmodel.within(ffn.feed_forward(t["x"], t["up"], t["down"]), *want["out"], "forward alone")
+
+
+ROUTED = [(1, 64, 32, 4, 4, 2, BF16), (1, 64, 32, 8, 2, 1, F16), (5, 136, 72, 16, 16, 8, BF16),
+          (64, 128, 64, 37, 10, 6, F16), (130, 264, 136, 4, 4, 2, BF16), (333, 72, 200, 9, 5, 4, BF16),
+          (600, 128, 128, 130, 128, 8, BF16), (257, 64, 64, 1, 1, 1, F16), (40, 64, 64, 1000, 700, 4, BF16)]
+
+
+@pytest.mark.parametrize("T,H,I,E,L,k,dtype", ROUTED)
+def test_experts_and_gradients(T, H, I, E, L, k, dtype):
+    c = case(T, H, I, E, L, k, dtype, seed=T)
+    check(run_experts(*c), ffnmodel.layer(*c[:6], c[6]))
+
+
+def test_one_expert_has_every_token():
+    c = case(300, 64, 72, 16, 16, 2, BF16, seed=3, hot=5)
+    check(run_experts(*c), ffnmodel.layer(*c[:6], c[6]))
+
+
+def test_ids_beyond_the_experts_and_the_same_expert_twice():
+    x, ids, weights, up, down, slot, dout = case(70, 64, 32, 8, 8, 4, BF16, seed=9)
+    ids[0] = torch.tensor([-1, 8, 1 << 30, -2 ** 31], dtype=torch.int32)     # nowhere: zeros
+    ids[1] = 3                                                               # four times the same
+    ids[2, 1] = 100
+    slot[ids[3, 0]] = 8                                                      # behind the last slot
+    got = run_experts(x, ids, weights, up, down, slot, dout)
+    check(got, ffnmodel.layer(x, ids, weights, up, down, slot, dout))
+    assert not got["out"][0].any() and not got["x"][0].any() and not got["weights"][0].any()
+
+
+def test_experts_that_share_a_slot():
+    x, ids, weights, up, down, slot, dout = case(90, 64, 40, 8, 3, 2, F16, seed=11)
+    slot = torch.arange(8, dtype=torch.int32) % 3
+    check(run_experts(x, ids, weights, up, down, slot, dout), ffnmodel.layer(x, ids, weights, up, down, slot, dout))
+
+
+def test_no_expert_here_and_no_tokens():
+    x, ids, weights, up, down, slot, dout = case(20, 64, 32, 8, 4, 2, BF16)
+    got = run_experts(x, ids, weights, up, down, torch.full_like(slot, -1), dout)
+    assert all(not v.any() for v in got.values())
+    got = run_experts(x[:0], ids[:0], weights[:0], up, down, slot, dout[:0])
+    assert got["out"].shape == (0, 64) and got["up"].shape == up.shape
+    assert not got["up"].any() and not got["down"].any()
+    t = {n: v.to(DEV).requires_grad_() for n, v in (("x", x[:0]), ("up", up[0]), ("down", down[0]))}
+    out = ffn.feed_forward(t["x"], t["up"], t["down"])
+    assert all(not v.any() for v in gradients(out, dout[:0].to(DEV), **t).values())
+
+
+def test_rows_apart_and_gradient_strides():
+    x, ids, weights, up, down, slot, dout = case(140, 72, 64, 8, 8, 2, BF16, seed=21)
+    want = ffnmodel.layer(x, ids, weights, up, down, slot, dout)
+    wide = torch.full((140, 72 + 40), float("nan"), dtype=BF16)
+    wide[:, 8:80] = x
+    t = {n: v.to(DEV).requires_grad_() for n, v in (("weights", weights), ("up", up), ("down", down))}
+    xs = wide.to(DEV)[:, 8:80].requires_grad_()
+    out = ffn.experts(xs, ids.to(DEV), t["weights"], t["up"], t["down"], expert_slot=slot.to(DEV))
+    turned = dout.t().contiguous().t().to(DEV)                # columns along memory
+    assert not turned.is_contiguous()
+    check({"out": out, **gradients(out, turned, x=xs, **t)}, want)
+    # a gradient that is one value, broadcast
+    out = ffn.experts(xs, ids.to(DEV), t["weights"], t["up"], t["down"], expert_slot=slot.to(DEV))
+    got = gradients(out.sum(), None, x=xs, **t)
+    want = ffnmodel.layer(x, ids, weights, up, down, slot, torch.ones_like(dout))
+    for name in got:
+        ffnmodel.within(got[name], *want[name], name)
+
+
+@pytest.mark.parametrize("wanted", [("x",), ("weights",), ("up",), ("down",), ("x", "down"), ("weights", "up")])
+def test_gradients_that_are_wanted_alone(wanted):
+    x, ids, weights, up, down, slot, dout = case(50, 64, 48, 8, 8, 2, BF16, seed=31)
+    want = ffnmodel.layer(x, ids, weights, up, down, slot, dout)
+    t = {n: v.to(DEV).requires_grad_(n in wanted) for n, v in
+         (("x", x), ("weights", weights), ("up", up), ("down", down))}
+    out = ffn.experts(t["x"], ids.to(DEV), t["weights"], t["up"], t["down"], expert_slot=slot.to(DEV))
+    for name, v in gradients(out, dout.to(DEV), **{n: t[n] for n in wanted}).items():
+        ffnmodel.within(v, *want[name], name)
+
+
+def test_gradient_against_differences():
+    """<grad, d> against (f(+d) - f(-d)) / 2 of the 64-bit layer: the differences' own error is of third
+    order, 10^-6 of a step of 10^-3; the kernel's is at most its bounds times |d|."""
+    x, ids, weights, up, down, slot, dout = case(33, 64, 40, 8, 5, 2, F16, seed=41)
+    got = run_experts(x, ids, weights, up, down, slot, dout)
+    bounds = ffnmodel.layer(x, ids, weights, up, down, slot, dout)
+    at = dict(x=x.double(), weights=weights.double(), up=up.double(), down=down.double())
+
+    def f(**kw):
+        v = {**at, **kw}
+        out = ffnmodel.layer(v["x"], ids, v["weights"], v["up"], v["down"], slot, dtype=F16)["out"][0]
+        return float((out * dout.double()).sum())
+
+    for i, name in enumerate(at):
+        d = normal(50 + i, *at[name].shape).double() * 1e-3 * float(at[name].std())
+        change = (f(**{name: at[name] + d}) - f(**{name: at[name] - d})) / 2
+        mine = float((got[name].cpu().double() * d).sum())
+        slack = float((bounds[name][1] * d.abs()).sum()) + 1e-5 * float((bounds[name][0] * d).abs().sum())
+        assert abs(mine - change) <= slack, (name, mine, change, slack)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_infinities_and_nan_stay_in_their_rows(dtype):
+    x, ids, weights, up, down, slot, dout = case(200, 64, 64, 8, 8, 2, dtype, seed=61)
+    want = ffnmodel.layer(x, ids, weights, up, down, slot)["out"]
+    bad = x.clone()
+    bad[7, 3], bad[150, 0] = float("nan"), float("inf")
+    with torch.no_grad():
+        out = ffn.experts(bad.to(DEV), ids.to(DEV), weights.to(DEV), up.to(DEV), down.to(DEV), slot.to(DEV)).cpu()
+    rest = torch.ones(200, dtype=torch.bool)
+    rest[7] = rest[150] = False
+    assert torch.isnan(out[7]).all() and not torch.isfinite(out[150]).all()
+    ffnmodel.within(out[rest], want[0][rest], want[1][rest], "the other rows")
+
+
+def test_equal_calls_give_equal_bits_and_rows_are_alike_in_any_batch():
+    c = case(260, 128, 64, 16, 16, 4, BF16, seed=71)
+    a, b = run_experts(*c), run_experts(*c)
+    for name in a:
+        assert torch.equal(a[name], b[name]), name
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^32 bytes and 2^31 elements between the first and the last row."""
+    H, I, ld = 64, 32, 1 << 24
+    rows = 140
+    flat = torch.zeros(rows * ld, dtype=BF16, device=DEV)
+    x = flat.view(rows, ld)[:, :H]
+    small = normal(81, rows, H, dtype=BF16)
+    x.copy_(small)
+    up, down, dout = (normal(82, 2 * I, H, dtype=BF16, std=0.1), normal(83, H, I, dtype=BF16, std=0.1),
+                      normal(84, rows, H, dtype=BF16))
+    t = {"x": x.requires_grad_(), "up": up.to(DEV).requires_grad_(), "down": down.to(DEV).requires_grad_()}
+    out = ffn.feed_forward(*t.values())
+    got = {"out": out, **gradients(out, dout.to(DEV), **t)}
+    check(got, ffnmodel.dense(small, up, down, dout))
+
+
+def test_refusals():
+    x, ids, weights, up, down, slot, dout = (v.to(DEV) for v in case(20, 64, 32, 8, 8, 2, BF16))
+    with pytest.raises(TypeError, match="bfloat16 or float16"):
+        ffn.experts(x.float(), ids, weights, up, down)
+    with pytest.raises(TypeError, match="up must be"):
+        ffn.experts(x, ids, weights, up.half(), down)
+    with pytest.raises(ValueError, match="contiguous"):
+        ffn.experts(x, ids, weights, up.transpose(1, 2), down)
+    with pytest.raises(ValueError, match="H"):
+        ffn.experts(x[:, :56], ids, weights, up, down)
+    with pytest.raises(TypeError, match="ids must be"):
+        ffn.experts(x, ids.long(), weights, up, down)
+    with pytest.raises(ValueError, match="row for each"):
+        ffn.experts(x, ids[:-1], weights, up, down)
+    with pytest.raises(TypeError, match="weights must be"):
+        ffn.experts(x, ids, weights.to(BF16), up, down)
+    with pytest.raises(ValueError, match="rows that do not overlap"):
+        ffn.feed_forward(x.t().contiguous().t(), up[0], down[0])
+    with pytest.raises(moe.TopoepError):      # rows at no multiple of 16 bytes
+        ffn.feed_forward(torch.zeros(4, 68, dtype=BF16, device=DEV)[:, 4:], up[0], down[0])
+    with pytest.raises(moe.TopoepError):      # H no multiple of 8
+        ffn.feed_forward(torch.zeros(4, 20, dtype=BF16, device=DEV), torch.zeros(16, 20, dtype=BF16, device=DEV),
+                         torch.zeros(20, 8, dtype=BF16, device=DEV))
+    with pytest.raises(TypeError, match="GPU"):
+        ffn.feed_forward(x.cpu(), up[0].cpu(), down[0].cpu())
+    out = ffn.feed_forward(x.clone().requires_grad_(), up[0], down[0])
+    (g,) = torch.autograd.grad(out.sum(), out.grad_fn.next_functions[0][0].variable, create_graph=True)
+    with pytest.raises(RuntimeError):         # no second derivative
+        g.sum().backward()
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))
+        with pytest.raises(RuntimeError, match="tangent"):
+            ffn.feed_forward(dual, up[0], down[0])
