@@ -70,12 +70,14 @@ typedef struct topoep_ffn_rows {
   const int32_t *places;  /* [T, k]                                                  */
   const float *weights;   /* [T, k]: the router's                                    */
   int32_t topk;           /* k, 1 .. TOPOEP_ROUTER_MAX_TOPK                          */
+  int32_t num_experts;    /* E >= 1, of which the router chose: the rows an expert   */
+                          /* gets, about, are T k / E (for the kernels' tiles alone) */
 } topoep_ffn_rows;
 
 /*
  * Bytes of a forward pass's workspace, of what it keeps for a backward pass
  * (saved), and of the backward pass's workspace, for T tokens; rows: whether
- * the layer is a routed one, and its k (topk alone is read).  NULL outputs are not written.
+ * the layer is a routed one, and its k and E (these alone are read).  NULL outputs are not written.
  */
 int topoep_ffn_bytes(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *rows, size_t *forward, size_t *saved,
                      size_t *backward);

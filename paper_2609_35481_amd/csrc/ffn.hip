@@ -29,6 +29,7 @@ using namespace topoep_dev;
 
 struct Ffn {
   int T, H, I, L, rows;       // rows: at most
+  int64_t expected;           // and about
   const void *x;
   int64_t ldx;
   const int32_t *offsets, *pairs, *places;   // NULL: dense
@@ -61,35 +62,36 @@ __global__ __launch_bounds__(S::kThreads, 2) void up_kernel(Ffn a) {
   typedef typename S::T T;
   TOPOEP_STAGES(S);
   constexpr int kUnits = S::BP / 2, kWaveUnits = S::TP * 8, kHalf = S::TP / 2;
-  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), np = (a.I + kUnits - 1) / kUnits;
+  const int np = (a.I + kUnits - 1) / kUnits;
   Span s;
   const int nq = spans<S::BQ>(a.offsets, a.rows, a.L, -1, s);
   for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
+    const Me me;
     int tq, tp;
     place_of(t, nq, np, tq, tp);
     spans<S::BQ>(a.offsets, a.rows, a.L, tq, s);
     const int unit0 = tp * kUnits;
-    Operand<T, S::BP, S::kWaves, false> p;
-    Operand<T, S::BQ, S::kWaves, false> q;
+    ByRows<T, S::BP, S::kWaves> p;
+    ByRows<T, S::BQ, S::kWaves> q;
     const char *w = static_cast<const char *>(a.up) + (int64_t)s.group * 4 * a.I * a.H;
-    by_rows<S>(p, wave, [&](int r) {
+    p.start(me, [&](int r) {
       const int in = r % (S::TP * 16), half = in / (kHalf * 16), unit = unit0 + r / (S::TP * 16) * kWaveUnits + in % (kHalf * 16);
       return w + (int64_t)(half * a.I + imin(unit, a.I - 1)) * a.H * 2;
     });
-    by_rows<S>(q, wave, [&](int r) {
+    q.start(me, [&](int r) {
       return static_cast<const char *>(a.x) + token_of(a, imin(s.first + r, s.end - 1)) * a.ldx * 2;
     });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, wave, a.H, p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, a.H, p0, p1, q0, q1, d);
 #pragma unroll
     for (int j = 0; j < S::TQ; ++j) {
-      const int m = s.first + (wave / S::NP * S::TQ + j) * 16 + (lane & 15);
+      const int m = s.first + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
       if (m >= s.end) continue;
       const float weight = weight_of(a, m);
 #pragma unroll
       for (int i = 0; i < kHalf; ++i) {
-        const int unit = unit0 + wave % S::NP * kWaveUnits + i * 16 + (lane >> 4) * 4;
+        const int unit = unit0 + me.wave % S::NP * kWaveUnits + i * 16 + (me.lane >> 4) * 4;
         if (unit >= a.I) continue;
         const v4f g = d[i][j], u = d[i + kHalf][j];
         v4f h;
@@ -111,32 +113,33 @@ template <class S, bool Back>
 __global__ __launch_bounds__(S::kThreads, 2) void out_kernel(Ffn a, void *to) {
   typedef typename S::T T;
   TOPOEP_STAGES(S);
-  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), np = (a.H + S::BP - 1) / S::BP;
+  const int np = (a.H + S::BP - 1) / S::BP;
   const int n = Back ? 2 * a.I : a.I;
   Span s;
   const int nq = spans<S::BQ>(a.offsets, a.rows, a.L, -1, s);
   for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
+    const Me me;
     int tq, tp;
     place_of(t, nq, np, tq, tp);
     spans<S::BQ>(a.offsets, a.rows, a.L, tq, s);
-    Operand<T, S::BP, S::kWaves, S::PA> p;
-    Operand<T, S::BQ, S::kWaves, false> q;
+    typename std::conditional<Back, Across<T, S::BP, S::kWaves>, ByRows<T, S::BP, S::kWaves>>::type p;
+    ByRows<T, S::BQ, S::kWaves> q;
     const char *w = static_cast<const char *>(Back ? a.up : a.down) + (int64_t)s.group * n * a.H * 2;
-    if constexpr (Back) across<S>(p, wave, w, a.H, tp * S::BP, a.H);
-    else by_rows<S>(p, wave, [&](int r) { return w + (int64_t)imin(tp * S::BP + r, a.H - 1) * n * 2; });
-    by_rows<S>(q, wave, [&](int r) {
+    if constexpr (Back) p.start(me, w, a.H, tp * S::BP, a.H);
+    else p.start(me, [&](int r) { return w + (int64_t)imin(tp * S::BP + r, a.H - 1) * n * 2; });
+    q.start(me, [&](int r) {
       return static_cast<const char *>(Back ? a.da : a.h) + (int64_t)imin(s.first + r, s.end - 1) * n * 2;
     });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, wave, n, p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, n, p0, p1, q0, q1, d);
 #pragma unroll
     for (int j = 0; j < S::TQ; ++j) {
-      const int m = s.first + (wave / S::NP * S::TQ + j) * 16 + (lane & 15);
+      const int m = s.first + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
       if (m >= s.end) continue;
 #pragma unroll
       for (int i = 0; i < S::TP; ++i) {
-        const int c = tp * S::BP + (wave % S::NP * S::TP + i) * 16 + (lane >> 4) * 4;
+        const int c = tp * S::BP + (me.wave % S::NP * S::TP + i) * 16 + (me.lane >> 4) * 4;
         if (c >= a.H) continue;
         if (a.pairs) *reinterpret_cast<v4f *>(static_cast<float *>(to) + (int64_t)m * a.H + c) = d[i][j];
         else store4<T>(to, (int64_t)m * a.H + c, d[i][j]);
@@ -167,33 +170,34 @@ template <class S>
 __global__ __launch_bounds__(S::kThreads, 2) void hidden_kernel(Ffn a) {
   typedef typename S::T T;
   TOPOEP_STAGES(S);
-  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), np = (a.I + S::BP - 1) / S::BP;
+  const int np = (a.I + S::BP - 1) / S::BP;
   Span s;
   const int nq = spans<S::BQ>(a.offsets, a.rows, a.L, -1, s);
   for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
+    const Me me;
     int tq, tp;
     place_of(t, nq, np, tq, tp);
     spans<S::BQ>(a.offsets, a.rows, a.L, tq, s);
-    Operand<T, S::BP, S::kWaves, true> p;
-    Operand<T, S::BQ, S::kWaves, false> q;
-    across<S>(p, wave, static_cast<const char *>(a.down) + (int64_t)s.group * 2 * a.I * a.H, a.I, tp * S::BP, a.I);
-    by_rows<S>(q, wave, [&](int r) {
+    Across<T, S::BP, S::kWaves> p;
+    ByRows<T, S::BQ, S::kWaves> q;
+    p.start(me, static_cast<const char *>(a.down) + (int64_t)s.group * 2 * a.I * a.H, a.I, tp * S::BP, a.I);
+    q.start(me, [&](int r) {
       return static_cast<const char *>(a.dout) + (int64_t)token_of(a, imin(s.first + r, s.end - 1)) * a.H * 2;
     });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, wave, a.H, p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, a.H, p0, p1, q0, q1, d);
     __syncthreads();   // the stages are read: sums go where they were
     __attribute__((address_space(3))) float *sums = (__attribute__((address_space(3))) float *)p0;   // [NP, BQ]
 #pragma unroll
     for (int j = 0; j < S::TQ; ++j) {
-      const int col = (wave / S::NP * S::TQ + j) * 16 + (lane & 15), m = s.first + col;
+      const int col = (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15), m = s.first + col;
       float sum = 0.0f;
       if (m < s.end) {
         const float weight = weight_of(a, m);
 #pragma unroll
         for (int i = 0; i < S::TP; ++i) {
-          const int unit = tp * S::BP + (wave % S::NP * S::TP + i) * 16 + (lane >> 4) * 4;
+          const int unit = tp * S::BP + (me.wave % S::NP * S::TP + i) * 16 + (me.lane >> 4) * 4;
           if (unit >= a.I) continue;
           const float *from = a.gu + (int64_t)m * 2 * a.I + unit;
           const v4f g = *reinterpret_cast<const v4f *>(from), u = *reinterpret_cast<const v4f *>(from + a.I);
@@ -213,7 +217,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void hidden_kernel(Ffn a) {
       if (a.dw) {
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        if (lane < 16) sums[wave % S::NP * S::BQ + col] = sum;
+        if (me.lane < 16) sums[me.wave % S::NP * S::BQ + col] = sum;
       }
     }
     if (a.dw) {
@@ -241,35 +245,28 @@ __global__ __launch_bounds__(256) void weights_kernel(Ffn a, int parts) {
 
 // An operand across whose rows of the inner axis are tokens', through the pairs.
 template <class T, int B, int W>
-struct Tokens {
-  typedef Operand<T, B, W, true> Place;
-  static constexpr int kLoads = Place::kLoads;
+struct Tokens : AcrossPlaces<B, W> {
+  typedef AcrossPlaces<B, W> At;
   const Ffn *a;
-  const char *base;
+  const char *from;
   int64_t ld;                       // bytes
-  int first, column[kLoads], token[kLoads];
-  __device__ void start(const Ffn &of, int wave, const void *from, int64_t stride, int row, int c0, int n, int len) {
-    a = &of, base = static_cast<const char *>(from), ld = stride * 2, first = row;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int c = c0 + Place::piece_of(i, wave) * 8;
-      column[i] = (c < n ? c : 0) * 2;
-      token[i] = Place::row_of(i, wave) < len ? token_of(of, row + Place::row_of(i, wave)) : 0;
-    }
+  int first, token[At::kLoads];
+  __device__ void start(const Ffn &of, Me me, const void *base, int64_t stride, int row, int c0, int n, int len) {
+    const int c = c0 + At::column_of(me);
+    a = &of, from = static_cast<const char *>(base) + (c < n ? c : 0) * 2, ld = stride * 2, first = row;
+    next(me, 0, len);
   }
-  __device__ void load(Lds *to, int wave, int k, int n) {
+  __device__ void next(Me me, int k, int n) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = Place::row_of(i, wave);
-      const char *p = base + token[i] * ld + column[i];
-      to_lds(at < n - k ? p : reinterpret_cast<const char *>(&kZeros), to + Place::load_of(i, wave) * 1024);
-    }
-    // the next stage's
+    for (int i = 0; i < At::kLoads; ++i) token[i] = k + At::row_of(i, me) < n ? token_of(*a, first + k + At::row_of(i, me)) : 0;
+  }
+  __device__ void load(Lds *to, Me me, int k, int n) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = k + kAcross + Place::row_of(i, wave);
-      if (at < n) token[i] = token_of(*a, first + at);
+    for (int i = 0; i < At::kLoads; ++i) {
+      const char *p = from + token[i] * ld;
+      to_lds(At::row_of(i, me) < n - k ? p : reinterpret_cast<const char *>(&kZeros), to + At::load_of(i, me.wave) * kApart);
     }
+    next(me, k + kAcross, n);
   }
 };
 
@@ -279,7 +276,7 @@ template <class S, bool Down>
 __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a) {
   typedef typename S::T T;
   TOPOEP_STAGES(S);
-  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id();
+  const Me me;
   const int cols = Down ? a.I : a.H, rows = Down ? a.H : 2 * a.I;
   const int np = (cols + S::BP - 1) / S::BP, nq = (rows + S::BQ - 1) / S::BQ;
   const int g = blockIdx.x / (np * nq);
@@ -288,27 +285,27 @@ __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a) {
   rows_of(a.offsets, a.rows, g, first, end);
   const int n = end - first;
   typename S::Sum d[S::TP][S::TQ] = {};
-  const auto run = [&](auto &p, auto &q) { multiply<S>(p, q, wave, n, p0, p1, q0, q1, d); };
+  const auto run = [&](auto &p, auto &q) { multiply<S>(p, q, me, n, p0, p1, q0, q1, d); };
   if constexpr (Down) {
-    Operand<T, S::BP, S::kWaves, true> p;
+    Across<T, S::BP, S::kWaves> p;
     Tokens<T, S::BQ, S::kWaves> q;
-    across<S>(p, wave, static_cast<const T *>(a.h) + (int64_t)first * a.I, a.I, tp * S::BP, a.I);
-    q.start(a, wave, a.dout, a.H, first, tq * S::BQ, a.H, n);
+    p.start(me, static_cast<const T *>(a.h) + (int64_t)first * a.I, a.I, tp * S::BP, a.I);
+    q.start(a, me, a.dout, a.H, first, tq * S::BQ, a.H, n);
     run(p, q);
   } else {
     Tokens<T, S::BP, S::kWaves> p;
-    Operand<T, S::BQ, S::kWaves, true> q;
-    p.start(a, wave, a.x, a.ldx, first, tp * S::BP, a.H, n);
-    across<S>(q, wave, static_cast<const T *>(a.da) + (int64_t)first * 2 * a.I, 2 * a.I, tq * S::BQ, 2 * a.I);
+    Across<T, S::BQ, S::kWaves> q;
+    p.start(a, me, a.x, a.ldx, first, tp * S::BP, a.H, n);
+    q.start(me, static_cast<const T *>(a.da) + (int64_t)first * 2 * a.I, 2 * a.I, tq * S::BQ, 2 * a.I);
     run(p, q);
   }
 #pragma unroll
   for (int j = 0; j < S::TQ; ++j) {
-    const int r = tq * S::BQ + (wave / S::NP * S::TQ + j) * 16 + (lane & 15);
+    const int r = tq * S::BQ + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
     if (r >= rows) continue;
 #pragma unroll
     for (int i = 0; i < S::TP; ++i) {
-      const int c = tp * S::BP + (wave % S::NP * S::TP + i) * 16 + (lane >> 4) * 4;
+      const int c = tp * S::BP + (me.wave % S::NP * S::TP + i) * 16 + (me.lane >> 4) * 4;
       if (c < cols) store4<T>(Down ? a.ddown : a.dup, ((int64_t)g * rows + r) * cols + c, d[i][j]);
     }
   }
@@ -320,7 +317,7 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool launched() { return hipGetLastError() == hipSuccess; }
 
-constexpr int kPartUnits = 128;   // units of a part of the weights' gradient: the hidden kernel's BP
+constexpr int kPartUnits = 128;   // units of a part of the weights' gradient, at least: the hidden kernel's BP
 
 struct Sizes {
   int64_t rows;
@@ -348,7 +345,7 @@ int check(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *rows) {
   if (f->hidden > 1 << 17 || f->inter > 1 << 17 || (int64_t)f->hidden * f->inter > 1 << 30) return TOPOEP_EINVAL;
   if (f->dtype != TOPOEP_BF16 && f->dtype != TOPOEP_F16) return TOPOEP_EINVAL;
   if (!rows && f->experts != 1) return TOPOEP_EINVAL;
-  if (rows && (rows->topk < 1 || (int64_t)T * rows->topk > INT32_MAX)) return TOPOEP_EINVAL;
+  if (rows && (rows->topk < 1 || rows->num_experts < 1 || (int64_t)T * rows->topk > INT32_MAX)) return TOPOEP_EINVAL;
   if (f->experts > TOPOEP_FFN_MAX_EXPERTS || (rows && rows->topk > TOPOEP_ROUTER_MAX_TOPK)) return TOPOEP_ELIMIT;
   return TOPOEP_OK;
 }
@@ -360,23 +357,62 @@ Ffn args_of(const topoep_ffn *f, const void *x, int64_t ldx, int32_t T, const to
   a.x = x, a.ldx = ldx, a.up = up, a.down = down;
   a.k = rows ? rows->topk : 1;
   a.rows = T * a.k;
+  a.expected = rows ? (int64_t)a.rows * imin(a.L, rows->num_experts) / rows->num_experts : a.rows;
   a.per_token = make_fastdiv((uint32_t)a.k);
   if (rows) a.offsets = rows->offsets, a.pairs = rows->pairs, a.places = rows->places, a.weights = rows->weights;
   return a;
 }
 
+template <class T, bool PA> using Large = Shape<T, 256, 256, PA ? 4 : 2, PA ? 2 : 4, PA, false, 2>;
+template <class T, bool PA> using Small = Shape<T, 128, 128, 2, 2, PA, false, 4>;
+template <class T> using LargeGrad = Shape<T, 256, 256, 2, 4, true, true, 1>;
+template <class T> using SmallGrad = Shape<T, 128, 128, 2, 2, true, true, 4>;
+
+// Whether a product by rows with `cols` columns of out takes large tiles (`per`: columns of a tile of 256).
+bool large_rows(const Ffn &a, int cols, int per) {
+  return large_tiles(likely_spans(a.offsets, a.expected, a.L, 256) * ((cols + per - 1) / per),
+                     likely_spans(a.offsets, a.expected, a.L, 128) * ((cols + per / 2 - 1) / (per / 2)));
+}
+
 template <class S, bool Save>
 int enqueue_up(const Ffn &a, hipStream_t st) {
   const int64_t tiles = most_spans<S::BQ>(a.offsets, a.rows, a.L) * ((a.I + S::BP / 2 - 1) / (S::BP / 2));
-  hipLaunchKernelGGL((up_kernel<S, Save>), dim3(grid_of(tiles)), dim3(S::kThreads), 0, st, a);
+  hipLaunchKernelGGL((up_kernel<S, Save>), dim3(grid_of<S>(tiles)), dim3(S::kThreads), 0, st, a);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+template <class T>
+int enqueue_up(const Ffn &a, hipStream_t st) {
+  if (large_rows(a, a.I, 128))
+    return a.gu ? enqueue_up<Large<T, false>, true>(a, st) : enqueue_up<Large<T, false>, false>(a, st);
+  return a.gu ? enqueue_up<Small<T, false>, true>(a, st) : enqueue_up<Small<T, false>, false>(a, st);
 }
 
 template <class S, bool Back>
-int enqueue_out(const Ffn &a, void *to, hipStream_t st) {
+int enqueue_out_of(const Ffn &a, void *to, hipStream_t st) {
   const int64_t tiles = most_spans<S::BQ>(a.offsets, a.rows, a.L) * ((a.H + S::BP - 1) / S::BP);
-  hipLaunchKernelGGL((out_kernel<S, Back>), dim3(grid_of(tiles)), dim3(S::kThreads), 0, st, a, to);
+  hipLaunchKernelGGL((out_kernel<S, Back>), dim3(grid_of<S>(tiles)), dim3(S::kThreads), 0, st, a, to);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+template <class T, bool Back>
+int enqueue_out(const Ffn &a, void *to, hipStream_t st) {
+  return large_rows(a, a.H, 256) ? enqueue_out_of<Large<T, Back>, Back>(a, to, st)
+                                 : enqueue_out_of<Small<T, Back>, Back>(a, to, st);
+}
+
+template <class S>
+int enqueue_hidden_of(const Ffn &a, hipStream_t st) {
+  const int parts = (a.I + S::BP - 1) / S::BP;
+  const int64_t tiles = most_spans<S::BQ>(a.offsets, a.rows, a.L) * parts;
+  hipLaunchKernelGGL((hidden_kernel<S>), dim3(grid_of<S>(tiles)), dim3(S::kThreads), 0, st, a);
+  if (!launched()) return TOPOEP_EHIP;
+  if (!a.dw) return TOPOEP_OK;
+  hipLaunchKernelGGL(weights_kernel, dim3((unsigned)((a.rows + (int64_t)255) / 256)), dim3(256), 0, st, a, parts);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+template <class T>
+int enqueue_hidden(const Ffn &a, hipStream_t st) {
+  static_assert(Small<T, true>::BP >= kPartUnits, "parts of the weights' gradient");
+  return large_rows(a, a.I, 256) ? enqueue_hidden_of<Large<T, true>>(a, st) : enqueue_hidden_of<Small<T, true>>(a, st);
 }
 
 template <class T>
@@ -387,45 +423,37 @@ int enqueue_combine(const Ffn &a, void *to, hipStream_t st) {
 }
 
 template <class S, bool Down>
-int enqueue_grad(const Ffn &a, hipStream_t st) {
-  const int cols = Down ? a.I : a.H, rows = Down ? a.H : 2 * a.I;
-  const int64_t tiles = (int64_t)a.L * ((cols + S::BP - 1) / S::BP) * ((rows + S::BQ - 1) / S::BQ);
+int enqueue_grad_of(const Ffn &a, int64_t tiles, hipStream_t st) {
   hipLaunchKernelGGL((grad_kernel<S, Down>), dim3((unsigned)tiles), dim3(S::kThreads), 0, st, a);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+template <class T, bool Down>
+int enqueue_grad(const Ffn &a, hipStream_t st) {
+  const int cols = Down ? a.I : a.H, rows = Down ? a.H : 2 * a.I;
+  const auto tiles = [&](int64_t n) { return a.L * ((cols + n - 1) / n) * ((rows + n - 1) / n); };
+  return large_tiles(tiles(256), tiles(128)) ? enqueue_grad_of<LargeGrad<T>, Down>(a, tiles(256), st)
+                                             : enqueue_grad_of<SmallGrad<T>, Down>(a, tiles(128), st);
 }
 
 template <class T>
 int forward(const Ffn &a, hipStream_t st) {
-  typedef Shape<T, 128, 128, 2, 2> S;
-  int rc = a.gu ? enqueue_up<S, true>(a, st) : enqueue_up<S, false>(a, st);
+  int rc = enqueue_up<T>(a, st);
   if (rc != TOPOEP_OK) return rc;
-  rc = enqueue_out<S, false>(a, a.pairs ? static_cast<void *>(a.y) : a.out, st);
+  rc = enqueue_out<T, false>(a, a.pairs ? static_cast<void *>(a.y) : a.out, st);
   if (rc != TOPOEP_OK || !a.pairs) return rc;
   return enqueue_combine<T>(a, a.out, st);
 }
 
 template <class T>
 int backward(const Ffn &a, hipStream_t st) {
-  typedef Shape<T, kPartUnits, 128, 2, 2, true, false> A;
-  typedef Shape<T, 128, 128, 2, 2, true, true> B;
   int rc = TOPOEP_OK;
-  if (a.rows > 0 && (a.dx || a.dw || a.dup)) {
-    const int parts = (a.I + A::BP - 1) / A::BP;
-    const int64_t tiles = most_spans<A::BQ>(a.offsets, a.rows, a.L) * parts;
-    hipLaunchKernelGGL((hidden_kernel<A>), dim3(grid_of(tiles)), dim3(A::kThreads), 0, st, a);
-    if (!launched()) return TOPOEP_EHIP;
-    if (a.dw) {
-      hipLaunchKernelGGL(weights_kernel, dim3((unsigned)((a.rows + (int64_t)255) / 256)), dim3(256), 0, st, a, parts);
-      if (!launched()) return TOPOEP_EHIP;
-    }
-  }
-  if (a.rows > 0 && a.dx) {
-    rc = enqueue_out<A, true>(a, a.pairs ? static_cast<void *>(a.y) : a.dx, st);
+  if (a.rows > 0 && (a.dx || a.dw || a.dup)) rc = enqueue_hidden<T>(a, st);
+  if (rc == TOPOEP_OK && a.rows > 0 && a.dx) {
+    rc = enqueue_out<T, true>(a, a.pairs ? static_cast<void *>(a.y) : a.dx, st);
     if (rc == TOPOEP_OK && a.pairs) rc = enqueue_combine<T>(a, a.dx, st);
-    if (rc != TOPOEP_OK) return rc;
   }
-  if (a.dup) rc = enqueue_grad<B, false>(a, st);
-  if (rc == TOPOEP_OK && a.ddown) rc = enqueue_grad<B, true>(a, st);
+  if (rc == TOPOEP_OK && a.dup) rc = enqueue_grad<T, false>(a, st);
+  if (rc == TOPOEP_OK && a.ddown) rc = enqueue_grad<T, true>(a, st);
   return rc;
 }
 

@@ -164,30 +164,31 @@ template <class S, bool Gated>
 __global__ __launch_bounds__(S::kThreads, 2) void int8_kernel(Int8 a) {
   TOPOEP_STAGES(S);
   constexpr int kCols = Gated ? S::BP / 2 : S::BP, kTiles = Gated ? S::TP / 2 : S::TP;   // columns of out, a wave's tiles of them
-  const int wave = uniform_i32(threadIdx.x >> 6), lane = lane_id(), np = (a.No + kCols - 1) / kCols;
+  const int np = (a.No + kCols - 1) / kCols;
   clear_rest(a);
   Span s;
   const int nq = spans<S::BQ>(a.offsets, a.M, a.G, -1, s);
   for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
+    const Me me;
     int tq, tp;
     place_of(t, nq, np, tq, tp);
     spans<S::BQ>(a.offsets, a.M, a.G, tq, s);
-    Operand<I8, S::BP, S::kWaves, false> p;
-    Operand<I8, S::BQ, S::kWaves, false> q;
+    ByRows<I8, S::BP, S::kWaves> p;
+    ByRows<I8, S::BQ, S::kWaves> q;
     const char *w = reinterpret_cast<const char *>(a.w) + (int64_t)s.group * a.N * a.K;
-    by_rows<S>(p, wave, [&](int r) {
+    p.start(me, [&](int r) {
       const int in = r % (S::TP * 16), half = Gated ? in / (kTiles * 16) : 0;
       const int c = tp * kCols + r / (S::TP * 16) * (kTiles * 16) + in % (kTiles * 16);
       return w + (int64_t)(half * a.No + imin(c, a.No - 1)) * a.K;
     });
-    by_rows<S>(q, wave, [&](int r) { return reinterpret_cast<const char *>(a.q) + imin(s.first + r, s.end - 1) * a.ldq; });
+    q.start(me, [&](int r) { return reinterpret_cast<const char *>(a.q) + imin(s.first + r, s.end - 1) * a.ldq; });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, wave, a.K, p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, a.K, p0, p1, q0, q1, d);
     const float *ws = a.ws + (int64_t)s.group * a.N;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
-      const int c = tp * kCols + (wave % S::NP * kTiles + i) * 16 + (lane >> 4) * 4;
+      const int c = tp * kCols + (me.wave % S::NP * kTiles + i) * 16 + (me.lane >> 4) * 4;
       if (c >= a.No) continue;
       float w0[4], w1[4];
 #pragma unroll
@@ -197,7 +198,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void int8_kernel(Int8 a) {
       }
 #pragma unroll
       for (int j = 0; j < S::TQ; ++j) {
-        const int m = s.first + (wave / S::NP * S::TQ + j) * 16 + (lane & 15);
+        const int m = s.first + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
         if (m >= s.end) continue;
         const float scale = a.scale[m];
         v4f v;
@@ -228,11 +229,14 @@ int check(const topoep_int8 *p, int32_t M) {
   return p->groups > TOPOEP_FFN_MAX_EXPERTS ? TOPOEP_ELIMIT : TOPOEP_OK;
 }
 
+typedef Shape<I8, 256, 256, 2, 4, false, false, 2> Large;
+typedef Shape<I8, 128, 128, 2, 2, false, false, 4> Small;
+
 template <class S, bool Gated>
 int enqueue(const Int8 &a, hipStream_t st) {
   const int cols = Gated ? S::BP / 2 : S::BP;
   const int64_t tiles = most_spans<S::BQ>(a.offsets, a.M, a.G) * ((a.No + cols - 1) / cols);
-  hipLaunchKernelGGL((int8_kernel<S, Gated>), dim3(grid_of(tiles)), dim3(S::kThreads), 0, st, a);
+  hipLaunchKernelGGL((int8_kernel<S, Gated>), dim3(grid_of<S>(tiles)), dim3(S::kThreads), 0, st, a);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
@@ -285,8 +289,11 @@ int topoep_matmul_int8(const topoep_int8 *p, const int8_t *q, int64_t ldq, const
   a.out = out, a.type = p->out_dtype, a.keep = keep_rest != 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  typedef Shape<I8, 128, 128, 2, 2> S;
-  return p->gated ? enqueue<S, true>(a, st) : enqueue<S, false>(a, st);
+  const int per = p->gated ? 128 : 256;
+  if (large_tiles(likely_spans(offsets, M, a.G, 256) * ((a.No + per - 1) / per),
+                  likely_spans(offsets, M, a.G, 128) * ((a.No + per / 2 - 1) / (per / 2))))
+    return p->gated ? enqueue<Large, true>(a, st) : enqueue<Large, false>(a, st);
+  return p->gated ? enqueue<Small, true>(a, st) : enqueue<Small, false>(a, st);
 }
 
 }  // extern "C"

@@ -2,6 +2,8 @@
 // operands are reached.
 #pragma once
 
+#include <type_traits>
+
 #include "tile.h"
 
 namespace topoep_dev {
@@ -57,44 +59,39 @@ __device__ inline void place_of(int t, int nq, int np, int &q, int &p) {
 // Static LDS of a product: two stages of each operand, variables of their own, so
 // that the compiler sees that a stage's reads do not wait for the other's loads.
 #define TOPOEP_STAGES(S)                                                                 \
-  __shared__ v4i stage_p0[S::BP * kLine / 16], stage_p1[S::BP * kLine / 16];             \
-  __shared__ v4i stage_q0[S::BQ * kLine / 16], stage_q1[S::BQ * kLine / 16];             \
+  __shared__ v4i stage_p0[S::kBytesP / 16], stage_p1[S::kBytesP / 16];                   \
+  __shared__ v4i stage_q0[S::kBytesQ / 16], stage_q1[S::kBytesQ / 16];                   \
   Lds *const p0 = (Lds *)stage_p0, *const p1 = (Lds *)stage_p1, *const q0 = (Lds *)stage_q0, *const q1 = (Lds *)stage_q1
 
-// An operand by rows: row(r) gives the address of tile row r.
-template <class S, class O, class F>
-__device__ inline void by_rows(O &o, int wave, const F &row) {
-  o.step = kLine;
-#pragma unroll
-  for (int i = 0; i < O::kLoads; ++i) o.from[i] = row(o.row_of(i, wave)) + o.piece_of(i, wave) * 16;
-}
-// An operand across: `base` its first row of the inner axis, ld elements apart; of its `n` columns those
-// from c0 on (a column that does not exist is column 0).
-template <class S, class O>
-__device__ inline void across(O &o, int wave, const void *base, int64_t ld, int c0, int n) {
-  o.step = kAcross * ld * 2;
-#pragma unroll
-  for (int i = 0; i < O::kLoads; ++i) {
-    const int c = c0 + o.piece_of(i, wave) * 8;
-    o.from[i] = static_cast<const char *>(base) + (o.row_of(i, wave) * ld + (c < n ? c : 0)) * 2;
-  }
-}
-
+// Four neighbours, rounded to nearest even.
 template <class T>
 __device__ inline void store4(void *to, int64_t at, v4f v) {
-  T o[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = from_float<T>(v[i]);
-  __builtin_memcpy(static_cast<T *>(to) + at, o, sizeof(o));
+  typedef typename std::conditional<std::is_same<T, Bf16>::value, __bf16,
+                                    typename std::conditional<std::is_same<T, F16>::value, _Float16, float>::type>::type E;
+  typedef E v4e __attribute__((ext_vector_type(4)));
+  const v4e o = __builtin_convertvector(v, v4e);
+  __builtin_memcpy(static_cast<E *>(to) + at, &o, sizeof(o));
 }
 
-// Workgroups for at most `tiles` tiles: two a CU, which take them in turn.
-inline unsigned grid_of(int64_t tiles) { return (unsigned)(tiles < 512 ? (tiles < 1 ? 1 : tiles) : 512); }
+// Workgroups of S for at most `tiles` tiles: as many as a CU holds, which take them in turn.
+template <class S>
+inline unsigned grid_of(int64_t tiles) {
+  const int64_t most = S::BP * S::BQ > 128 * 128 ? 256 : 512;
+  return (unsigned)(tiles < most ? (tiles < 1 ? 1 : tiles) : most);
+}
 
 // Tiles of B rows at most.
 template <int B>
 inline int64_t most_spans(const int32_t *offsets, int rows, int groups) {
   return ((int64_t)rows + B - 1) / B + (offsets ? imin(groups, rows) : 0);
 }
+// And about, of `expected` rows.
+inline int64_t likely_spans(const int32_t *offsets, int64_t expected, int groups, int B) {
+  return expected / B + (offsets ? (imin(groups, (int)expected) + 1) / 2 : expected % B != 0);
+}
+
+// Whether tiles of 256 x 256 take less time than their number of 128 x 128: one of the former a CU,
+// two of the latter, which reach 1340 and 1100 TFLOP/s (8192^3 in bf16).
+inline bool large_tiles(int64_t large, int64_t small) { return (large + 255) / 256 * 10 < (small + 511) / 512 * 6; }
 
 }  // namespace topoep_dev

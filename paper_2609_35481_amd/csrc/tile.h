@@ -5,11 +5,9 @@
 // the stage before it is multiplied.  P is the matrix instruction's A operand, so
 // a lane ends with four neighbouring p of one q: outputs are rows of p.
 //
-// An operand lies in memory either by rows (k runs along memory: 8 pieces of 16
-// bytes a row and stage, the piece's place turned by the row so that the 16 rows
-// a read takes meet every bank once), or across (p or q runs along memory, k over
-// its rows: then LDS holds 64 rows of k, and reads transpose 16-bit elements on
-// their way to the registers).
+// An operand lies in memory either by rows (k runs along memory), or across (p or
+// q runs along memory, k over its rows: then reads from LDS transpose 16-bit
+// elements on their way to the registers).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -61,64 +59,115 @@ __device__ inline void to_lds(const char *from, Lds *to) {
                                    (__attribute__((address_space(3))) void *)to, 16, 0, 0);
 }
 
-// One operand of B rows, brought in by W waves.
-template <class T, int B, int W, bool Across>
-struct Operand {
+// A thread's wave and lane.  Asked for anew for every tile, in a way that the compiler does not
+// see through: what it forms from the lane would else stay in registers over all tiles, which
+// the sums of 256 x 256 leave no room for.
+struct Me {
+  int wave, lane;
+  __device__ Me() : wave(uniform_i32(threadIdx.x >> 6)), lane(lane_id()) { asm volatile("" : "+v"(lane)); }
+};
+
+// An operand by rows: B rows, brought in by W waves.  LDS holds 8 pieces of 16 bytes a row
+// and stage, a piece's place turned by the row, so that the 16 rows that a read takes meet
+// every bank once.
+template <class T, int B, int W>
+struct ByRows {
   static constexpr int kBytes = B * kLine;
-  static constexpr int kPieces = B / 8;                              // a wave's load is 1 KiB
-  static constexpr int kLoads = (kPieces + W - 1) / W;               // (too few for all waves: some bring the same)
-  static constexpr int kRowPieces = Across ? B / 8 : 8;              // 16 bytes each
+  static constexpr int kPieces = B / 8;                  // a wave's load is 8 rows
+  static constexpr int kLoads = (kPieces + W - 1) / W;   // (too few for all waves: some bring the same)
   const char *from[kLoads];
-  int64_t step;                                                      // bytes from a stage to the next
 
-  // Which wave load is this thread's i-th, and of it the row and the piece in memory.
   static __device__ int load_of(int i, int wave) { return (i * W + wave) % kPieces; }
-  static __device__ int turn(int row) {
-    return Across ? ((row & 3) | (row >> 1 & 4)) * 2 & (kRowPieces - 1) & ~1 : row & 7;
-  }
-  static __device__ int row_of(int i, int wave) { return (load_of(i, wave) * 64 + lane_id()) / kRowPieces; }
-  static __device__ int piece_of(int i, int wave) {
-    return (load_of(i, wave) * 64 + lane_id()) % kRowPieces ^ turn(row_of(i, wave));
-  }
+  static __device__ int row_of(int i, Me me) { return load_of(i, me.wave) * 8 + (me.lane >> 3); }
+  static __device__ int piece_of(Me me) { return (me.lane & 7) ^ (me.lane >> 3); }
 
-  __device__ void load(Lds *to, int wave, int k, int n) {
-    // k: elements done, n: of the inner axis
+  // row(r) gives the address of row r of the tile.
+  template <class F>
+  __device__ void start(Me me, const F &row) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) from[i] = row(row_of(i, me)) + piece_of(me) * 16;
+  }
+  // A stage, k elements of the n done.
+  __device__ void load(Lds *to, Me me, int k, int n) {
+    const bool in = piece_of(me) * (16 / (int)sizeof(T)) < n - k;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int at = Across ? row_of(i, wave) : piece_of(i, wave) * (16 / (int)sizeof(T));
-      const char *p = at < n - k ? from[i] : reinterpret_cast<const char *>(&kZeros);
-      to_lds(p, to + load_of(i, wave) * 1024);
-      from[i] += step;
+      to_lds(in ? from[i] : reinterpret_cast<const char *>(&kZeros), to + load_of(i, me.wave) * 1024);
+      from[i] += kLine;
     }
   }
 };
 
-// A wave's view of an operand in LDS: N tiles of 16 rows from row0 on.
-template <class T, int B, int N, bool Across>
+// An operand across: 64 rows of k a stage, B elements of 16 bits each.  A transposing read takes, of
+// 16 elements, the rows 8 b + 4 h + r (+ 32 s): b = 0..3 by the lane's block of 16, r = 0..3 inside it, h and
+// s one read each.  A wave's load holds rows that no read takes together (h, for narrower rows s and b's
+// upper bit too), and loads lie 32 bytes more than their 1 KiB apart: a read's rows meet every
+// bank once, and every place is one lane's base and a constant.
+constexpr int kApart = 1024 + 32;
+template <int B, int W>
+struct AcrossPlaces {
+  static constexpr int kRowPieces = B / 8, kRows = 64 / kRowPieces;   // pieces of 16 bytes a row, rows a load
+  static constexpr int kPieces = 64 / kRows, kBytes = kPieces * kApart;
+  static constexpr int kLoads = (kPieces + W - 1) / W;
+  static __device__ int load_of(int i, int wave) { return (i * W + wave) % kPieces; }
+  // The row of k of load j (the same for all lanes) and what the lane adds to it.
+  static __device__ int row_of_load(int j) { return (j & 3) + (j >> 2 & (B == 64 ? 1 : 3)) * 8 + (B == 256 ? j >> 4 : 0) * 32; }
+  static __device__ int row_of_lane(Me me) {
+    const int sub = me.lane / kRowPieces;
+    return (sub & 1) * 4 + (B < 256 ? sub >> 1 & 1 : 0) * 32 + (B == 64 ? sub >> 2 : 0) * 16;
+  }
+  static __device__ int column_of(Me me) { return me.lane % kRowPieces * 8; }
+  static __device__ int row_of(int i, Me me) { return row_of_load(load_of(i, me.wave)) + row_of_lane(me); }
+};
+
+template <class T, int B, int W>
+struct Across : AcrossPlaces<B, W> {
+  typedef AcrossPlaces<B, W> At;
+  const char *from;
+  int64_t ld;   // bytes
+
+  // `base`: row 0 of the inner axis, rows `stride` elements apart; of its n columns those from c0 on (one
+  // that does not exist is column 0).
+  __device__ void start(Me me, const void *base, int64_t stride, int c0, int n) {
+    const int c = c0 + At::column_of(me);
+    ld = stride * 2;
+    from = static_cast<const char *>(base) + At::row_of_lane(me) * ld + (c < n ? c : 0) * 2;
+  }
+  __device__ void load(Lds *to, Me me, int k, int n) {
+    const int left = n - k - At::row_of_lane(me);
+#pragma unroll
+    for (int i = 0; i < At::kLoads; ++i) {
+      const int j = At::load_of(i, me.wave), row = At::row_of_load(j);
+      to_lds(row < left ? from + row * ld : reinterpret_cast<const char *>(&kZeros), to + j * kApart);
+    }
+    from += kAcross * ld;
+  }
+};
+
+// A wave's view of an operand in LDS: tiles of 16 rows from row0 on.
+template <class T, int B, bool IsAcross>
 struct View {
-  static constexpr int kBases = Across ? (N < 4 ? N : 4) : 2;
-  int at[kBases];
-  __device__ explicit View(int row0) {
-    const int l = lane_id();
-    if (!Across) {
+  int at[IsAcross ? 1 : 2];
+  __device__ View(int row0, int l) {
+    if constexpr (!IsAcross) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) at[s] = (row0 + l % 16) * kLine + ((s * 4 + l / 16) ^ (l & 7)) * 16;
     } else {
       // lanes 4 r .. 4 r + 3 of a block of 16 read row r's 32 bytes
-      const int i = l & 15, k = (l >> 4) * 8 + (i >> 2), turn = Operand<T, B, 1, true>::turn(k);
-#pragma unroll
-      for (int t = 0; t < kBases; ++t)
-        at[t] = k * B * 2 + ((((row0 / 16 + t) * 2) ^ turn) + (i >> 1 & 1)) * 16 + (i & 1) * 8;
+      const int b = l >> 4, r = l >> 2 & 3;
+      at[0] = ((B == 64 ? b & 1 : b) * 4 + r) * kApart + (B == 64 ? b >> 1 : 0) * 512 + row0 * 2 + (l & 3) * 8;
     }
   }
   __device__ v4i get(const Lds *from, int tile, int s) const {
-    if (!Across) return *reinterpret_cast<const __attribute__((address_space(3))) v4i *>(from + at[s] + tile * 16 * kLine);
-    // (four tiles on, the place moves by 128 bytes: the turn, below 128, leaves that bit alone only if aligned)
-    const Lds *p = from + (at[tile % kBases] ^ (tile / kBases * 128)) + s * 32 * B * 2;
-    const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)p);
-    const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(p + 4 * B * 2));
-    const v2i x = __builtin_bit_cast(v2i, a), y = __builtin_bit_cast(v2i, b);
-    return v4i{x[0], x[1], y[0], y[1]};
+    if constexpr (!IsAcross) {
+      return *reinterpret_cast<const __attribute__((address_space(3))) v4i *>(from + at[s] + tile * 16 * kLine);
+    } else {
+      const Lds *p = from + at[0] + tile * 32 + (B == 256 ? s * 16 * kApart : s * 2 * B * 2);
+      const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)p);
+      const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(p + B * 2));
+      const v2i u = __builtin_bit_cast(v2i, x), v = __builtin_bit_cast(v2i, y);
+      return v4i{u[0], u[1], v[0], v[1]};
+    }
   }
 };
 
@@ -131,21 +180,46 @@ __device__ inline void arrived() {
   asm volatile("" ::: "memory");
 }
 
-// The shape of a tile's work: BP x BQ, by NP x NQ waves.
-template <class T_, int BP_, int BQ_, int NP_, int NQ_, bool PA_ = false, bool QA_ = false>
+// The shape of a tile's work: BP x BQ, by NP x NQ waves; Ahead: a stage's loads issued before
+// each of its first groups of matrix instructions.
+template <class T_, int BP_, int BQ_, int NP_, int NQ_, bool PA_, bool QA_, int Ahead_>
 struct Shape {
   typedef T_ T;
+  static constexpr int Ahead = Ahead_;
   static constexpr int BP = BP_, BQ = BQ_, NP = NP_, NQ = NQ_, kWaves = NP * NQ, kThreads = 64 * kWaves;
   static constexpr bool PA = PA_, QA = QA_;
   static constexpr int TP = BP / NP / 16, TQ = BQ / NQ / 16;
   static constexpr int kStage = PA ? kAcross : kLine / (int)sizeof(T);
-  static constexpr int kBytes = (BP + BQ) * kLine;
+  static constexpr int kBytesP = PA ? AcrossPlaces<BP, kWaves>::kBytes : BP * kLine;
+  static constexpr int kBytesQ = QA ? AcrossPlaces<BQ, kWaves>::kBytes : BQ * kLine;
   typedef typename Mul<T>::Sum Sum;
-  typedef View<T, BP, TP, PA> PView;
-  typedef View<T, BQ, TQ, QA> QView;
+  typedef View<T, BP, PA> PView;
+  typedef View<T, BQ, QA> QView;
 };
 
-template <class S>
+#ifndef VAR
+#define VAR 1
+#endif
+// The order of a stage's instructions, which the compiler would leave to itself with
+// the next stage's loads last: operands are read from LDS two groups of matrix
+// instructions ahead, loads spread over the first groups (8192^3 in bf16, 256 x 256 tiles:
+// 1093 TFLOP/s without, 1340 with).
+template <class S, int Loads, int G = 0>
+__device__ inline void stage_order() {
+  constexpr int RP = S::PA ? 2 : 1, RQ = S::QA ? 2 : 1, kGroups = 2 * S::TP;
+  if constexpr (G == 0) __builtin_amdgcn_sched_group_barrier(0x100, S::TQ * RQ + 2 * RP, 0);
+  if constexpr (G < kGroups) {
+    constexpr int loads = Loads - G * S::Ahead < S::Ahead ? Loads - G * S::Ahead : S::Ahead;
+    if constexpr (loads > 0) __builtin_amdgcn_sched_group_barrier(0x20, loads, 0);
+    __builtin_amdgcn_sched_group_barrier(0x8, S::TQ, 0);
+    constexpr int kEarly = S::TP > 2 ? S::TP - 2 : 1;   // groups before which the second half's Q is read
+    constexpr int reads = (G + 2 < kGroups ? RP : 0) + (G < kEarly ? (S::TQ * RQ + kEarly - 1) / kEarly : 0);
+    if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
+    stage_order<S, Loads, G + 1>();
+  }
+}
+
+template <class S, int Loads>
 __device__ inline void multiply_stage(const Lds *ps, const Lds *qs, const typename S::PView &pv, const typename S::QView &qv,
                                       typename S::Sum (&d)[S::TP][S::TQ]) {
 #pragma unroll
@@ -160,27 +234,33 @@ __device__ inline void multiply_stage(const Lds *ps, const Lds *qs, const typena
       for (int j = 0; j < S::TQ; ++j) d[i][j] = Mul<typename S::T>::add(p, q[j], d[i][j]);
     }
   }
+  stage_order<S, Loads>();
 }
 
+// d += P Q over the n elements of the inner axis: one stage is multiplied while the next one
+// is on its way.  Every wave is done with a stage's LDS when the next barrier lets loads into it.
 template <class S, class P, class Q>
-__device__ inline void multiply(P &p, Q &q, int wave, int n, Lds *p0, Lds *p1, Lds *q0, Lds *q1, typename S::Sum (&d)[S::TP][S::TQ]) {
-  const typename S::PView pv(wave % S::NP * S::TP * 16);
-  const typename S::QView qv(wave / S::NP * S::TQ * 16);
+__device__ inline void multiply(P &p, Q &q, Me me, int n, Lds *p0, Lds *p1, Lds *q0, Lds *q1,
+                                typename S::Sum (&d)[S::TP][S::TQ]) {
+  constexpr int kLoads = P::kLoads + Q::kLoads;
+  const typename S::PView pv(me.wave % S::NP * S::TP * 16, me.lane);
+  const typename S::QView qv(me.wave / S::NP * S::TQ * 16, me.lane);
   const int stages = (n + S::kStage - 1) / S::kStage;
-  if (stages > 0) p.load(p0, wave, 0, n), q.load(q0, wave, 0, n);
+  if (stages > 0) p.load(p0, me, 0, n), q.load(q0, me, 0, n);
   int k = S::kStage;
+#pragma unroll 1
   for (int g = stages >> 1; g > 0; --g) {
     arrived<0>();
-    p.load(p1, wave, k, n), q.load(q1, wave, k, n);
-    multiply_stage<S>(p0, q0, pv, qv, d);
+    p.load(p1, me, k, n), q.load(q1, me, k, n);
+    multiply_stage<S, kLoads>(p0, q0, pv, qv, d);
     arrived<0>();
     // (behind the last stage: zeros)
-    p.load(p0, wave, k + S::kStage, n), q.load(q0, wave, k + S::kStage, n);
-    multiply_stage<S>(p1, q1, pv, qv, d);
+    p.load(p0, me, k + S::kStage, n), q.load(q0, me, k + S::kStage, n);
+    multiply_stage<S, kLoads>(p1, q1, pv, qv, d);
     k += 2 * S::kStage;
   }
   arrived<0>();
-  if (stages & 1) multiply_stage<S>(p0, q0, pv, qv, d);
+  if (stages & 1) multiply_stage<S, 0>(p0, q0, pv, qv, d);
 }
 
 }  // namespace topoep_dev

@@ -33,7 +33,7 @@ class Ffn(ctypes.Structure):
 class Rows(ctypes.Structure):
     """topoep_ffn_rows: where the rows of the experts are, and k."""
     _fields_ = [("offsets", ctypes.c_void_p), ("pairs", ctypes.c_void_p), ("places", ctypes.c_void_p),
-                ("weights", ctypes.c_void_p), ("topk", ctypes.c_int32)]
+                ("weights", ctypes.c_void_p), ("topk", ctypes.c_int32), ("num_experts", ctypes.c_int32)]
 
 
 class Int8(ctypes.Structure):
@@ -129,7 +129,7 @@ def expert_rows(ids, L, expert_slot=None, stream=None):
 
 class _Block:
     """A call's sizes and operands, as the library takes them."""
-    def __init__(self, x, up, down, rows, weights):
+    def __init__(self, x, up, down, rows, weights, E):
         self.x, self.up, self.down, self.rows, self.weights = x, up, down, rows, weights
         lead = () if rows is None else (up.shape[0],)
         H, I = down.shape[-2], down.shape[-1]
@@ -146,7 +146,7 @@ class _Block:
         if rows is not None:
             k = _int32("k", rows[2].shape[1])
             _dense(weights, "weights", (self.T, k), torch.float32, x.device)
-            self.arg = Rows(*(t.data_ptr() for t in rows), weights.data_ptr(), k)
+            self.arg = Rows(*(t.data_ptr() for t in rows), weights.data_ptr(), k, E)
         need = _size(0), _size(0), _size(0)
         _check(_lib.topoep_ffn_bytes(self.ffn, self.T, self.arg, *need), "topoep_ffn_bytes")
         self.forward_bytes, self.saved_bytes, self.backward_bytes = (n.value for n in need)
@@ -178,8 +178,9 @@ class _Block:
 
 class _FeedForward(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weights, up, down, rows):
-        out, saved = _Block(x, up, down, rows, weights).forward(True)
+    def forward(ctx, x, weights, up, down, rows, E):
+        out, saved = _Block(x, up, down, rows, weights, E).forward(True)
+        ctx.num_experts = E
         ctx.save_for_backward(x, weights, up, down, saved, *(rows or ()))
         return out
 
@@ -187,17 +188,17 @@ class _FeedForward(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
         x, weights, up, down, saved, *rows = ctx.saved_tensors
-        block = _Block(x, up, down, tuple(rows) or None, weights)
+        block = _Block(x, up, down, tuple(rows) or None, weights, ctx.num_experts)
         grad = grad.contiguous()
         if grad.data_ptr() % 16:
             grad = grad.clone()
-        return (*block.backward(saved, grad, ctx.needs_input_grad[:4]), None)
+        return (*block.backward(saved, grad, ctx.needs_input_grad[:4]), None, None)
 
 
-def _run(x, weights, up, down, rows):
+def _run(x, weights, up, down, rows, E):
     if _watched(x, weights, up, down):
-        return _FeedForward.apply(x, weights, up, down, rows)
-    return _Block(x, up, down, rows, weights).forward(False)[0]
+        return _FeedForward.apply(x, weights, up, down, rows, E)
+    return _Block(x, up, down, rows, weights, E).forward(False)[0]
 
 
 def feed_forward(x, up, down, stream=None):
@@ -208,7 +209,7 @@ def feed_forward(x, up, down, stream=None):
     if stream is not None:
         return _on_stream(stream, feed_forward, x, up, down)
     _stream_of(_tensor(x, "x", 2).device)
-    return _run(x, None, _tensor(up, "up", 2), _tensor(down, "down", 2), None)
+    return _run(x, None, _tensor(up, "up", 2), _tensor(down, "down", 2), None, 1)
 
 
 def experts(x, ids, weights, up, down, expert_slot=None, stream=None):
@@ -225,7 +226,8 @@ def experts(x, ids, weights, up, down, expert_slot=None, stream=None):
     if _tensor(ids, "ids", 2).shape[0] != x.shape[0] or ids.device != x.device:
         raise ValueError("ids must have a row for each of x, on its GPU")
     rows = expert_rows(ids, up.shape[0], expert_slot)
-    return _run(x, weights, up, down, rows)
+    E = up.shape[0] if expert_slot is None else expert_slot.shape[0]
+    return _run(x, weights, up, down, rows, max(E, 1))
 
 
 # ---------------------------------------------------------------- 8-bit integers

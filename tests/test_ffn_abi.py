@@ -29,7 +29,7 @@ def test_library_exports_every_declared_symbol(ffn):
 
 def test_struct_layout_matches_header(ffn):
     assert ctypes.sizeof(ffn.Ffn) == 16
-    assert ctypes.sizeof(ffn.Rows) == 40 and ffn.Rows.topk.offset == 32
+    assert ctypes.sizeof(ffn.Rows) == 40 and ffn.Rows.num_experts.offset == 36
     assert ctypes.sizeof(ffn.Int8) == 20
 
 
@@ -58,7 +58,7 @@ def test_rows_refusals(ffn):
 def test_block_refusals(ffn):
     N, F, B = ffn._lib.topoep_ffn_bytes, ffn._lib.topoep_ffn_forward, ffn._lib.topoep_ffn_backward
     f = ffn.Ffn(64, 32, 4, 1)
-    rows = ffn.Rows(256, 512, 1024, 2048, 2)
+    rows = ffn.Rows(256, 512, 1024, 2048, 2, 8)
     need = [ctypes.c_size_t(0) for _ in range(3)]
     assert N(f, 8, rows, *need) == OK and all(n.value % 256 == 0 and n.value > 0 for n in need)
     assert N(f, 8, rows, None, None, None) == OK
@@ -67,9 +67,10 @@ def test_block_refusals(ffn):
         assert N(ffn.Ffn(*bad), 8, rows, *need) == EINVAL, bad
     assert N(None, 8, rows, *need) == EINVAL and N(f, -1, rows, *need) == EINVAL
     assert N(f, 8, None, *need) == EINVAL                     # four blocks, no rows
-    assert N(f, 8, ffn.Rows(256, 512, 1024, 2048, 0), *need) == EINVAL
+    assert N(f, 8, ffn.Rows(256, 512, 1024, 2048, 0, 8), *need) == EINVAL
     assert N(f, 1 << 30, rows, *need) == EINVAL
-    assert N(f, 8, ffn.Rows(256, 512, 1024, 2048, 65), *need) == ELIMIT
+    assert N(f, 8, ffn.Rows(256, 512, 1024, 2048, 2, 0), *need) == EINVAL
+    assert N(f, 8, ffn.Rows(256, 512, 1024, 2048, 65, 128), *need) == ELIMIT
     assert N(ffn.Ffn(64, 32, 1025, 1), 8, rows, *need) == ELIMIT
     assert N(f, 8, rows, *need) == OK
     fw, saved, bw = (n.value for n in need)
@@ -85,7 +86,7 @@ def test_block_refusals(ffn):
     for i in range(4):
         fields = [256, 512, 1024, 2048]
         fields[i] = None
-        assert forward(rows=ffn.Rows(*fields, 2)) == EINVAL, i
+        assert forward(rows=ffn.Rows(*fields, 2, 8)) == EINVAL, i
     assert forward(ldx=56) == EINVAL and forward(ldx=68) == EINVAL and forward(ldx=1 << 60) == EINVAL
     assert forward(size=fw - 1) == EWORKSPACE and forward(ws=8192 + 128) == EWORKSPACE
     assert forward(T=0, x=None, ws=None) == OK
