@@ -19,6 +19,7 @@
 // Which tiles there are depends on the experts' rows, which the host does not know:
 // every workgroup counts them from the offsets and takes tiles by its number.
 #include "fastdiv.h"
+#include "few.h"
 #include "spans.h"
 #include "tile.h"
 #include "topoep_ffn.h"
@@ -145,6 +146,54 @@ __global__ __launch_bounds__(S::kThreads, 2) void out_kernel(Ffn a, void *to) {
         else store4<T>(to, (int64_t)m * a.H + c, d[i][j]);
       }
     }
+  }
+}
+
+// A few rows an expert: up and down for 16 rows of weights and up to 4 C of a group at a time.
+template <class T, bool Save, int C, int KS>
+__global__ __launch_bounds__(64 * few_waves(KS), few_per_simd(C)) void few_up_kernel(Ffn a) {
+  __shared__ FewSums<float, C, KS> lds;
+  const int np = (a.I + 7) / 8;
+  Span s;
+  const int nq = spans<4 * C>(a.offsets, a.rows, a.L, -1, s);
+  for (int t = few_first<KS>(); t < nq * np; t += few_next<KS>()) {
+    const int tp = t / nq, unit0 = tp * 8;
+    spans<4 * C>(a.offsets, a.rows, a.L, t - tp * nq, s);
+    const char *w = static_cast<const char *>(a.up) + (int64_t)s.group * 4 * a.I * a.H;
+    few_product<T, C, KS>(
+        [&](int r) { return w + (int64_t)((r >> 3) * a.I + imin(unit0 + (r & 7), a.I - 1)) * a.H * 2; },
+        [&](int c) { return static_cast<const char *>(a.x) + token_of(a, s.first + c) * a.ldx * 2; },
+        imin(s.end - s.first, 4 * C), a.H * 2, lds, 8, [&](int u, int c, float g, float up) {
+          if (unit0 + u >= a.I) return;
+          const int m = s.first + c;
+          static_cast<T *>(a.h)[(int64_t)m * a.I + unit0 + u] = from_float<T>(weight_of(a, m) * (g * sigmoid(g) * up));
+          if (Save) {
+            float *to = a.gu + (int64_t)m * 2 * a.I + unit0 + u;
+            to[0] = g;
+            to[a.I] = up;
+          }
+        });
+  }
+}
+
+template <class T, int C, int KS>
+__global__ __launch_bounds__(64 * few_waves(KS), few_per_simd(C)) void few_down_kernel(Ffn a, void *to) {
+  __shared__ FewSums<float, C, KS> lds;
+  const int np = (a.H + kFewRows - 1) / kFewRows;
+  Span s;
+  const int nq = spans<4 * C>(a.offsets, a.rows, a.L, -1, s);
+  for (int t = few_first<KS>(); t < nq * np; t += few_next<KS>()) {
+    const int tp = t / nq, h0 = tp * kFewRows;
+    spans<4 * C>(a.offsets, a.rows, a.L, t - tp * nq, s);
+    const char *w = static_cast<const char *>(a.down) + (int64_t)s.group * 2 * a.I * a.H;
+    few_product<T, C, KS>([&](int r) { return w + (int64_t)imin(h0 + r, a.H - 1) * a.I * 2; },
+                          [&](int c) { return static_cast<const char *>(a.h) + (int64_t)(s.first + c) * a.I * 2; },
+                          imin(s.end - s.first, 4 * C), a.I * 2, lds, 16, [&](int r, int c, float v, float) {
+                            if (h0 + r >= a.H) return;
+                            const int64_t at = (int64_t)(s.first + c) * a.H + h0 + r;
+                            if (a.pairs) static_cast<float *>(to)[at] = v;
+                            else static_cast<T *>(to)[at] = from_float<T>(v);
+                          });
   }
 }
 
@@ -357,7 +406,7 @@ Ffn args_of(const topoep_ffn *f, const void *x, int64_t ldx, int32_t T, const to
   a.x = x, a.ldx = ldx, a.up = up, a.down = down;
   a.k = rows ? rows->topk : 1;
   a.rows = T * a.k;
-  a.expected = rows ? (int64_t)a.rows * imin(a.L, rows->num_experts) / rows->num_experts : a.rows;
+  a.expected = rows ? ((int64_t)a.rows * imin(a.L, rows->num_experts) + rows->num_experts - 1) / rows->num_experts : a.rows;
   a.per_token = make_fastdiv((uint32_t)a.k);
   if (rows) a.offsets = rows->offsets, a.pairs = rows->pairs, a.places = rows->places, a.weights = rows->weights;
   return a;
@@ -435,11 +484,37 @@ int enqueue_grad(const Ffn &a, hipStream_t st) {
                                              : enqueue_grad_of<SmallGrad<T>, Down>(a, tiles(128), st);
 }
 
+// A few rows a group (16 and fewer): the weights' bytes count, not the tiles.
+bool few_rows(const Ffn &a) { return a.expected <= 16 * (int64_t)a.L; }
+
+template <class T>
+int enqueue_few(const Ffn &a, hipStream_t st) {
+  const int64_t groups = imin(a.L, (int)a.expected), each = (a.expected + groups - 1) / groups;
+  const int64_t nu = (a.I + 7) / 8, nh = (a.H + kFewRows - 1) / kFewRows;
+  few_shape(each, groups * nu, [&](auto c, auto ks) {
+    constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
+    const dim3 grid = few_grid<KS>(most_spans<4 * C>(a.offsets, a.rows, a.L) * nu), block(64 * few_waves(KS));
+    if (a.gu) hipLaunchKernelGGL((few_up_kernel<T, true, C, KS>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((few_up_kernel<T, false, C, KS>), grid, block, 0, st, a);
+  });
+  if (!launched()) return TOPOEP_EHIP;
+  few_shape(each, groups * nh, [&](auto c, auto ks) {
+    constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
+    const dim3 grid = few_grid<KS>(most_spans<4 * C>(a.offsets, a.rows, a.L) * nh), block(64 * few_waves(KS));
+    hipLaunchKernelGGL((few_down_kernel<T, C, KS>), grid, block, 0, st, a, a.pairs ? static_cast<void *>(a.y) : a.out);
+  });
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+
 template <class T>
 int forward(const Ffn &a, hipStream_t st) {
-  int rc = enqueue_up<T>(a, st);
-  if (rc != TOPOEP_OK) return rc;
-  rc = enqueue_out<T, false>(a, a.pairs ? static_cast<void *>(a.y) : a.out, st);
+  int rc;
+  if (few_rows(a)) {
+    rc = enqueue_few<T>(a, st);
+  } else {
+    rc = enqueue_up<T>(a, st);
+    if (rc == TOPOEP_OK) rc = enqueue_out<T, false>(a, a.pairs ? static_cast<void *>(a.y) : a.out, st);
+  }
   if (rc != TOPOEP_OK || !a.pairs) return rc;
   return enqueue_combine<T>(a, a.out, st);
 }

@@ -4,9 +4,9 @@
 //
 // The sums are whole numbers, exact in 32 bits; scales (and the activation of a gated
 // block) are the epilogue, in 32 bits, rounded once.
-#include "tile.h"
-#include "topoep_ffn.h"
+#include "few.h"
 #include "spans.h"
+#include "topoep_ffn.h"
 
 namespace {
 
@@ -216,6 +216,33 @@ __global__ __launch_bounds__(S::kThreads, 2) void int8_kernel(Int8 a) {
   }
 }
 
+// A few rows a group: 16 rows of weights (8 columns' gate and up rows) against up to 4 C rows.
+template <bool Gated, int C, int KS>
+__global__ __launch_bounds__(64 * few_waves(KS), few_per_simd(C)) void few_int8_kernel(Int8 a) {
+  __shared__ FewSums<int, C, KS> lds;
+  constexpr int kCols = Gated ? 8 : 16;
+  const int np = (a.No + kCols - 1) / kCols;
+  clear_rest(a);
+  Span s;
+  const int nq = spans<4 * C>(a.offsets, a.M, a.G, -1, s);
+  for (int t = few_first<KS>(); t < nq * np; t += few_next<KS>()) {
+    const int tp = t / nq, c0 = tp * kCols;
+    spans<4 * C>(a.offsets, a.M, a.G, t - tp * nq, s);
+    const char *w = reinterpret_cast<const char *>(a.w) + (int64_t)s.group * a.N * a.K;
+    few_product<I8, C, KS>(
+        [&](int r) { return w + (int64_t)((Gated ? r >> 3 : 0) * a.No + imin(c0 + r % kCols, a.No - 1)) * a.K; },
+        [&](int c) { return reinterpret_cast<const char *>(a.q) + (s.first + c) * a.ldq; },
+        imin(s.end - s.first, 4 * C), a.K, lds, kCols, [&](int r, int c, int first, int second) {
+          if (c0 + r >= a.No) return;
+          const float *ws = a.ws + (int64_t)s.group * a.N + c0 + r;
+          const float scale = a.scale[s.first + c];
+          float v = (float)first * scale * ws[0];
+          if (Gated) v = v * sigmoid(v) * ((float)second * scale * ws[a.No]);
+          store1(a.out, a.type, (int64_t)(s.first + c) * a.No + c0 + r, v);
+        });
+  }
+}
+
 // ---------------------------------------------------------------- host
 
 bool launched() { return hipGetLastError() == hipSuccess; }
@@ -289,6 +316,18 @@ int topoep_matmul_int8(const topoep_int8 *p, const int8_t *q, int64_t ldq, const
   a.out = out, a.type = p->out_dtype, a.keep = keep_rest != 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
+  // a few rows a group (16 and fewer): the weights' bytes count, not the tiles
+  const int64_t groups = imin(a.G, M);
+  if (M <= 16 * groups) {
+    const int64_t np = (a.No + (p->gated ? 7 : 15)) / (p->gated ? 8 : 16);
+    few_shape((M + groups - 1) / groups, groups * np, [&](auto c, auto ks) {
+      constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
+      const dim3 grid = few_grid<KS>(most_spans<4 * C>(offsets, M, a.G) * np), block(64 * few_waves(KS));
+      if (p->gated) hipLaunchKernelGGL((few_int8_kernel<true, C, KS>), grid, block, 0, st, a);
+      else hipLaunchKernelGGL((few_int8_kernel<false, C, KS>), grid, block, 0, st, a);
+    });
+    return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+  }
   const int per = p->gated ? 128 : 256;
   if (large_tiles(likely_spans(offsets, M, a.G, 256) * ((a.No + per - 1) / per),
                   likely_spans(offsets, M, a.G, 128) * ((a.No + per / 2 - 1) / (per / 2))))
