@@ -1,9 +1,9 @@
 // The rows of a routed layer by expert: a stable counting sort of the router's
 // choices on gfx950.
 //
-// A workgroup ranks a chunk of 8192 pairs: its waves take 512 neighbours each, 64
-// at a time, whose ranks among equals come from ballots and a row of counts a
-// wave in LDS; the rows of counts are then summed in the order of the waves. One chunk
+// A workgroup ranks a chunk of 1024 to 8192 pairs: its waves take equal shares of
+// neighbours, 64 at a time, whose ranks among equals come from ballots and a row of counts a
+// wave in LDS; the rows of counts are then summed in the order of the waves.  One chunk
 // is one launch; more are three (ranks, sums over the chunks, places).  Nothing
 // here is decided by the order in which anything runs.
 //
@@ -17,14 +17,14 @@ namespace {
 
 using namespace topoep_dev;
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kRounds = 8, kChunk = kThreads * kRounds;
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kRounds = 8;
 
 struct Rows {
   const int32_t *ids, *slot;
   int E, L, n, bits;
   int32_t *offsets, *pairs, *places;
   int32_t *counts;   // [chunks, L]
-  int chunks;
+  int chunks, rounds;   // a chunk is kThreads * rounds pairs
 };
 
 // Where pair i's expert is among those here, -1 if nowhere.
@@ -42,11 +42,11 @@ __global__ __launch_bounds__(kThreads) void rank_kernel(Rows a) {
   const int tid = threadIdx.x, wave = uniform_i32(tid >> 6);
   for (int i = tid; i < kWaves * a.L; i += kThreads) lds[i] = 0;
   __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * kChunk + wave * (64 * kRounds) + lane_id();
+  const int64_t first = ((int64_t)blockIdx.x * kWaves + wave) * (64 * a.rounds) + lane_id();
   int *mine = lds + wave * a.L;
   int slot[kRounds], rank[kRounds];
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) slot[r] = first + r * 64 < a.n ? slot_at(a, (int)first + r * 64) : -1;
+  for (int r = 0; r < kRounds; ++r) slot[r] = r < a.rounds && first + r * 64 < a.n ? slot_at(a, (int)first + r * 64) : -1;
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
     rank[r] = 0;
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kThreads) void rank_kernel(Rows a) {
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
     const int64_t i = first + r * 64;
-    if (i >= a.n) continue;
+    if (r >= a.rounds || i >= a.n) continue;
     const int at = slot[r] < 0 ? -1 : mine[slot[r]] + rank[r] + (One ? totals[slot[r]] : 0);
     a.places[i] = at;   // (more chunks than one: in the chunk)
     if (One) {
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(256) void place_kernel(Rows a) {
   if (i >= a.n) return;
   const int s = slot_at(a, (int)i);
   if (s >= 0) {
-    const int at = a.places[i] + a.counts[i / kChunk * a.L + s];
+    const int at = a.places[i] + a.counts[i / (kThreads * a.rounds) * a.L + s];
     a.places[i] = at;
     a.pairs[at] = (int)i;
   }
@@ -137,9 +137,21 @@ int check(int32_t T, int32_t k, int32_t L) {
   return L > TOPOEP_FFN_MAX_EXPERTS ? TOPOEP_ELIMIT : TOPOEP_OK;
 }
 
-int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+// Rounds of a chunk's waves: one chunk where eight do, else as few as leave the sums' one workgroup
+// no more than 64 chunks.
+constexpr int kChunks = 64;
+int rounds_of(int64_t n) {
+  const int64_t one = (n + kThreads - 1) / kThreads;
+  if (one <= kRounds) return (int)one;
+  const int64_t r = (one + kChunks - 1) / kChunks;
+  return (int)(r < kRounds ? r : kRounds);
+}
 
-size_t need(int32_t T, int32_t k, int32_t L) { return align256((size_t)chunks_of((int64_t)T * k) * L * sizeof(int32_t)); }
+// (enough for fewer pairs too, which may have more chunks)
+size_t need(int32_t T, int32_t k, int32_t L) {
+  const int64_t one = ((int64_t)T * k + kThreads - 1) / kThreads, most = (one + kRounds - 1) / kRounds;
+  return align256((size_t)(one < kChunks ? one : most < kChunks ? kChunks : most) * L * sizeof(int32_t));
+}
 
 bool launched() { return hipGetLastError() == hipSuccess; }
 
@@ -175,7 +187,8 @@ int topoep_expert_rows(const int32_t *ids, int32_t T, int32_t k, const int32_t *
   a.pairs = pairs;
   a.places = places;
   a.counts = static_cast<int32_t *>(workspace);
-  a.chunks = (int)chunks_of(a.n);
+  a.rounds = rounds_of(a.n);
+  a.chunks = a.n == 0 ? 0 : (int)(((int64_t)a.n + kThreads * a.rounds - 1) / (kThreads * a.rounds));
   const size_t lds = ((size_t)(kWaves + 1) * L + kWaves + 1) * sizeof(int);
   if (lds > 64 * 1024) {
     const int most = ((kWaves + 1) * TOPOEP_FFN_MAX_EXPERTS + kWaves + 1) * (int)sizeof(int);
