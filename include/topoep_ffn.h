@@ -158,7 +158,7 @@ typedef struct topoep_int8 {
   int32_t out_dtype;
 } topoep_int8;
 
-/* Bytes of device workspace topoep_matmul_int8 needs for M rows or fewer. */
+/* Bytes of device workspace topoep_matmul_int8 needs for M rows (0: none). */
 int topoep_matmul_int8_workspace_bytes(const topoep_int8 *p, int32_t M, size_t *bytes_out);
 
 /*

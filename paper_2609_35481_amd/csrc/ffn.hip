@@ -41,13 +41,14 @@ struct Ffn {
   void *out;
   float *gu;                  // [rows, 2, I]
   void *h;                    // [rows, I]
-  float *y;                   // [rows, H]
+  float *y;                   // [parts, rows, H]
   const void *dout;           // [T, H]
   void *da;                   // [rows, 2I]
   float *part;                // [tiles of I, rows]
   void *dx;
   float *dw;
   void *dup, *ddown;
+  float *sums;                // [parts, L, .., ..]: of a weights' gradient
 };
 
 __device__ inline int token_of(const Ffn &a, int row) {
@@ -109,31 +110,34 @@ __global__ __launch_bounds__(S::kThreads, 2) void up_kernel(Ffn a) {
   }
 }
 
-// y = down h (Back false), dx = up^T da (Back true): to `to`, of T where dense, else 32 bits.
+// y = down h (Back false), dx = up^T da (Back true): to `to`, of T where dense and whole, else 32 bits.
+// `parts` workgroups share a tile's inner axis where there are few tiles, each with sums of its own in `to`.
 template <class S, bool Back>
-__global__ __launch_bounds__(S::kThreads, 2) void out_kernel(Ffn a, void *to) {
+__global__ __launch_bounds__(S::kThreads, 2) void out_kernel(Ffn a, void *to, int parts) {
   typedef typename S::T T;
   TOPOEP_STAGES(S);
   const int np = (a.H + S::BP - 1) / S::BP;
-  const int n = Back ? 2 * a.I : a.I;
+  const int n = Back ? 2 * a.I : a.I, each = ((n + parts - 1) / parts + S::kStage - 1) / S::kStage * S::kStage;
   Span s;
   const int nq = spans<S::BQ>(a.offsets, a.rows, a.L, -1, s);
-  for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
+  for (int u = blockIdx.x; u < nq * np * parts; u += gridDim.x) {
     const Me me;
+    const int part = u / (nq * np), k0 = imin(part * each, n);
     int tq, tp;
-    place_of(t, nq, np, tq, tp);
+    place_of(u - part * nq * np, nq, np, tq, tp);
     spans<S::BQ>(a.offsets, a.rows, a.L, tq, s);
     typename std::conditional<Back, Across<T, S::BP, S::kWaves>, ByRows<T, S::BP, S::kWaves>>::type p;
     ByRows<T, S::BQ, S::kWaves> q;
-    const char *w = static_cast<const char *>(Back ? a.up : a.down) + (int64_t)s.group * n * a.H * 2;
-    if constexpr (Back) p.start(me, w, a.H, tp * S::BP, a.H);
-    else p.start(me, [&](int r) { return w + (int64_t)imin(tp * S::BP + r, a.H - 1) * n * 2; });
-    q.start(me, [&](int r) {
-      return static_cast<const char *>(Back ? a.da : a.h) + (int64_t)imin(s.first + r, s.end - 1) * n * 2;
-    });
+    const T *w = static_cast<const T *>(Back ? a.up : a.down) + (int64_t)s.group * n * a.H;
+    if constexpr (Back) p.start(me, w + (int64_t)k0 * a.H, a.H, tp * S::BP, a.H);
+    else p.start(me, [&](int r) { return reinterpret_cast<const char *>(w + (int64_t)imin(tp * S::BP + r, a.H - 1) * n + k0); });
+    const T *rows = static_cast<const T *>(Back ? a.da : a.h) + k0;
+    q.start(me, [&](int r) { return reinterpret_cast<const char *>(rows + (int64_t)imin(s.first + r, s.end - 1) * n); });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, me, n, p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, imin(each, n - k0), p0, p1, q0, q1, d);
+    const bool whole = !a.pairs && parts == 1;
+    const int64_t at = (int64_t)part * a.rows * a.H;
 #pragma unroll
     for (int j = 0; j < S::TQ; ++j) {
       const int m = s.first + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
@@ -142,8 +146,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void out_kernel(Ffn a, void *to) {
       for (int i = 0; i < S::TP; ++i) {
         const int c = tp * S::BP + (me.wave % S::NP * S::TP + i) * 16 + (me.lane >> 4) * 4;
         if (c >= a.H) continue;
-        if (a.pairs) *reinterpret_cast<v4f *>(static_cast<float *>(to) + (int64_t)m * a.H + c) = d[i][j];
-        else store4<T>(to, (int64_t)m * a.H + c, d[i][j]);
+        if (whole) store4<T>(to, (int64_t)m * a.H + c, d[i][j]);
+        else *reinterpret_cast<v4f *>(static_cast<float *>(to) + at + (int64_t)m * a.H + c) = d[i][j];
       }
     }
   }
@@ -197,17 +201,22 @@ __global__ __launch_bounds__(64 * few_waves(KS), few_per_simd(C)) void few_down_
   }
 }
 
-// out_t = the sum of its rows of `from`, in the order of its choices.
+// out_t = the sum of its rows of `from`, in the order of its choices (dense: its row), each the sum
+// of its parts.  A workgroup has a token and 1024 columns of it.
 template <class T>
-__global__ __launch_bounds__(256) void combine_kernel(Ffn a, const float *from, void *to) {
-  const int groups = a.H / 4;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)a.T * groups; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = i / groups;
-    const int c = (int)(i - t * groups) * 4;
-    v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int j = 0; j < a.k; ++j) {
-      const int m = a.places[t * a.k + j];
-      if ((unsigned)m < (unsigned)a.rows) s += *reinterpret_cast<const v4f *>(from + (int64_t)m * a.H + c);
+__global__ __launch_bounds__(256) void combine_kernel(Ffn a, const float *from, void *to, int parts) {
+  const int64_t t = blockIdx.x;
+  const int c = (blockIdx.y * 256 + threadIdx.x) * 4;
+  int place = -1;
+  if (lane_id() < a.k) place = a.pairs ? a.places[t * a.k + lane_id()] : (int)t;
+  uint64_t here = __ballot((unsigned)place < (unsigned)a.rows);
+  v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (c < a.H) {
+    for (; here != 0; here &= here - 1) {
+      const int64_t m = readlane_i32(place, __ffsll((unsigned long long)here) - 1);
+      v4f row = *reinterpret_cast<const v4f *>(from + m * a.H + c);
+      for (int p = 1; p < parts; ++p) row += *reinterpret_cast<const v4f *>(from + ((int64_t)p * a.rows + m) * a.H + c);
+      s += row;
     }
     store4<T>(to, t * a.H + c, s);
   }
@@ -320,19 +329,22 @@ struct Tokens : AcrossPlaces<B, W> {
 };
 
 // dup[g][r][c] = sum over the group's rows of da[m][r] x[token][c] (Down false), ddown[g][r][c] of
-// dout[token][r] h[m][c] (Down true).
+// dout[token][r] h[m][c] (Down true).  `parts` workgroups share a group's rows where there are few
+// tiles, each with sums of its own in a.sums.
 template <class S, bool Down>
-__global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a) {
+__global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a, int parts) {
   typedef typename S::T T;
   TOPOEP_STAGES(S);
   const Me me;
   const int cols = Down ? a.I : a.H, rows = Down ? a.H : 2 * a.I;
   const int np = (cols + S::BP - 1) / S::BP, nq = (rows + S::BQ - 1) / S::BQ;
-  const int g = blockIdx.x / (np * nq);
+  const int part = blockIdx.x / (np * nq) % parts, g = blockIdx.x / (np * nq) / parts;
   int tq, tp, first, end;
   place_of(blockIdx.x % (np * nq), nq, np, tq, tp);
   rows_of(a.offsets, a.rows, g, first, end);
-  const int n = end - first;
+  const int each = ((end - first + parts - 1) / parts + S::kStage - 1) / S::kStage * S::kStage;
+  first = imin(first + part * each, end);
+  const int n = imin(each, end - first);
   typename S::Sum d[S::TP][S::TQ] = {};
   const auto run = [&](auto &p, auto &q) { multiply<S>(p, q, me, n, p0, p1, q0, q1, d); };
   if constexpr (Down) {
@@ -348,6 +360,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a) {
     q.start(me, static_cast<const T *>(a.da) + (int64_t)first * 2 * a.I, 2 * a.I, tq * S::BQ, 2 * a.I);
     run(p, q);
   }
+  void *const to = Down ? a.ddown : a.dup;
+  const int64_t at = ((int64_t)part * a.L + g) * rows;
 #pragma unroll
   for (int j = 0; j < S::TQ; ++j) {
     const int r = tq * S::BQ + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
@@ -355,8 +369,20 @@ __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a) {
 #pragma unroll
     for (int i = 0; i < S::TP; ++i) {
       const int c = tp * S::BP + (me.wave % S::NP * S::TP + i) * 16 + (me.lane >> 4) * 4;
-      if (c < cols) store4<T>(Down ? a.ddown : a.dup, ((int64_t)g * rows + r) * cols + c, d[i][j]);
+      if (c >= cols) continue;
+      if (parts == 1) store4<T>(to, (at + r) * cols + c, d[i][j]);
+      else *reinterpret_cast<v4f *>(a.sums + (at + r) * cols + c) = d[i][j];
     }
+  }
+}
+
+// n values, each the sum of its parts in order.
+template <class T>
+__global__ __launch_bounds__(256) void parts_kernel(const float *from, void *to, int64_t n, int parts) {
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * 1024) {
+    v4f s = *reinterpret_cast<const v4f *>(from + i);
+    for (int p = 1; p < parts; ++p) s += *reinterpret_cast<const v4f *>(from + p * n + i);
+    store4<T>(to, i, s);
   }
 }
 
@@ -368,23 +394,46 @@ bool launched() { return hipGetLastError() == hipSuccess; }
 
 constexpr int kPartUnits = 128;   // units of a part of the weights' gradient, at least: the hidden kernel's BP
 
+// Rows of the experts that are here, at most and about.
+struct Counts { int64_t rows, expected; };
+Counts counts_of(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *r) {
+  if (!r) return Counts{T, T};
+  const int64_t rows = (int64_t)T * r->topk;
+  return Counts{rows, ceil_of(rows * imin(f->experts, r->num_experts), r->num_experts)};
+}
+
+// Of the products by rows with H columns (their sums are at most 256 MiB), n of the inner axis.
+int out_parts(const topoep_ffn *f, const Counts &c, const topoep_ffn_rows *r, int n) {
+  const int64_t tiles = likely_spans(r != nullptr, c.expected, f->experts, 128) * ceil_of(f->hidden, 128);
+  const int p = parts_of(tiles, n / 64, 8);
+  return c.rows * f->hidden * p > (int64_t)1 << 26 ? 1 : p;
+}
+// Of a weights' gradient of `rows` by `cols`.
+int grad_parts(const topoep_ffn *f, const Counts &c, int rows, int cols) {
+  return parts_of(f->experts * ceil_of(rows, 128) * ceil_of(cols, 128), c.expected / f->experts / 64, 16);
+}
+
 struct Sizes {
-  int64_t rows;
-  size_t gu, h, y, da, part, saved, forward, backward;
+  size_t gu, h, y, back, da, part, sums, saved, forward, backward;
 };
 
-Sizes sizes_of(const topoep_ffn *f, int32_t T, int topk) {
+Sizes sizes_of(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *r) {
   Sizes s;
-  s.rows = (int64_t)T * (topk ? topk : 1);
-  const size_t n = (size_t)s.rows, H = (size_t)f->hidden, I = (size_t)f->inter;
+  const Counts c = counts_of(f, T, r);
+  const size_t n = (size_t)c.rows, H = (size_t)f->hidden, I = (size_t)f->inter;
+  const int down = out_parts(f, c, r, f->inter), up = out_parts(f, c, r, 2 * f->inter);
+  const int pu = grad_parts(f, c, 2 * f->inter, f->hidden), pd = grad_parts(f, c, f->hidden, f->inter);
   s.gu = align256(n * 2 * I * sizeof(float));
   s.h = align256(n * I * 2);
-  s.y = topk ? align256(n * H * sizeof(float)) : 0;
+  s.y = r || down > 1 ? align256(down * n * H * sizeof(float)) : 0;
+  s.back = r || up > 1 ? align256(up * n * H * sizeof(float)) : 0;
   s.da = align256(n * 2 * I * 2);
-  s.part = topk ? align256((I + kPartUnits - 1) / kPartUnits * n * sizeof(float)) : 0;
+  s.part = r ? align256((I + kPartUnits - 1) / kPartUnits * n * sizeof(float)) : 0;
+  const size_t su = pu > 1 ? (size_t)pu * f->experts * 2 * I * H : 0, sd = pd > 1 ? (size_t)pd * f->experts * I * H : 0;
+  s.sums = align256((su > sd ? su : sd) * sizeof(float));
   s.saved = s.gu + s.h;
   s.forward = s.h + s.y;   // (h where nothing is saved)
-  s.backward = s.da + s.y + s.part;
+  s.backward = s.da + s.back + s.part + s.sums;
   return s;
 }
 
@@ -406,7 +455,7 @@ Ffn args_of(const topoep_ffn *f, const void *x, int64_t ldx, int32_t T, const to
   a.x = x, a.ldx = ldx, a.up = up, a.down = down;
   a.k = rows ? rows->topk : 1;
   a.rows = T * a.k;
-  a.expected = rows ? ((int64_t)a.rows * imin(a.L, rows->num_experts) + rows->num_experts - 1) / rows->num_experts : a.rows;
+  a.expected = counts_of(f, T, rows).expected;
   a.per_token = make_fastdiv((uint32_t)a.k);
   if (rows) a.offsets = rows->offsets, a.pairs = rows->pairs, a.places = rows->places, a.weights = rows->weights;
   return a;
@@ -419,8 +468,8 @@ template <class T> using SmallGrad = Shape<T, 128, 128, 2, 2, true, true, 4>;
 
 // Whether a product by rows with `cols` columns of out takes large tiles (`per`: columns of a tile of 256).
 bool large_rows(const Ffn &a, int cols, int per) {
-  return large_tiles(likely_spans(a.offsets, a.expected, a.L, 256) * ((cols + per - 1) / per),
-                     likely_spans(a.offsets, a.expected, a.L, 128) * ((cols + per / 2 - 1) / (per / 2)));
+  return large_tiles(likely_spans(a.offsets != nullptr, a.expected, a.L, 256) * ((cols + per - 1) / per),
+                     likely_spans(a.offsets != nullptr, a.expected, a.L, 128) * ((cols + per / 2 - 1) / (per / 2)));
 }
 
 template <class S, bool Save>
@@ -437,15 +486,22 @@ int enqueue_up(const Ffn &a, hipStream_t st) {
 }
 
 template <class S, bool Back>
-int enqueue_out_of(const Ffn &a, void *to, hipStream_t st) {
-  const int64_t tiles = most_spans<S::BQ>(a.offsets, a.rows, a.L) * ((a.H + S::BP - 1) / S::BP);
-  hipLaunchKernelGGL((out_kernel<S, Back>), dim3(grid_of<S>(tiles)), dim3(S::kThreads), 0, st, a, to);
+int enqueue_out_of(const Ffn &a, void *to, int parts, hipStream_t st) {
+  const int64_t tiles = most_spans<S::BQ>(a.offsets, a.rows, a.L) * ((a.H + S::BP - 1) / S::BP) * parts;
+  hipLaunchKernelGGL((out_kernel<S, Back>), dim3(grid_of<S>(tiles)), dim3(S::kThreads), 0, st, a, to, parts);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+template <class T>
+int enqueue_combine(const Ffn &a, void *to, int parts, hipStream_t st) {
+  hipLaunchKernelGGL((combine_kernel<T>), dim3(a.T, (a.H + 1023) / 1024), dim3(256), 0, st, a, a.y, to, parts);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 template <class T, bool Back>
-int enqueue_out(const Ffn &a, void *to, hipStream_t st) {
-  return large_rows(a, a.H, 256) ? enqueue_out_of<Large<T, Back>, Back>(a, to, st)
-                                 : enqueue_out_of<Small<T, Back>, Back>(a, to, st);
+int enqueue_out(const Ffn &a, void *to, int parts, hipStream_t st) {
+  void *const product = a.pairs || parts > 1 ? static_cast<void *>(a.y) : to;
+  const int rc = parts == 1 && large_rows(a, a.H, 256) ? enqueue_out_of<Large<T, Back>, Back>(a, product, 1, st)
+                                                       : enqueue_out_of<Small<T, Back>, Back>(a, product, parts, st);
+  return rc != TOPOEP_OK || product == to ? rc : enqueue_combine<T>(a, to, parts, st);
 }
 
 template <class S>
@@ -464,71 +520,69 @@ int enqueue_hidden(const Ffn &a, hipStream_t st) {
   return large_rows(a, a.I, 256) ? enqueue_hidden_of<Large<T, true>>(a, st) : enqueue_hidden_of<Small<T, true>>(a, st);
 }
 
-template <class T>
-int enqueue_combine(const Ffn &a, void *to, hipStream_t st) {
-  const int64_t blocks = ((int64_t)a.T * (a.H / 4) + 255) / 256;
-  hipLaunchKernelGGL((combine_kernel<T>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, st, a, a.y, to);
-  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
-}
-
 template <class S, bool Down>
-int enqueue_grad_of(const Ffn &a, int64_t tiles, hipStream_t st) {
-  hipLaunchKernelGGL((grad_kernel<S, Down>), dim3((unsigned)tiles), dim3(S::kThreads), 0, st, a);
+int enqueue_grad_of(const Ffn &a, int64_t tiles, int parts, hipStream_t st) {
+  hipLaunchKernelGGL((grad_kernel<S, Down>), dim3((unsigned)(tiles * parts)), dim3(S::kThreads), 0, st, a, parts);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 template <class T, bool Down>
-int enqueue_grad(const Ffn &a, hipStream_t st) {
+int enqueue_grad(const Ffn &a, int parts, hipStream_t st) {
   const int cols = Down ? a.I : a.H, rows = Down ? a.H : 2 * a.I;
   const auto tiles = [&](int64_t n) { return a.L * ((cols + n - 1) / n) * ((rows + n - 1) / n); };
-  return large_tiles(tiles(256), tiles(128)) ? enqueue_grad_of<LargeGrad<T>, Down>(a, tiles(256), st)
-                                             : enqueue_grad_of<SmallGrad<T>, Down>(a, tiles(128), st);
+  if (parts == 1 && large_tiles(tiles(256), tiles(128))) return enqueue_grad_of<LargeGrad<T>, Down>(a, tiles(256), 1, st);
+  const int rc = enqueue_grad_of<SmallGrad<T>, Down>(a, tiles(128), parts, st);
+  if (rc != TOPOEP_OK || parts == 1) return rc;
+  const int64_t n = (int64_t)a.L * rows * cols, blocks = (n + 1023) / 1024;
+  hipLaunchKernelGGL((parts_kernel<T>), dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, a.sums,
+                     Down ? a.ddown : a.dup, n, parts);
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
-// A few rows a group (16 and fewer): the weights' bytes count, not the tiles.
-bool few_rows(const Ffn &a) { return a.expected <= 16 * (int64_t)a.L; }
+// A few rows a group, 16 and fewer: the weights' bytes count, not the tiles.  Up to 64 also where tiles of
+// 128 x 128 would fill less than half of the chip's places (32 rows, H = 4096, I = 11008: 115 against
+// 196 us; 128 experts of H = 2048, I = 768 with 32 rows: 588 and 278).
+bool few_rows(const Ffn &a, int64_t np) {
+  return a.expected <= 16 * (int64_t)a.L ||
+         (a.expected <= 64 * (int64_t)a.L && likely_spans(a.offsets != nullptr, a.expected, a.L, 128) * np < 256);
+}
 
 template <class T>
-int enqueue_few(const Ffn &a, hipStream_t st) {
-  const int64_t groups = imin(a.L, (int)a.expected), each = (a.expected + groups - 1) / groups;
-  const int64_t nu = (a.I + 7) / 8, nh = (a.H + kFewRows - 1) / kFewRows;
-  few_shape(each, groups * nu, [&](auto c, auto ks) {
+int enqueue_few_up(const Ffn &a, hipStream_t st) {
+  const int64_t groups = imin(a.L, (int)a.expected), nu = (a.I + 7) / 8;
+  few_shape((a.expected + groups - 1) / groups, groups * nu, [&](auto c, auto ks) {
     constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
     const dim3 grid = few_grid<KS>(most_spans<4 * C>(a.offsets, a.rows, a.L) * nu), block(64 * few_waves(KS));
     if (a.gu) hipLaunchKernelGGL((few_up_kernel<T, true, C, KS>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((few_up_kernel<T, false, C, KS>), grid, block, 0, st, a);
   });
-  if (!launched()) return TOPOEP_EHIP;
-  few_shape(each, groups * nh, [&](auto c, auto ks) {
+  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+}
+template <class T>
+int enqueue_few_down(const Ffn &a, hipStream_t st) {
+  const int64_t groups = imin(a.L, (int)a.expected), nh = (a.H + kFewRows - 1) / kFewRows;
+  few_shape((a.expected + groups - 1) / groups, groups * nh, [&](auto c, auto ks) {
     constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
     const dim3 grid = few_grid<KS>(most_spans<4 * C>(a.offsets, a.rows, a.L) * nh), block(64 * few_waves(KS));
     hipLaunchKernelGGL((few_down_kernel<T, C, KS>), grid, block, 0, st, a, a.pairs ? static_cast<void *>(a.y) : a.out);
   });
-  return launched() ? TOPOEP_OK : TOPOEP_EHIP;
+  if (!launched()) return TOPOEP_EHIP;
+  return a.pairs ? enqueue_combine<T>(a, a.out, 1, st) : TOPOEP_OK;
 }
 
 template <class T>
-int forward(const Ffn &a, hipStream_t st) {
-  int rc;
-  if (few_rows(a)) {
-    rc = enqueue_few<T>(a, st);
-  } else {
-    rc = enqueue_up<T>(a, st);
-    if (rc == TOPOEP_OK) rc = enqueue_out<T, false>(a, a.pairs ? static_cast<void *>(a.y) : a.out, st);
-  }
-  if (rc != TOPOEP_OK || !a.pairs) return rc;
-  return enqueue_combine<T>(a, a.out, st);
+int forward(const Ffn &a, int parts, hipStream_t st) {
+  const int rc = few_rows(a, (a.I + 63) / 64) ? enqueue_few_up<T>(a, st) : enqueue_up<T>(a, st);
+  if (rc != TOPOEP_OK) return rc;
+  return few_rows(a, (a.H + 127) / 128) ? enqueue_few_down<T>(a, st) : enqueue_out<T, false>(a, a.out, parts, st);
 }
 
 template <class T>
-int backward(const Ffn &a, hipStream_t st) {
+int backward(const Ffn &a, int parts, int up_parts, int down_parts, hipStream_t st) {
   int rc = TOPOEP_OK;
   if (a.rows > 0 && (a.dx || a.dw || a.dup)) rc = enqueue_hidden<T>(a, st);
-  if (rc == TOPOEP_OK && a.rows > 0 && a.dx) {
-    rc = enqueue_out<T, true>(a, a.pairs ? static_cast<void *>(a.y) : a.dx, st);
-    if (rc == TOPOEP_OK && a.pairs) rc = enqueue_combine<T>(a, a.dx, st);
-  }
-  if (rc == TOPOEP_OK && a.dup) rc = enqueue_grad<T, false>(a, st);
-  if (rc == TOPOEP_OK && a.ddown) rc = enqueue_grad<T, true>(a, st);
+  if (rc == TOPOEP_OK && a.rows > 0 && a.dx) rc = enqueue_out<T, true>(a, a.dx, parts, st);
+  if (rc == TOPOEP_OK && a.dup) rc = enqueue_grad<T, false>(a, up_parts, st);
+  if (rc == TOPOEP_OK && a.ddown) rc = enqueue_grad<T, true>(a, down_parts, st);
   return rc;
 }
 
@@ -540,7 +594,7 @@ int topoep_ffn_bytes(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *rows
                      size_t *backward) {
   const int rc = check(f, T, rows);
   if (rc != TOPOEP_OK) return rc;
-  const Sizes s = sizes_of(f, T, rows ? rows->topk : 0);
+  const Sizes s = sizes_of(f, T, rows);
   if (forward) *forward = s.forward;
   if (saved) *saved = s.saved;
   if (backward) *backward = s.backward;
@@ -557,7 +611,7 @@ int topoep_ffn_forward(const topoep_ffn *f, const void *x, int64_t ldx, int32_t 
   if (rows && (!rows->offsets || !rows->pairs || !rows->places || !rows->weights)) return TOPOEP_EINVAL;
   if (ldx < f->hidden || (ldx & 7) || ldx > (int64_t)1 << 40) return TOPOEP_EINVAL;
   if (!aligned16(x) || !aligned16(up) || !aligned16(down) || !aligned16(out) || !aligned16(saved)) return TOPOEP_EINVAL;
-  const Sizes s = sizes_of(f, T, rows ? rows->topk : 0);
+  const Sizes s = sizes_of(f, T, rows);
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < s.forward) return TOPOEP_EWORKSPACE;
   Ffn a = args_of(f, x, ldx, T, rows, up, down);
   a.out = out;
@@ -566,7 +620,8 @@ int topoep_ffn_forward(const topoep_ffn *f, const void *x, int64_t ldx, int32_t 
   a.y = reinterpret_cast<float *>(static_cast<char *>(workspace) + s.h);
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  return f->dtype == TOPOEP_BF16 ? forward<Bf16>(a, st) : forward<F16>(a, st);
+  const int parts = out_parts(f, counts_of(f, T, rows), rows, f->inter);
+  return f->dtype == TOPOEP_BF16 ? forward<Bf16>(a, parts, st) : forward<F16>(a, parts, st);
 }
 
 int topoep_ffn_backward(const topoep_ffn *f, const void *x, int64_t ldx, int32_t T, const topoep_ffn_rows *rows,
@@ -583,7 +638,7 @@ int topoep_ffn_backward(const topoep_ffn *f, const void *x, int64_t ldx, int32_t
   if (!aligned16(x) || !aligned16(up) || !aligned16(down) || !aligned16(saved) || !aligned16(grad_out) ||
       !aligned16(grad_x) || !aligned16(grad_up) || !aligned16(grad_down))
     return TOPOEP_EINVAL;
-  const Sizes s = sizes_of(f, T, rows ? rows->topk : 0);
+  const Sizes s = sizes_of(f, T, rows);
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < s.backward) return TOPOEP_EWORKSPACE;
   Ffn a = args_of(f, x, ldx, T, rows, up, down);
   if (T == 0) a.offsets = nullptr;   // no rows, whatever they say
@@ -592,7 +647,8 @@ int topoep_ffn_backward(const topoep_ffn *f, const void *x, int64_t ldx, int32_t
   a.h = kept ? kept + s.gu : nullptr;
   a.da = ws;
   a.y = reinterpret_cast<float *>(ws + s.da);
-  a.part = reinterpret_cast<float *>(ws + s.da + s.y);
+  a.part = reinterpret_cast<float *>(ws + s.da + s.back);
+  a.sums = reinterpret_cast<float *>(ws + s.da + s.back + s.part);
   a.dout = grad_out;
   a.dx = grad_x;
   a.dw = rows ? grad_weights : nullptr;
@@ -600,7 +656,10 @@ int topoep_ffn_backward(const topoep_ffn *f, const void *x, int64_t ldx, int32_t
   a.ddown = grad_down;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  return f->dtype == TOPOEP_BF16 ? backward<Bf16>(a, st) : backward<F16>(a, st);
+  const Counts c = counts_of(f, T, rows);
+  const int parts = out_parts(f, c, rows, 2 * f->inter);
+  const int pu = grad_parts(f, c, 2 * f->inter, f->hidden), pd = grad_parts(f, c, f->hidden, f->inter);
+  return f->dtype == TOPOEP_BF16 ? backward<Bf16>(a, parts, pu, pd, st) : backward<F16>(a, parts, pu, pd, st);
 }
 
 }  // extern "C"

@@ -129,6 +129,8 @@ struct Int8 {
   void *out;
   int type;
   bool keep;
+  int parts;
+  int32_t *sums;              // [parts, M, N], parts > 1
 };
 
 __device__ inline void store1(void *out, int type, int64_t at, float v) {
@@ -168,23 +170,38 @@ __global__ __launch_bounds__(S::kThreads, 2) void int8_kernel(Int8 a) {
   clear_rest(a);
   Span s;
   const int nq = spans<S::BQ>(a.offsets, a.M, a.G, -1, s);
-  for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
+  const int each = ((a.K + a.parts - 1) / a.parts + S::kStage - 1) / S::kStage * S::kStage;
+  for (int t = blockIdx.x; t < nq * np * a.parts; t += gridDim.x) {
     const Me me;
+    const int part = t / (nq * np), k0 = imin(part * each, a.K);
     int tq, tp;
-    place_of(t, nq, np, tq, tp);
+    place_of(t - part * nq * np, nq, np, tq, tp);
     spans<S::BQ>(a.offsets, a.M, a.G, tq, s);
     ByRows<I8, S::BP, S::kWaves> p;
     ByRows<I8, S::BQ, S::kWaves> q;
-    const char *w = reinterpret_cast<const char *>(a.w) + (int64_t)s.group * a.N * a.K;
+    const char *w = reinterpret_cast<const char *>(a.w) + (int64_t)s.group * a.N * a.K + k0;
     p.start(me, [&](int r) {
       const int in = r % (S::TP * 16), half = Gated ? in / (kTiles * 16) : 0;
       const int c = tp * kCols + r / (S::TP * 16) * (kTiles * 16) + in % (kTiles * 16);
       return w + (int64_t)(half * a.No + imin(c, a.No - 1)) * a.K;
     });
-    q.start(me, [&](int r) { return reinterpret_cast<const char *>(a.q) + imin(s.first + r, s.end - 1) * a.ldq; });
+    q.start(me, [&](int r) { return reinterpret_cast<const char *>(a.q) + imin(s.first + r, s.end - 1) * a.ldq + k0; });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, me, a.K, p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, imin(each, a.K - k0), p0, p1, q0, q1, d);
+    if (a.parts > 1) {
+#pragma unroll
+      for (int j = 0; j < S::TQ; ++j) {
+        const int m = s.first + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
+        if (m >= s.end) continue;
+#pragma unroll
+        for (int i = 0; i < S::TP; ++i) {
+          const int c = tp * kCols + (me.wave % S::NP * kTiles + i % kTiles) * 16 + (me.lane >> 4) * 4;
+          if (c < a.No) *reinterpret_cast<v4i *>(a.sums + ((int64_t)part * a.M + m) * a.N + i / kTiles * a.No + c) = d[i][j];
+        }
+      }
+      continue;
+    }
     const float *ws = a.ws + (int64_t)s.group * a.N;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
@@ -213,6 +230,43 @@ __global__ __launch_bounds__(S::kThreads, 2) void int8_kernel(Int8 a) {
         store_row(a.out, a.type, m, a.No, c, v);
       }
     }
+  }
+}
+
+// The parts' sums, and what a product's epilogue makes of them; a workgroup has a row.
+template <bool Gated>
+__global__ __launch_bounds__(256) void parts_kernel(Int8 a) {
+  const int m = blockIdx.x;
+  int group = 0;
+  if (a.offsets) {
+    int first = 0, end = 0;
+    bool found = false;
+    for (int g0 = 0; g0 < a.G && !found; g0 += 64) {   // (the same in every lane)
+      const int g = g0 + lane_id();
+      if (g < a.G) rows_of(a.offsets, a.M, g, first, end);
+      const uint64_t has = __ballot(g < a.G && first <= m && m < end);
+      found = has != 0;
+      if (found) group = g0 + __ffsll((unsigned long long)has) - 1;
+    }
+    if (!found) return;
+  }
+  const float scale = a.scale[m], *ws = a.ws + (int64_t)group * a.N;
+  for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < a.No; c += gridDim.y * 1024) {
+    const auto sum = [&](int at) {
+      v4i s = *reinterpret_cast<const v4i *>(a.sums + (int64_t)m * a.N + at);
+      for (int p = 1; p < a.parts; ++p) s += *reinterpret_cast<const v4i *>(a.sums + ((int64_t)p * a.M + m) * a.N + at);
+      v4f v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * scale * ws[at + e];
+      return v;
+    };
+    v4f v = sum(c);
+    if (Gated) {
+      const v4f u = sum(a.No + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = v[e] * sigmoid(v[e]) * u[e];
+    }
+    store_row(a.out, a.type, m, a.No, c, v);
   }
 }
 
@@ -259,11 +313,37 @@ int check(const topoep_int8 *p, int32_t M) {
 typedef Shape<I8, 256, 256, 2, 4, false, false, 2> Large;
 typedef Shape<I8, 128, 128, 2, 2, false, false, 4> Small;
 
+int columns_of(const topoep_int8 *p) { return p->gated ? p->n / 2 : p->n; }
+// Tiles of 128 x 128, about.
+int64_t small_tiles(const topoep_int8 *p, int M) {
+  return likely_spans(p->groups > 1, M, p->groups, 128) * ceil_of(columns_of(p), p->gated ? 64 : 128);
+}
+// A few rows a group, 16 and fewer: the weights' bytes count, not the tiles.  Up to 64 also where
+// tiles would fill less than half of the chip's places (32 rows, N = 4096, K = 14336: 35 against 82
+// us; 128 matrices of 1536 x 2048 with 32 rows: 239 and 107).
+bool few_rows(const topoep_int8 *p, int M) {
+  const int64_t groups = imin(p->groups, M);
+  return M <= 16 * groups || (M <= 64 * groups && small_tiles(p, M) < 256);
+}
+// Workgroups that share a tile's inner axis (their sums are at most 256 MiB).
+int parts_of(const topoep_int8 *p, int M) {
+  if (M == 0 || few_rows(p, M) || columns_of(p) % 4) return 1;
+  const int parts = topoep_dev::parts_of(small_tiles(p, M), p->k / 128, 8);
+  return (int64_t)parts * M * p->n > (int64_t)1 << 26 ? 1 : parts;
+}
+size_t need(const topoep_int8 *p, int M) {
+  const int parts = parts_of(p, M);
+  return parts > 1 ? ((size_t)parts * M * p->n * sizeof(int32_t) + 255) & ~(size_t)255 : 0;
+}
+
 template <class S, bool Gated>
 int enqueue(const Int8 &a, hipStream_t st) {
   const int cols = Gated ? S::BP / 2 : S::BP;
-  const int64_t tiles = most_spans<S::BQ>(a.offsets, a.M, a.G) * ((a.No + cols - 1) / cols);
+  const int64_t tiles = most_spans<S::BQ>(a.offsets, a.M, a.G) * ((a.No + cols - 1) / cols) * a.parts;
   hipLaunchKernelGGL((int8_kernel<S, Gated>), dim3(grid_of<S>(tiles)), dim3(S::kThreads), 0, st, a);
+  if (!launched()) return TOPOEP_EHIP;
+  if (a.parts == 1) return TOPOEP_OK;
+  hipLaunchKernelGGL((parts_kernel<Gated>), dim3(a.M, imin((a.No + 1023) / 1024, 64)), dim3(256), 0, st, a);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
@@ -297,7 +377,7 @@ int topoep_matmul_int8_workspace_bytes(const topoep_int8 *p, int32_t M, size_t *
   const int rc = check(p, M);
   if (rc != TOPOEP_OK) return rc;
   if (!bytes_out) return TOPOEP_EINVAL;
-  *bytes_out = 0;
+  *bytes_out = need(p, M);
   return TOPOEP_OK;
 }
 
@@ -309,16 +389,17 @@ int topoep_matmul_int8(const topoep_int8 *p, const int8_t *q, int64_t ldq, const
   if (M == 0) return TOPOEP_OK;
   if (!q || !scale || !w || !w_scale || !out || (!offsets && p->groups != 1)) return TOPOEP_EINVAL;
   if (ldq < p->k || (ldq & 15) || ldq > (int64_t)1 << 40 || !aligned16(q) || !aligned16(w) || !aligned16(out)) return TOPOEP_EINVAL;
-  if (reinterpret_cast<uintptr_t>(workspace) & 255) return TOPOEP_EWORKSPACE;
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need(p, M)) return TOPOEP_EWORKSPACE;
+  if (!workspace && need(p, M)) return TOPOEP_EINVAL;
   Int8 a = {};
   a.M = M, a.N = p->n, a.K = p->k, a.G = p->groups, a.No = p->gated ? p->n / 2 : p->n;
   a.q = q, a.w = w, a.ldq = ldq, a.scale = scale, a.ws = w_scale, a.offsets = offsets;
   a.out = out, a.type = p->out_dtype, a.keep = keep_rest != 0;
+  a.parts = parts_of(p, M), a.sums = static_cast<int32_t *>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  // a few rows a group (16 and fewer): the weights' bytes count, not the tiles
-  const int64_t groups = imin(a.G, M);
-  if (M <= 16 * groups) {
+  if (few_rows(p, M)) {
+    const int64_t groups = imin(a.G, M);
     const int64_t np = (a.No + (p->gated ? 7 : 15)) / (p->gated ? 8 : 16);
     few_shape((M + groups - 1) / groups, groups * np, [&](auto c, auto ks) {
       constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
@@ -329,8 +410,8 @@ int topoep_matmul_int8(const topoep_int8 *p, const int8_t *q, int64_t ldq, const
     return launched() ? TOPOEP_OK : TOPOEP_EHIP;
   }
   const int per = p->gated ? 128 : 256;
-  if (large_tiles(likely_spans(offsets, M, a.G, 256) * ((a.No + per - 1) / per),
-                  likely_spans(offsets, M, a.G, 128) * ((a.No + per / 2 - 1) / (per / 2))))
+  if (a.parts == 1 && large_tiles(likely_spans(offsets != nullptr, M, a.G, 256) * ((a.No + per - 1) / per),
+                  likely_spans(offsets != nullptr, M, a.G, 128) * ((a.No + per / 2 - 1) / (per / 2))))
     return p->gated ? enqueue<Large, true>(a, st) : enqueue<Large, false>(a, st);
   return p->gated ? enqueue<Small, true>(a, st) : enqueue<Small, false>(a, st);
 }

@@ -85,13 +85,22 @@ template <int B>
 inline int64_t most_spans(const int32_t *offsets, int rows, int groups) {
   return ((int64_t)rows + B - 1) / B + (offsets ? imin(groups, rows) : 0);
 }
-// And about, of `expected` rows.
-inline int64_t likely_spans(const int32_t *offsets, int64_t expected, int groups, int B) {
-  return expected / B + (offsets ? (imin(groups, (int)expected) + 1) / 2 : expected % B != 0);
+// And about, of `expected` rows (by groups or not).
+inline int64_t likely_spans(bool by_groups, int64_t expected, int groups, int B) {
+  return expected / B + (by_groups ? ((expected < groups ? expected : groups) + 1) / 2 : expected % B != 0);
 }
 
 // Whether tiles of 256 x 256 take less time than their number of 128 x 128: one of the former a CU,
 // two of the latter, which reach 1340 and 1100 TFLOP/s (8192^3 in bf16).
 inline bool large_tiles(int64_t large, int64_t small) { return (large + 255) / 256 * 10 < (small + 511) / 512 * 6; }
 
+inline int64_t ceil_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Workgroups that share a tile: `tiles` of 128 x 128 leave most of the chip's 512 places empty (two
+// thirds of them measured no different from all), and every part has eight stages at least.
+inline int parts_of(int64_t tiles, int64_t stages, int most) {
+  const int64_t n = tiles < 1 || tiles > 256 ? 1 : 512 / tiles, by_stages = stages / 8;
+  const int64_t p = n < by_stages ? n : by_stages;
+  return (int)(p < 1 ? 1 : p < most ? p : most);
+}
 }  // namespace topoep_dev

@@ -139,6 +139,9 @@ def test_int8_refusals(ffn):
         assert call(**{name: good[name] + 8}) == EINVAL, name
     assert call(ldq=48) == EINVAL and call(ldq=72) == EINVAL and call(ldq=1 << 60) == EINVAL
     assert call(work=16384 + 16) == EWORKSPACE
+    p = good["p"] = ffn.Int8(64, 4096, 1, 0, 1)           # workgroups share the inner axis: their sums
+    assert W(p, 100, need) == OK and need.value >= 2 * 100 * 64 * 4
+    assert call(M=100, size=need.value - 1, ldq=4096) == EWORKSPACE and call(M=100, size=0, ldq=4096) == EWORKSPACE
     assert call(M=0, q=None) == OK
 
 

@@ -55,7 +55,9 @@ DENSE = [(1, 64, 32, BF16), (1, 8, 8, F16), (2, 520, 248, BF16), (15, 128, 128, 
          (17, 256, 64, BF16), (127, 136, 72, BF16), (128, 128, 256, F16), (129, 264, 104, BF16), (300, 64, 520, F16),
          (515, 392, 200, BF16),
          # large tiles: of the hidden axis, of the outputs, of the weights' gradients
-         (3000, 72, 3080, BF16), (3000, 3080, 72, F16), (70, 2056, 2064, BF16)]
+         (3000, 72, 3080, BF16), (3000, 3080, 72, F16), (70, 2056, 2064, BF16),
+         # few tiles: workgroups share the inner axis
+         (70, 264, 3080, BF16), (200, 128, 1544, F16), (2085, 136, 72, BF16), (4099, 64, 64, F16)]
 
 
 @pytest.mark.parametrize("T,H,I,dtype", DENSE)
@@ -73,7 +75,8 @@ def test_dense_block_and_gradients(T, H, I, dtype):
 ROUTED = [(1, 64, 32, 4, 4, 2, BF16), (1, 64, 32, 8, 2, 1, F16), (5, 136, 72, 16, 16, 8, BF16),
           (64, 128, 64, 37, 10, 6, F16), (130, 264, 136, 4, 4, 2, BF16), (333, 72, 200, 9, 5, 4, BF16),
           (600, 128, 128, 130, 128, 8, BF16), (3001, 136, 2056, 3, 3, 2, BF16), (2500, 2056, 136, 4, 3, 2, F16),
-          (90, 1032, 1040, 9, 9, 3, BF16), (257, 64, 64, 1, 1, 1, F16), (40, 64, 64, 1000, 700, 4, BF16)]
+          (90, 1032, 1040, 9, 9, 3, BF16), (300, 72, 2056, 3, 2, 2, F16), (3000, 64, 64, 2, 2, 1, BF16),
+          (257, 64, 64, 1, 1, 1, F16), (40, 64, 64, 1000, 700, 4, BF16)]
 
 
 @pytest.mark.parametrize("T,H,I,E,L,k,dtype", ROUTED)

@@ -112,7 +112,8 @@ def weights(seed, *shape):
 
 
 SHAPES = [(1, 16, 16), (1, 1, 64), (1, 100, 4096), (2, 37, 208), (4, 128, 128), (5, 130, 144), (16, 64, 1024), (17, 66, 256),
-          (33, 257, 80), (128, 128, 512), (129, 384, 272), (300, 129, 2064), (3000, 3082, 144)]
+          (33, 257, 80), (128, 128, 512), (129, 384, 272), (300, 129, 2064), (3000, 3082, 144),
+          (100, 200, 4112), (70, 1040, 14336), (65, 1, 2048)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -131,7 +132,8 @@ def test_product(M, N, K, gated, dtype, out):
 
 GROUPS = [([0, 0, 1], 64, 64), ([0, 5, 5, 9, 9], 48, 128), ([0, 1, 2, 3, 40, 41], 130, 256), ([0, 128, 129, 300], 72, 144),
           ([0, 17, 300, 301], 256, 96), ([0] * 70 + [3] + [7] * 80 + [8], 34, 64),
-          ([0, 1500, 1501, 4001], 2310, 80)]
+          ([0, 1500, 1501, 4001], 2310, 80),
+          ([0, 0, 65, 250], 96, 3088), ([0, 40, 41, 128], 136, 2064)]
 
 
 @pytest.mark.parametrize("ends,N,K", GROUPS)
