@@ -52,7 +52,9 @@ struct Ffn {
 };
 
 __device__ inline int token_of(const Ffn &a, int row) {
-  return a.pairs ? (int)fdiv((uint32_t)a.pairs[row], a.per_token) : row;
+  if (!a.pairs) return row;
+  const uint32_t pair = (uint32_t)a.pairs[row];
+  return (int)(a.k == 1 ? pair : __umulhi(pair, a.per_token.m) >> (a.per_token.sh - 32));   // (fdiv's upper half)
 }
 __device__ inline float weight_of(const Ffn &a, int row) { return a.pairs ? a.weights[a.pairs[row]] : 1.0f; }
 
@@ -69,9 +71,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void up_kernel(Ffn a) {
   const int nq = spans<S::BQ>(a.offsets, a.rows, a.L, -1, s);
   for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
     const Me me;
-    int tq, tp;
-    place_of(t, nq, np, tq, tp);
-    spans<S::BQ>(a.offsets, a.rows, a.L, tq, s);
+    const int tp = find_tile<S::BQ>(a.offsets, a.rows, a.L, t, np, nq * np, s);
     const int unit0 = tp * kUnits;
     ByRows<T, S::BP, S::kWaves> p;
     ByRows<T, S::BQ, S::kWaves> q;
@@ -91,21 +91,22 @@ __global__ __launch_bounds__(S::kThreads, 2) void up_kernel(Ffn a) {
       const int m = s.first + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
       if (m >= s.end) continue;
       const float weight = weight_of(a, m);
-#pragma unroll
-      for (int i = 0; i < kHalf; ++i) {
-        const int unit = unit0 + me.wave % S::NP * kWaveUnits + i * 16 + (me.lane >> 4) * 4;
-        if (unit >= a.I) continue;
+      const int first = unit0 + me.wave % S::NP * kWaveUnits;
+      store_rows<T>(me, kHalf, static_cast<T *>(a.h) + (int64_t)m * a.I, first, a.I, [&](int i) {
         const v4f g = d[i][j], u = d[i + kHalf][j];
+        if (Save) {
+          const int unit = first + i * 16 + (me.lane >> 4) * 4;
+          float *to = a.gu + (int64_t)m * 2 * a.I + unit;
+          if (unit < a.I) {
+            *reinterpret_cast<v4f *>(to) = g;
+            *reinterpret_cast<v4f *>(to + a.I) = u;
+          }
+        }
         v4f h;
 #pragma unroll
         for (int e = 0; e < 4; ++e) h[e] = weight * (g[e] * sigmoid(g[e]) * u[e]);
-        store4<T>(a.h, (int64_t)m * a.I + unit, h);
-        if (Save) {
-          float *to = a.gu + (int64_t)m * 2 * a.I + unit;
-          *reinterpret_cast<v4f *>(to) = g;
-          *reinterpret_cast<v4f *>(to + a.I) = u;
-        }
-      }
+        return h;
+      });
     }
   }
 }
@@ -123,9 +124,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void out_kernel(Ffn a, void *to, in
   for (int u = blockIdx.x; u < nq * np * parts; u += gridDim.x) {
     const Me me;
     const int part = u / (nq * np), k0 = imin(part * each, n);
-    int tq, tp;
-    place_of(u - part * nq * np, nq, np, tq, tp);
-    spans<S::BQ>(a.offsets, a.rows, a.L, tq, s);
+    const int tp = find_tile<S::BQ>(a.offsets, a.rows, a.L, u - part * nq * np, np, nq * np, s);
     typename std::conditional<Back, Across<T, S::BP, S::kWaves>, ByRows<T, S::BP, S::kWaves>>::type p;
     ByRows<T, S::BQ, S::kWaves> q;
     const T *w = static_cast<const T *>(Back ? a.up : a.down) + (int64_t)s.group * n * a.H;
@@ -142,12 +141,15 @@ __global__ __launch_bounds__(S::kThreads, 2) void out_kernel(Ffn a, void *to, in
     for (int j = 0; j < S::TQ; ++j) {
       const int m = s.first + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
       if (m >= s.end) continue;
+      const int first = tp * S::BP + me.wave % S::NP * S::TP * 16;
+      if (whole) {
+        store_rows<T>(me, S::TP, static_cast<T *>(to) + (int64_t)m * a.H, first, a.H, [&](int i) { return d[i][j]; });
+        continue;
+      }
 #pragma unroll
       for (int i = 0; i < S::TP; ++i) {
-        const int c = tp * S::BP + (me.wave % S::NP * S::TP + i) * 16 + (me.lane >> 4) * 4;
-        if (c >= a.H) continue;
-        if (whole) store4<T>(to, (int64_t)m * a.H + c, d[i][j]);
-        else *reinterpret_cast<v4f *>(static_cast<float *>(to) + at + (int64_t)m * a.H + c) = d[i][j];
+        const int c = first + i * 16 + (me.lane >> 4) * 4;
+        if (c < a.H) *reinterpret_cast<v4f *>(static_cast<float *>(to) + at + (int64_t)m * a.H + c) = d[i][j];
       }
     }
   }
@@ -233,9 +235,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void hidden_kernel(Ffn a) {
   const int nq = spans<S::BQ>(a.offsets, a.rows, a.L, -1, s);
   for (int t = blockIdx.x; t < nq * np; t += gridDim.x) {
     const Me me;
-    int tq, tp;
-    place_of(t, nq, np, tq, tp);
-    spans<S::BQ>(a.offsets, a.rows, a.L, tq, s);
+    const int tp = find_tile<S::BQ>(a.offsets, a.rows, a.L, t, np, nq * np, s);
     Across<T, S::BP, S::kWaves> p;
     ByRows<T, S::BQ, S::kWaves> q;
     p.start(me, static_cast<const char *>(a.down) + (int64_t)s.group * 2 * a.I * a.H, a.I, tp * S::BP, a.I);
@@ -253,23 +253,35 @@ __global__ __launch_bounds__(S::kThreads, 2) void hidden_kernel(Ffn a) {
       float sum = 0.0f;
       if (m < s.end) {
         const float weight = weight_of(a, m);
+        const int first = tp * S::BP + me.wave % S::NP * S::TP * 16;
+        T *const to = static_cast<T *>(a.da) + (int64_t)m * 2 * a.I;
 #pragma unroll
-        for (int i = 0; i < S::TP; ++i) {
-          const int unit = tp * S::BP + (me.wave % S::NP * S::TP + i) * 16 + (me.lane >> 4) * 4;
-          if (unit >= a.I) continue;
-          const float *from = a.gu + (int64_t)m * 2 * a.I + unit;
-          const v4f g = *reinterpret_cast<const v4f *>(from), u = *reinterpret_cast<const v4f *>(from + a.I);
-          v4f dg, du;
+        for (int i = 0; i < S::TP; i += 2) {
+          __builtin_amdgcn_sched_barrier(0);   // (all tiles' values loaded at once: scratch)
+          v4f dg[2], du[2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float sg = sigmoid(g[e]), act = g[e] * sg, dh = d[i][j][e];
-            sum += dh * (act * u[e]);
-            dg[e] = weight * (dh * u[e] * (sg + act * (1.0f - sg)));
-            du[e] = weight * (dh * act);
+          for (int t = 0; t < 2; ++t) {
+            const int unit = first + (i + t) * 16 + (me.lane >> 4) * 4;
+            v4f g = {}, u = {};
+            if (unit < a.I) {
+              const float *from = a.gu + (int64_t)m * 2 * a.I + unit;
+              g = *reinterpret_cast<const v4f *>(from);
+              u = *reinterpret_cast<const v4f *>(from + a.I);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float sg = sigmoid(g[e]), act = g[e] * sg, dh = d[i + t][j][e];
+              sum += unit < a.I ? dh * (act * u[e]) : 0.0f;
+              dg[t][e] = weight * (dh * u[e] * (sg + act * (1.0f - sg)));
+              du[t][e] = weight * (dh * act);
+            }
           }
-          const int64_t at = (int64_t)m * 2 * a.I + unit;
-          store4<T>(a.da, at, dg);
-          store4<T>(a.da, at + a.I, du);
+          const v4i og = pair_of<T>(dg[0], dg[1]), ou = pair_of<T>(du[0], du[1]);
+          const int unit = first + i * 16 + pair_column(me);
+          if (unit < a.I) {
+            *reinterpret_cast<v4i *>(to + unit) = og;
+            *reinterpret_cast<v4i *>(to + a.I + unit) = ou;
+          }
         }
       }
       if (a.dw) {
@@ -312,11 +324,14 @@ struct Tokens : AcrossPlaces<B, W> {
   __device__ void start(const Ffn &of, Me me, const void *base, int64_t stride, int row, int c0, int n, int len) {
     const int c = c0 + At::column_of(me);
     a = &of, from = static_cast<const char *>(base) + (c < n ? c : 0) * 2, ld = stride * 2, first = row;
-    next(me, 0, len);
+    if (len > 0) next(me, 0, len);
   }
   __device__ void next(Me me, int k, int n) {
 #pragma unroll
-    for (int i = 0; i < At::kLoads; ++i) token[i] = k + At::row_of(i, me) < n ? token_of(*a, first + k + At::row_of(i, me)) : 0;
+    for (int i = 0; i < At::kLoads; ++i) {
+      const int at = k + At::row_of(i, me);
+      token[i] = token_of(*a, first + (at < n ? at : 0));
+    }
   }
   __device__ void load(Lds *to, Me me, int k, int n) {
 #pragma unroll
@@ -340,7 +355,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a, int parts) 
   const int np = (cols + S::BP - 1) / S::BP, nq = (rows + S::BQ - 1) / S::BQ;
   const int part = blockIdx.x / (np * nq) % parts, g = blockIdx.x / (np * nq) / parts;
   int tq, tp, first, end;
-  place_of(blockIdx.x % (np * nq), nq, np, tq, tp);
+  place_of(by_xcd(blockIdx.x % (np * nq), np * nq), nq, np, tq, tp);
   rows_of(a.offsets, a.rows, g, first, end);
   const int each = ((end - first + parts - 1) / parts + S::kStage - 1) / S::kStage * S::kStage;
   first = imin(first + part * each, end);
@@ -366,12 +381,15 @@ __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a, int parts) 
   for (int j = 0; j < S::TQ; ++j) {
     const int r = tq * S::BQ + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
     if (r >= rows) continue;
+    const int left = tp * S::BP + me.wave % S::NP * S::TP * 16;
+    if (parts == 1) {
+      store_rows<T>(me, S::TP, static_cast<T *>(to) + (at + r) * cols, left, cols, [&](int i) { return d[i][j]; });
+      continue;
+    }
 #pragma unroll
     for (int i = 0; i < S::TP; ++i) {
-      const int c = tp * S::BP + (me.wave % S::NP * S::TP + i) * 16 + (me.lane >> 4) * 4;
-      if (c >= cols) continue;
-      if (parts == 1) store4<T>(to, (at + r) * cols + c, d[i][j]);
-      else *reinterpret_cast<v4f *>(a.sums + (at + r) * cols + c) = d[i][j];
+      const int c = left + i * 16 + (me.lane >> 4) * 4;
+      if (c < cols) *reinterpret_cast<v4f *>(a.sums + (at + r) * cols + c) = d[i][j];
     }
   }
 }
@@ -462,6 +480,7 @@ Ffn args_of(const topoep_ffn *f, const void *x, int64_t ldx, int32_t T, const to
 }
 
 template <class T, bool PA> using Large = Shape<T, 256, 256, PA ? 4 : 2, PA ? 2 : 4, PA, false, 2>;
+template <class T> using LargeHidden = Shape<T, 256, 256, 2, 4, true, false, 2>;
 template <class T, bool PA> using Small = Shape<T, 128, 128, 2, 2, PA, false, 4>;
 template <class T> using LargeGrad = Shape<T, 256, 256, 2, 4, true, true, 1>;
 template <class T> using SmallGrad = Shape<T, 128, 128, 2, 2, true, true, 4>;
@@ -517,7 +536,7 @@ int enqueue_hidden_of(const Ffn &a, hipStream_t st) {
 template <class T>
 int enqueue_hidden(const Ffn &a, hipStream_t st) {
   static_assert(Small<T, true>::BP >= kPartUnits, "parts of the weights' gradient");
-  return large_rows(a, a.I, 256) ? enqueue_hidden_of<Large<T, true>>(a, st) : enqueue_hidden_of<Small<T, true>>(a, st);
+  return large_rows(a, a.I, 256) ? enqueue_hidden_of<LargeHidden<T>>(a, st) : enqueue_hidden_of<Small<T, true>>(a, st);
 }
 
 template <class S, bool Down>
@@ -538,18 +557,25 @@ int enqueue_grad(const Ffn &a, int parts, hipStream_t st) {
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
-// A few rows a group, 16 and fewer: the weights' bytes count, not the tiles.  Up to 64 also where tiles of
-// 128 x 128 would fill less than half of the chip's places (32 rows, H = 4096, I = 11008: 115 against
-// 196 us; 128 experts of H = 2048, I = 768 with 32 rows: 588 and 278).
-bool few_rows(const Ffn &a, int64_t np) {
-  return a.expected <= 16 * (int64_t)a.L ||
-         (a.expected <= 64 * (int64_t)a.L && likely_spans(a.offsets != nullptr, a.expected, a.L, 128) * np < 256);
+// A few rows a group, 16 and fewer: the weights' bytes count, not the tiles.  Up to 64 also where a product
+// of `n` rows of weights is small (rows times weights of 512 MiB: 32 rows, H = I = 2048, both products:
+// 17.8 against 30.2 us; I = 5632: 41.4 and 38.7).
+bool few_rows(const Ffn &a, int64_t n, int64_t k) {
+  const int64_t groups = imin(a.L, (int)a.expected);
+  return a.expected <= 16 * groups || (a.expected <= 64 * groups && (double)a.expected * groups * n * k <= 0x1p28);
+}
+
+// Columns for a group's rows at once: groups differ, and twice the mean is what most have at most (128
+// experts, four rows on average: 202 against 225 us with the mean).
+int64_t few_each(const Ffn &a) {
+  const int64_t groups = imin(a.L, (int)a.expected), mean = (a.expected + groups - 1) / groups;
+  return groups > 1 ? 2 * mean : mean;
 }
 
 template <class T>
 int enqueue_few_up(const Ffn &a, hipStream_t st) {
   const int64_t groups = imin(a.L, (int)a.expected), nu = (a.I + 7) / 8;
-  few_shape((a.expected + groups - 1) / groups, groups * nu, [&](auto c, auto ks) {
+  few_shape(few_each(a), groups * nu, [&](auto c, auto ks) {
     constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
     const dim3 grid = few_grid<KS>(most_spans<4 * C>(a.offsets, a.rows, a.L) * nu), block(64 * few_waves(KS));
     if (a.gu) hipLaunchKernelGGL((few_up_kernel<T, true, C, KS>), grid, block, 0, st, a);
@@ -560,7 +586,7 @@ int enqueue_few_up(const Ffn &a, hipStream_t st) {
 template <class T>
 int enqueue_few_down(const Ffn &a, hipStream_t st) {
   const int64_t groups = imin(a.L, (int)a.expected), nh = (a.H + kFewRows - 1) / kFewRows;
-  few_shape((a.expected + groups - 1) / groups, groups * nh, [&](auto c, auto ks) {
+  few_shape(few_each(a), groups * nh, [&](auto c, auto ks) {
     constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
     const dim3 grid = few_grid<KS>(most_spans<4 * C>(a.offsets, a.rows, a.L) * nh), block(64 * few_waves(KS));
     hipLaunchKernelGGL((few_down_kernel<T, C, KS>), grid, block, 0, st, a, a.pairs ? static_cast<void *>(a.y) : a.out);
@@ -571,9 +597,9 @@ int enqueue_few_down(const Ffn &a, hipStream_t st) {
 
 template <class T>
 int forward(const Ffn &a, int parts, hipStream_t st) {
-  const int rc = few_rows(a, (a.I + 63) / 64) ? enqueue_few_up<T>(a, st) : enqueue_up<T>(a, st);
+  const int rc = few_rows(a, 2 * a.I, a.H) ? enqueue_few_up<T>(a, st) : enqueue_up<T>(a, st);
   if (rc != TOPOEP_OK) return rc;
-  return few_rows(a, (a.H + 127) / 128) ? enqueue_few_down<T>(a, st) : enqueue_out<T, false>(a, a.out, parts, st);
+  return few_rows(a, a.H, a.I) ? enqueue_few_down<T>(a, st) : enqueue_out<T, false>(a, a.out, parts, st);
 }
 
 template <class T>

@@ -174,9 +174,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void int8_kernel(Int8 a) {
   for (int t = blockIdx.x; t < nq * np * a.parts; t += gridDim.x) {
     const Me me;
     const int part = t / (nq * np), k0 = imin(part * each, a.K);
-    int tq, tp;
-    place_of(t - part * nq * np, nq, np, tq, tp);
-    spans<S::BQ>(a.offsets, a.M, a.G, tq, s);
+    const int tp = find_tile<S::BQ>(a.offsets, a.M, a.G, t - part * nq * np, np, nq * np, s);
     ByRows<I8, S::BP, S::kWaves> p;
     ByRows<I8, S::BQ, S::kWaves> q;
     const char *w = reinterpret_cast<const char *>(a.w) + (int64_t)s.group * a.N * a.K + k0;
@@ -318,12 +316,11 @@ int columns_of(const topoep_int8 *p) { return p->gated ? p->n / 2 : p->n; }
 int64_t small_tiles(const topoep_int8 *p, int M) {
   return likely_spans(p->groups > 1, M, p->groups, 128) * ceil_of(columns_of(p), p->gated ? 64 : 128);
 }
-// A few rows a group, 16 and fewer: the weights' bytes count, not the tiles.  Up to 64 also where
-// tiles would fill less than half of the chip's places (32 rows, N = 4096, K = 14336: 35 against 82
-// us; 128 matrices of 1536 x 2048 with 32 rows: 239 and 107).
+// A few rows a group, 16 and fewer: the weights' bytes count, not the tiles.  Up to 64 also where a
+// product is small (rows times weights of 512 MiB: 32 rows, 4096 x 4096: 14.9 against 17.1 us, 64: 24.3 and 18.3).
 bool few_rows(const topoep_int8 *p, int M) {
   const int64_t groups = imin(p->groups, M);
-  return M <= 16 * groups || (M <= 64 * groups && small_tiles(p, M) < 256);
+  return M <= 16 * groups || (M <= 64 * groups && (double)M * groups * p->n * p->k <= 0x1p29);
 }
 // Workgroups that share a tile's inner axis (their sums are at most 256 MiB).
 int parts_of(const topoep_int8 *p, int M) {
@@ -401,7 +398,8 @@ int topoep_matmul_int8(const topoep_int8 *p, const int8_t *q, int64_t ldq, const
   if (few_rows(p, M)) {
     const int64_t groups = imin(a.G, M);
     const int64_t np = (a.No + (p->gated ? 7 : 15)) / (p->gated ? 8 : 16);
-    few_shape((M + groups - 1) / groups, groups * np, [&](auto c, auto ks) {
+    // (groups differ: twice the mean is what most have at most)
+    few_shape((M + groups - 1) / groups * (groups > 1 ? 2 : 1), groups * np, [&](auto c, auto ks) {
       constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
       const dim3 grid = few_grid<KS>(most_spans<4 * C>(offsets, M, a.G) * np), block(64 * few_waves(KS));
       if (p->gated) hipLaunchKernelGGL((few_int8_kernel<true, C, KS>), grid, block, 0, st, a);

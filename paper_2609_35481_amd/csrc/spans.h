@@ -17,15 +17,16 @@ __device__ inline void rows_of(const int32_t *offsets, int rows, int g, int &fir
   }
 }
 
-// A tile of rows: `first` .. `end` - 1 are what is left of its group from its first on.
-struct Span { int group, first, end; };
+// A tile of rows: `first` .. `end` - 1 are what is left of its group from its first on; the group's
+// `tiles` start with number `before`.
+struct Span { int group, first, end, before, tiles; };
 
 // How many tiles of B rows the groups have, and the rows of tile n (n < 0: none).
 template <int B>
 __device__ inline int spans(const int32_t *offsets, int rows, int groups, int n, Span &s) {
   if (!offsets) {
-    s = Span{0, n * B, rows};
-    return (rows + B - 1) / B;
+    s = Span{0, n * B, rows, 0, (rows + B - 1) / B};
+    return s.tiles;
   }
   int before = 0;
   for (int g0 = 0; g0 < groups; g0 += 64) {
@@ -37,7 +38,9 @@ __device__ inline int spans(const int32_t *offsets, int rows, int groups, int n,
     if (has) {
       const int l = __ffsll((unsigned long long)has) - 1;
       s.group = g0 + l;
-      s.first = readlane_i32(first, l) + (n - (readlane_i32(upto, l) - readlane_i32(mine, l))) * B;
+      s.tiles = readlane_i32(mine, l);
+      s.before = readlane_i32(upto, l) - s.tiles;
+      s.first = readlane_i32(first, l) + (n - s.before) * B;
       s.end = readlane_i32(end, l);
     }
     before = readlane_i32(upto, 63);
@@ -45,15 +48,28 @@ __device__ inline int spans(const int32_t *offsets, int rows, int groups, int n,
   return before;
 }
 
-// Tile t of nq by np: bands of eight q, of a band q first.  The tiles of an XCD (every eighth
-// workgroup) are neighbours, so that its L2 serves both operands.
+// The neighbour order of an XCD's workgroups (every eighth): tile t of `total`.
+__device__ inline int by_xcd(int t, int total) {
+  const int each = total / 8;
+  return t < each * 8 ? t % 8 * each + t / 8 : t;
+}
+// Tile t of nq by np: bands of eight q, of a band q first, so that an L2 serves both operands.
 __device__ inline void place_of(int t, int nq, int np, int &q, int &p) {
   constexpr int kBand = 8;
-  const int total = nq * np, each = total / 8;
-  if (t < each * 8) t = t % 8 * each + t / 8;
   const int band = t / (kBand * np), r = t - band * kBand * np, high = imin(kBand, nq - band * kBand);
   q = band * kBand + r % high;
   p = r / high;
+}
+// Tile t of all groups', np of P each: a group's tiles are neighbours, so that its weights come from
+// memory once.  s: its rows; the result: its tile of P.
+template <int B>
+__device__ inline int find_tile(const int32_t *offsets, int rows, int groups, int t, int np, int total, Span &s) {
+  t = by_xcd(t, total);
+  spans<B>(offsets, rows, groups, t / np, s);
+  int q, p;
+  place_of(t - s.before * np, s.tiles, np, q, p);
+  s.first += (s.before + q - t / np) * B;
+  return p;
 }
 
 // Static LDS of a product: two stages of each operand, variables of their own, so
@@ -71,6 +87,40 @@ __device__ inline void store4(void *to, int64_t at, v4f v) {
   typedef E v4e __attribute__((ext_vector_type(4)));
   const v4e o = __builtin_convertvector(v, v4e);
   __builtin_memcpy(static_cast<E *>(to) + at, &o, sizeof(o));
+}
+
+// A wave's 16-bit results, rows of neighbouring p (whole eights of them): two tiles of 16 at a time, whose
+// halves lanes exchange, so that a lane stores 16 bytes and a row's 64 are together.
+template <class T>
+__device__ inline v2i pack4(v4f v) {
+  v2i o;
+  store4<T>(&o, 0, v);
+  return o;
+}
+// Of tiles i and i + 1: what a lane stores, and the columns (of those from tile i's first on) where.
+template <class T>
+__device__ inline v4i pair_of(v4f first, v4f second) {
+  const v2i a = pack4<T>(first), b = pack4<T>(second);
+  v4i o;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const auto x = __builtin_amdgcn_permlane16_swap((uint32_t)a[e], (uint32_t)b[e], false, false);
+    o[e] = (int)x[0];
+    o[e + 2] = (int)x[1];
+  }
+  return o;
+}
+__device__ inline int pair_column(Me me) { return (me.lane >> 4 & 1) * 16 + (me.lane >> 5) * 8; }
+
+// `tiles` of them, value(i), to the columns from `c` on of the row at `to`, of which there are n.
+template <class T, class FV>
+__device__ inline void store_rows(Me me, int tiles, void *to, int c, int n, const FV &value) {
+#pragma unroll
+  for (int i = 0; i < tiles; i += 2) {
+    const v4i o = pair_of<T>(value(i), value(i + 1));
+    const int at = c + i * 16 + pair_column(me);
+    if (at < n) *reinterpret_cast<v4i *>(static_cast<T *>(to) + at) = o;
+  }
 }
 
 // Workgroups of S for at most `tiles` tiles: as many as a CU holds, which take them in turn.
