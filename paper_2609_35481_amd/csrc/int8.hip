@@ -20,7 +20,6 @@ struct Quant {
   int M, K;
   int8_t *q;
   float *scale;
-  bool wide;   // rows of x at multiples of 16 bytes, K a multiple of 8
 };
 
 // x / s to the nearest integer, ties to even, at most 127 in magnitude.  The quotient rounded to 32 bits
@@ -36,85 +35,114 @@ __device__ inline int nearest(float x, float s) {
   return (int)fminf(fmaxf(r, -127.0f), 127.0f);
 }
 
-constexpr int kEach = 8;   // elements of a load
-
-template <class T>
-__device__ inline void load8(const T *row, int k, int K, bool wide, float (&v)[kEach]) {
-  if (wide) {
-    T e[kEach];
-    __builtin_memcpy(e, __builtin_assume_aligned(row + k, 16), sizeof(e));
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) v[i] = to_float(e[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) v[i] = k + i < K ? to_float(row[k + i]) : 0.0f;
+// What a row's elements are divided by.  A quotient is first taken as a product with the reciprocal, off by
+// at most 127 (2^-24 + 2^-24) = 1.6 10^-5; only one that near to a border is divided (16-bit rows of 14336:
+// 114 us with a division each, FIGURE).
+struct Divisor {
+  float scale, inverse, lift;
+  bool plain, quick;
+  __device__ explicit Divisor(uint32_t top) {   // the largest magnitude's bits
+    scale = __uint_as_float(top) / 127.0f;
+    plain = scale > 0.0f && top < 0x7F800000u;
+    quick = scale >= 0x1p-100f;
+    // (both times 2^64 where a remainder could be too small for 32 bits)
+    lift = quick ? 1.0f : 0x1p64f;
+    inverse = 1.0f / scale;
   }
-}
+  template <int N>
+  __device__ void divide(const float (&v)[N], int8_t (&q)[N]) const {
+    bool near = !quick;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float t = v[e] * inverse, r = rintf(t);
+      near |= fabsf(t - r) > 0.5f - 0x1p-14f;
+      q[e] = plain ? (int8_t)(int)r : (int8_t)0;
+    }
+    if (near && plain)
+#pragma unroll
+      for (int e = 0; e < N; ++e) q[e] = (int8_t)nearest(v[e] * lift, scale * lift);
+  }
+};
 
 // Of magnitudes as unsigned words the largest: NaN's lie above infinity's.
 __device__ inline uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
-// W waves a row, 256 / (64 W) rows a workgroup; a thread keeps V loads of the row in registers, and reads
-// what is behind them again.
+// Over a row's W waves.
+template <int W>
+__device__ inline uint32_t most_of(uint32_t top) {
+  __shared__ uint32_t most[4];
+  top = row_max<64>(top);
+  if (W > 1) {
+    most[threadIdx.x >> 6] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = max(top, most[w]);
+  }
+  return top;
+}
+
+// W waves a row, 4 / W rows a workgroup, 16 bytes a lane and load (x and its rows at multiples of that, K of
+// the elements in it); V loads a lane stay in registers, what is behind them is read again.
 template <class T, int W, int V>
 __global__ __launch_bounds__(256) void quantize_kernel(Quant a) {
-  __shared__ uint32_t most[4];
+  constexpr int N = 16 / (int)sizeof(T), kAll = 64 * W * N;
   const int wave = uniform_i32(threadIdx.x >> 6), lane = threadIdx.x % (64 * W);
   const int m = blockIdx.x * (4 / W) + wave / W;
   const bool live = m < a.M;
   const T *row = static_cast<const T *>(a.x) + (live ? m : 0) * a.ldx;
   const int K = live ? a.K : 0;
-  float v[V][kEach];
+  const auto load = [&](int k) { return *reinterpret_cast<const v4i *>(row + k); };
+  const auto floats = [](v4i r, float (&v)[N]) {
+    T e[N];
+    __builtin_memcpy(e, &r, 16);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = to_float(e[i]);
+  };
   uint32_t top = 0;
+  const auto look = [&](v4i r) {
+    float v[N];
+    floats(r, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = max(top, magnitude(v[i]));
+  };
+  v4i held[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int k = (i * 64 * W + lane) * kEach;
-    if (k < K) {
-      load8(row, k, K, a.wide, v[i]);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) top = max(top, magnitude(v[i][e]));
-    }
+    const int k = i * kAll + lane * N;
+    held[i] = k < K ? load(k) : v4i{0, 0, 0, 0};
   }
-  for (int k = (V * 64 * W + lane) * kEach; k < K; k += 64 * W * kEach) {
-    float u[kEach];
-    load8(row, k, K, a.wide, u);
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) top = max(top, magnitude(u[e]));
-  }
-  top = row_max<64>(top);
-  if (W > 1) {
-    most[wave] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < W; ++w) top = max(top, most[w]);
-  }
-  const float scale = __uint_as_float(top) / 127.0f;
-  const bool plain = scale > 0.0f && top < 0x7F800000u;
-  if (live && lane == 0) a.scale[m] = scale;
-  // (both times 2^64 where a remainder could be too small for 32 bits)
-  const float lift = scale < 0x1p-100f ? 0x1p64f : 1.0f, step = scale * lift;
-  const auto store = [&](int k, const float (&u)[kEach]) {
-    int8_t q[kEach];
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) q[e] = plain ? (int8_t)nearest(u[e] * lift, step) : (int8_t)0;
-    int8_t *to = a.q + (int64_t)m * a.K + k;
-    if (a.wide) {
-      __builtin_memcpy(to, q, kEach);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kEach; ++e)
-        if (k + e < K) to[e] = q[e];
-    }
+  for (int i = 0; i < V; ++i) look(held[i]);
+  for (int k = V * kAll + lane * N; k < K; k += kAll) look(load(k));
+  const Divisor d(most_of<W>(top));
+  if (live && lane == 0) a.scale[m] = d.scale;
+  const auto store = [&](int k, v4i r) {
+    float v[N];
+    int8_t q[N];
+    floats(r, v);
+    d.divide(v, q);
+    __builtin_memcpy(a.q + (int64_t)m * a.K + k, q, N);
   };
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int k = (i * 64 * W + lane) * kEach;
-    if (k < K) store(k, v[i]);
-  }
-  for (int k = (V * 64 * W + lane) * kEach; k < K; k += 64 * W * kEach) {
-    float u[kEach];
-    load8(row, k, K, a.wide, u);
-    store(k, u);
+  for (int i = 0; i < V; ++i)
+    if (i * kAll + lane * N < K) store(i * kAll + lane * N, held[i]);
+  for (int k = V * kAll + lane * N; k < K; k += kAll) store(k, load(k));
+}
+
+// Rows of any alignment: a workgroup a row, an element a lane.
+template <class T>
+__global__ __launch_bounds__(256) void quantize_any_kernel(Quant a) {
+  const int m = blockIdx.x;
+  const T *row = static_cast<const T *>(a.x) + m * a.ldx;
+  uint32_t top = 0;
+  for (int k = threadIdx.x; k < a.K; k += 256) top = max(top, magnitude(to_float(row[k])));
+  const Divisor d(most_of<4>(top));
+  if (threadIdx.x == 0) a.scale[m] = d.scale;
+  for (int k = threadIdx.x; k < a.K; k += 256) {
+    const float v[1] = {to_float(row[k])};
+    int8_t q[1];
+    d.divide(v, q);
+    a.q[(int64_t)m * a.K + k] = q[0];
   }
 }
 
@@ -186,7 +214,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void int8_kernel(Int8 a) {
     q.start(me, [&](int r) { return reinterpret_cast<const char *>(a.q) + imin(s.first + r, s.end - 1) * a.ldq + k0; });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, me, imin(each, a.K - k0), p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, imin(each, a.K - k0), start_of<S>(imin(each, a.K - k0), s.group), p0, p1, q0, q1, d);
     if (a.parts > 1) {
 #pragma unroll
       for (int j = 0; j < S::TQ; ++j) {
@@ -346,9 +374,13 @@ int enqueue(const Int8 &a, hipStream_t st) {
 
 template <class T>
 int enqueue_quantize(const Quant &a, hipStream_t st) {
+  constexpr int N = 16 / (int)sizeof(T);
+  const bool wide = aligned16(a.x) && a.ldx % N == 0 && a.K % N == 0 && reinterpret_cast<uintptr_t>(a.q) % N == 0;
   // a wave a row where that keeps the row in registers
-  if (a.K <= 64 * kEach * 4 && a.M > 1) hipLaunchKernelGGL((quantize_kernel<T, 1, 4>), dim3((a.M + 3) / 4), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((quantize_kernel<T, 4, 4>), dim3(a.M), dim3(256), 0, st, a);
+  if (!wide) hipLaunchKernelGGL((quantize_any_kernel<T>), dim3(a.M), dim3(256), 0, st, a);
+  else if (a.K <= 64 * N * 4 && a.M > 1) hipLaunchKernelGGL((quantize_kernel<T, 1, 4>), dim3((a.M + 3) / 4), dim3(256), 0, st, a);
+  else if (a.K <= 256 * N * 4) hipLaunchKernelGGL((quantize_kernel<T, 4, 4>), dim3(a.M), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((quantize_kernel<T, 4, 8>), dim3(a.M), dim3(256), 0, st, a);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 
@@ -362,8 +394,7 @@ int topoep_quantize(const void *x, int32_t dtype, int64_t ldx, int32_t M, int32_
   if (M == 0) return TOPOEP_OK;
   const int size = dtype == TOPOEP_F32 ? 4 : 2;
   if (!x || !q || !scale || reinterpret_cast<uintptr_t>(x) % size || reinterpret_cast<uintptr_t>(scale) % 4) return TOPOEP_EINVAL;
-  Quant a{x, ldx, M, K, q, scale, false};
-  a.wide = aligned16(x) && ldx * size % 16 == 0 && K % kEach == 0 && reinterpret_cast<uintptr_t>(q) % kEach == 0;
+  const Quant a{x, ldx, M, K, q, scale};
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   if (dtype == TOPOEP_F32) return enqueue_quantize<float>(a, st);
@@ -408,7 +439,7 @@ int topoep_matmul_int8(const topoep_int8 *p, const int8_t *q, int64_t ldq, const
     return launched() ? TOPOEP_OK : TOPOEP_EHIP;
   }
   const int per = p->gated ? 128 : 256;
-  if (a.parts == 1 && large_tiles(likely_spans(offsets != nullptr, M, a.G, 256) * ((a.No + per - 1) / per),
+  if (a.parts == 1 && (!offsets || M >= 1024 * (int64_t)a.G) && large_tiles(likely_spans(offsets != nullptr, M, a.G, 256) * ((a.No + per - 1) / per),
                   likely_spans(offsets != nullptr, M, a.G, 128) * ((a.No + per / 2 - 1) / (per / 2))))
     return p->gated ? enqueue<Large, true>(a, st) : enqueue<Large, false>(a, st);
   return p->gated ? enqueue<Small, true>(a, st) : enqueue<Small, false>(a, st);

@@ -135,9 +135,10 @@ template <int B>
 inline int64_t most_spans(const int32_t *offsets, int rows, int groups) {
   return ((int64_t)rows + B - 1) / B + (offsets ? imin(groups, rows) : 0);
 }
-// And about, of `expected` rows (by groups or not).
+// And about, of `expected` rows (by groups or not; groups differ, and a quarter more leaves room for that).
 inline int64_t likely_spans(bool by_groups, int64_t expected, int groups, int B) {
-  return expected / B + (by_groups ? ((expected < groups ? expected : groups) + 1) / 2 : expected % B != 0);
+  if (!by_groups) return (expected + B - 1) / B;
+  return (expected / B + ((expected < groups ? expected : groups) + 1) / 2) * 5 / 4;
 }
 
 // Whether tiles of 256 x 256 take less time than their number of 128 x 128: one of the former a CU,

@@ -87,14 +87,12 @@ struct ByRows {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) from[i] = row(row_of(i, me)) + piece_of(me) * 16;
   }
-  // A stage, k elements of the n done.
-  __device__ void load(Lds *to, Me me, int k, int n) {
+  // The stage from element k of n on (`next`: the one after it).
+  __device__ void load(Lds *to, Me me, int k, int next, int n) {
     const bool in = piece_of(me) * (16 / (int)sizeof(T)) < n - k;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      to_lds(in ? from[i] : reinterpret_cast<const char *>(&kZeros), to + load_of(i, me.wave) * 1024);
-      from[i] += kLine;
-    }
+    for (int i = 0; i < kLoads; ++i)
+      to_lds(in ? from[i] + (int64_t)k * (int)sizeof(T) : reinterpret_cast<const char *>(&kZeros), to + load_of(i, me.wave) * 1024);
   }
 };
 
@@ -133,14 +131,13 @@ struct Across : AcrossPlaces<B, W> {
     ld = stride * 2;
     from = static_cast<const char *>(base) + At::row_of_lane(me) * ld + (c < n ? c : 0) * 2;
   }
-  __device__ void load(Lds *to, Me me, int k, int n) {
+  __device__ void load(Lds *to, Me me, int k, int next, int n) {
     const int left = n - k - At::row_of_lane(me);
 #pragma unroll
     for (int i = 0; i < At::kLoads; ++i) {
       const int j = At::load_of(i, me.wave), row = At::row_of_load(j);
-      to_lds(row < left ? from + row * ld : reinterpret_cast<const char *>(&kZeros), to + j * kApart);
+      to_lds(row < left ? from + (k + row) * ld : reinterpret_cast<const char *>(&kZeros), to + j * kApart);
     }
-    from += kAcross * ld;
   }
 };
 
@@ -237,30 +234,46 @@ __device__ inline void multiply_stage(const Lds *ps, const Lds *qs, const typena
   stage_order<S, Loads>();
 }
 
-// d += P Q over the n elements of the inner axis: one stage is multiplied while the next one
-// is on its way.  Every wave is done with a stage's LDS when the next barrier lets loads into it.
+// d += P Q over the n elements of the inner axis, from stage `start` on and round: one stage is multiplied
+// while the next one is on its way.  Every wave is done with a stage's LDS when the next barrier
+// lets loads into it.
 template <class S, class P, class Q>
-__device__ inline void multiply(P &p, Q &q, Me me, int n, Lds *p0, Lds *p1, Lds *q0, Lds *q1,
+__device__ inline void multiply(P &p, Q &q, Me me, int n, int start, Lds *p0, Lds *p1, Lds *q0, Lds *q1,
                                 typename S::Sum (&d)[S::TP][S::TQ]) {
   constexpr int kLoads = P::kLoads + Q::kLoads;
   const typename S::PView pv(me.wave % S::NP * S::TP * 16, me.lane);
   const typename S::QView qv(me.wave / S::NP * S::TQ * 16, me.lane);
   const int stages = (n + S::kStage - 1) / S::kStage;
-  if (stages > 0) p.load(p0, me, 0, n), q.load(q0, me, 0, n);
-  int k = S::kStage;
+  // the stage after next; behind the last one: zeros
+  int left = stages, k = start * S::kStage, next = k;
+  const auto turn = [&] {
+    k = next;
+    next = --left > 0 ? (next + S::kStage < n ? next + S::kStage : 0) : n;
+  };
+  turn();
+  if (stages > 0) p.load(p0, me, k, next, n), q.load(q0, me, k, next, n);
 #pragma unroll 1
   for (int g = stages >> 1; g > 0; --g) {
     arrived<0>();
-    p.load(p1, me, k, n), q.load(q1, me, k, n);
+    turn();
+    p.load(p1, me, k, next, n), q.load(q1, me, k, next, n);
     multiply_stage<S, kLoads>(p0, q0, pv, qv, d);
     arrived<0>();
-    // (behind the last stage: zeros)
-    p.load(p0, me, k + S::kStage, n), q.load(q0, me, k + S::kStage, n);
+    turn();
+    p.load(p0, me, k, next, n), q.load(q0, me, k, next, n);
     multiply_stage<S, kLoads>(p1, q1, pv, qv, d);
-    k += 2 * S::kStage;
   }
   arrived<0>();
   if (stages & 1) multiply_stage<S, 0>(p0, q0, pv, qv, d);
+}
+
+// The stage a workgroup starts with.  Rows lie multiples of some kilobytes apart: workgroups that read the
+// same place of all their rows meet few of memory's channels.  Those of an XCD and a group share operands
+// and stay together.
+template <class S>
+__device__ inline int start_of(int n, int group) {
+  const int stages = (n + S::kStage - 1) / S::kStage;
+  return stages > 0 ? (int)(((blockIdx.x & 7) * (unsigned)stages / 8 + (unsigned)group * 5u) % (unsigned)stages) : 0;
 }
 
 }  // namespace topoep_dev
