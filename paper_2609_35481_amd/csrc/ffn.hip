@@ -51,11 +51,11 @@ struct Ffn {
   float *sums;                // [parts, L, .., ..]: of a weights' gradient
 };
 
-__device__ inline int token_of(const Ffn &a, int row) {
-  if (!a.pairs) return row;
-  const uint32_t pair = (uint32_t)a.pairs[row];
-  return (int)(a.k == 1 ? pair : __umulhi(pair, a.per_token.m) >> (a.per_token.sh - 32));   // (fdiv's upper half)
+__device__ inline int token_of_pair(const Ffn &a, int pair) {
+  return a.k == 1 ? pair : (int)(__umulhi((uint32_t)pair, a.per_token.m) >> (a.per_token.sh - 32));   // (fdiv's upper half)
 }
+__device__ inline int pair_of_row(const Ffn &a, int row) { return a.pairs ? a.pairs[row] : row; }   // (dense: k = 1)
+__device__ inline int token_of(const Ffn &a, int row) { return token_of_pair(a, pair_of_row(a, row)); }
 __device__ inline float weight_of(const Ffn &a, int row) { return a.pairs ? a.weights[a.pairs[row]] : 1.0f; }
 
 // ---------------------------------------------------------------- forward
@@ -320,23 +320,25 @@ struct Tokens : AcrossPlaces<B, W> {
   const Ffn *a;
   const char *from;
   int64_t ld;                       // bytes
-  int first, token[At::kLoads];
+  int first, pair[At::kLoads];      // of the next stage's rows
   __device__ void start(const Ffn &of, Me me, const void *base, int64_t stride, int row, int c0, int n, int len) {
     const int c = c0 + At::column_of(me);
     a = &of, from = static_cast<const char *>(base) + (c < n ? c : 0) * 2, ld = stride * 2, first = row;
     if (len > 0) next(me, 0, len);
   }
+  // The pairs as they are: a token formed here would have to wait for them, and with them for
+  // every load before them (3.3 us a stage of a few experts' rows, and FIGURE).
   __device__ void next(Me me, int k, int n) {
 #pragma unroll
     for (int i = 0; i < At::kLoads; ++i) {
       const int at = k + At::row_of(i, me);
-      token[i] = token_of(*a, first + (at < n ? at : 0));
+      pair[i] = pair_of_row(*a, first + (at < n ? at : 0));
     }
   }
   __device__ void load(Lds *to, Me me, int k, int after, int n) {
 #pragma unroll
     for (int i = 0; i < At::kLoads; ++i) {
-      const char *p = from + token[i] * ld;
+      const char *p = from + token_of_pair(*a, pair[i]) * ld;
       to_lds(At::row_of(i, me) < n - k ? p : reinterpret_cast<const char *>(&kZeros), to + At::load_of(i, me.wave) * kApart);
     }
     next(me, after, n);
