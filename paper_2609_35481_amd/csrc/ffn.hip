@@ -54,8 +54,7 @@ struct Ffn {
 __device__ inline int token_of_pair(const Ffn &a, int pair) {
   return a.k == 1 ? pair : (int)(__umulhi((uint32_t)pair, a.per_token.m) >> (a.per_token.sh - 32));   // (fdiv's upper half)
 }
-__device__ inline int pair_of_row(const Ffn &a, int row) { return a.pairs ? a.pairs[row] : row; }   // (dense: k = 1)
-__device__ inline int token_of(const Ffn &a, int row) { return token_of_pair(a, pair_of_row(a, row)); }
+__device__ inline int token_of(const Ffn &a, int row) { return a.pairs ? token_of_pair(a, a.pairs[row]) : row; }
 __device__ inline float weight_of(const Ffn &a, int row) { return a.pairs ? a.weights[a.pairs[row]] : 1.0f; }
 
 // ---------------------------------------------------------------- forward
@@ -332,7 +331,7 @@ struct Tokens : AcrossPlaces<B, W> {
 #pragma unroll
     for (int i = 0; i < At::kLoads; ++i) {
       const int at = k + At::row_of(i, me);
-      pair[i] = pair_of_row(*a, first + (at < n ? at : 0));
+      pair[i] = a->pairs[first + (at < n ? at : 0)];
     }
   }
   __device__ void load(Lds *to, Me me, int k, int after, int n) {
@@ -348,34 +347,42 @@ struct Tokens : AcrossPlaces<B, W> {
 // dup[g][r][c] = sum over the group's rows of da[m][r] x[token][c] (Down false), ddown[g][r][c] of
 // dout[token][r] h[m][c] (Down true).  `parts` workgroups share a group's rows where there are few
 // tiles, each with sums of its own in a.sums.
-template <class S, bool Down>
-__global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a, int parts) {
+//
+// A group's tiles (and parts) go to `xcds` 64Ds, groups in turn: an L2 that has few tiles of every group reads
+// most of their operands, and those that miss it take 2.5 us a stage (128 experts of 48 tiles: 466 us, FIGURE).
+template <class S, bool Down, bool Routed>
+__global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a, int parts, int xcds) {
   typedef typename S::T T;
   TOPOEP_STAGES(S);
   const Me me;
   const int cols = Down ? a.I : a.H, rows = Down ? a.H : 2 * a.I;
   const int np = (cols + S::BP - 1) / S::BP, nq = (rows + S::BQ - 1) / S::BQ;
-  const int part = blockIdx.x / (np * nq) % parts, g = blockIdx.x / (np * nq) / parts;
+  const int all = np * nq * parts, each_xcd = (all + xcds - 1) / xcds, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+  const int turn = slot / each_xcd, g = turn * (8 / xcds) + xcd / xcds, tile = xcd % xcds * each_xcd + slot - turn * each_xcd;
+  if (g >= a.L || tile >= all) return;
+  const int part = tile / (np * nq);
   int tq, tp, first, end;
-  place_of(by_xcd(blockIdx.x % (np * nq), np * nq), nq, np, tq, tp);
+  place_of(tile - part * np * nq, nq, np, tq, tp);
   rows_of(a.offsets, a.rows, g, first, end);
   const int each = ((end - first + parts - 1) / parts + S::kStage - 1) / S::kStage * S::kStage;
   first = imin(first + part * each, end);
   const int n = imin(each, end - first);
   typename S::Sum d[S::TP][S::TQ] = {};
-  const auto run = [&](auto &p, auto &q) { multiply<S>(p, q, me, n, 0, p0, p1, q0, q1, d); };
+  constexpr int B = Down ? S::BQ : S::BP;
+  typename std::conditional<Routed, Tokens<T, B, S::kWaves>, Across<T, B, S::kWaves>>::type tokens;
+  const void *const from = Down ? a.dout : a.x;
+  const int64_t ld = Down ? a.H : a.ldx;
+  const int c0 = Down ? tq * S::BQ : tp * S::BP;
+  if constexpr (Routed) tokens.start(a, me, from, ld, first, c0, a.H, n);
+  else tokens.start(me, static_cast<const T *>(from) + first * ld, ld, c0, a.H);
   if constexpr (Down) {
     Across<T, S::BP, S::kWaves> p;
-    Tokens<T, S::BQ, S::kWaves> q;
     p.start(me, static_cast<const T *>(a.h) + (int64_t)first * a.I, a.I, tp * S::BP, a.I);
-    q.start(a, me, a.dout, a.H, first, tq * S::BQ, a.H, n);
-    run(p, q);
+    multiply<S>(p, tokens, me, n, 0, p0, p1, q0, q1, d);
   } else {
-    Tokens<T, S::BP, S::kWaves> p;
     Across<T, S::BQ, S::kWaves> q;
-    p.start(a, me, a.x, a.ldx, first, tp * S::BP, a.H, n);
     q.start(me, static_cast<const T *>(a.da) + (int64_t)first * 2 * a.I, 2 * a.I, tq * S::BQ, 2 * a.I);
-    run(p, q);
+    multiply<S>(tokens, q, me, n, 0, p0, p1, q0, q1, d);
   }
   void *const to = Down ? a.ddown : a.dup;
   const int64_t at = ((int64_t)part * a.L + g) * rows;
@@ -546,7 +553,13 @@ int enqueue_hidden(const Ffn &a, hipStream_t st) {
 
 template <class S, bool Down>
 int enqueue_grad_of(const Ffn &a, int64_t tiles, int parts, hipStream_t st) {
-  hipLaunchKernelGGL((grad_kernel<S, Down>), dim3((unsigned)(tiles * parts)), dim3(S::kThreads), 0, st, a, parts);
+  // 64Ds of a group: 32 tiles for each, which its CUs take at once; all where there are few groups
+  const int64_t all = tiles / a.L * parts;
+  int xcds = 1;
+  while (xcds < 8 && (all >= 24 * xcds || a.L * 2 < 8 / xcds * 4)) xcds *= 2;
+  const int64_t blocks = 8 * ceil_of(all, xcds) * ceil_of(a.L, 8 / xcds);
+  if (a.pairs) hipLaunchKernelGGL((grad_kernel<S, Down, true>), dim3((unsigned)blocks), dim3(S::kThreads), 0, st, a, parts, xcds);
+  else hipLaunchKernelGGL((grad_kernel<S, Down, false>), dim3((unsigned)blocks), dim3(S::kThreads), 0, st, a, parts, xcds);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 template <class T, bool Down>
