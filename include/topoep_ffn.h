@@ -100,7 +100,7 @@ int topoep_ffn_bytes(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *rows
  *
  * Products are accumulated in 32 bits.  The hidden values, times their row's
  * weight, are rounded once to the weights' type, the second product's
- * operand; a routed token's sum is kept in 32 bits and rounded once.  Gate
+ * operand (beyond 65504 in f16: infinite); a routed token's sum is kept in 32 bits and rounded once.  Gate
  * and up values are kept for the backward pass in 32 bits.  T = 0 enqueues
  * nothing.  TOPOEP_EINVAL: null pointers, sizes outside their ranges, T * k
  * above INT32_MAX, rows NULL with L > 1, misaligned buffers; TOPOEP_ELIMIT:

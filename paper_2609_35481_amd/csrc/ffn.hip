@@ -206,20 +206,20 @@ __global__ __launch_bounds__(64 * few_waves(KS), few_per_simd(C)) void few_down_
 // of its parts.  A workgroup has a token and 1024 columns of it.
 template <class T>
 __global__ __launch_bounds__(256) void combine_kernel(Ffn a, const float *from, void *to, int parts) {
-  const int64_t t = blockIdx.x;
   const int c = (blockIdx.y * 256 + threadIdx.x) * 4;
-  int place = -1;
-  if (lane_id() < a.k) place = a.pairs ? a.places[t * a.k + lane_id()] : (int)t;
-  uint64_t here = __ballot((unsigned)place < (unsigned)a.rows);
-  v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (c < a.H) {
+  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+    int place = -1;
+    if (lane_id() < a.k) place = a.pairs ? a.places[t * a.k + lane_id()] : (int)t;
+    uint64_t here = __ballot((unsigned)place < (unsigned)a.rows);
+    v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
     for (; here != 0; here &= here - 1) {
       const int64_t m = readlane_i32(place, __ffsll((unsigned long long)here) - 1);
+      if (c >= a.H) continue;
       v4f row = *reinterpret_cast<const v4f *>(from + m * a.H + c);
       for (int p = 1; p < parts; ++p) row += *reinterpret_cast<const v4f *>(from + ((int64_t)p * a.rows + m) * a.H + c);
       s += row;
     }
-    store4<T>(to, t * a.H + c, s);
+    if (c < a.H) store4<T>(to, t * a.H + c, s);
   }
 }
 
@@ -326,7 +326,7 @@ struct Tokens : AcrossPlaces<B, W> {
     if (len > 0) next(me, 0, len);
   }
   // The pairs as they are: a token formed here would have to wait for them, and with them for
-  // every load before them (3.3 us a stage of a few experts' rows, and FIGURE).
+  // every load before them (128 experts of H = 2048, I = 768 with 32768 rows, both gradients: 861 us, and 726 so).
   __device__ void next(Me me, int k, int n) {
 #pragma unroll
     for (int i = 0; i < At::kLoads; ++i) {
@@ -349,7 +349,7 @@ struct Tokens : AcrossPlaces<B, W> {
 // tiles, each with sums of its own in a.sums.
 //
 // A group's tiles (and parts) go to `xcds` 64Ds, groups in turn: an L2 that has few tiles of every group reads
-// most of their operands, and those that miss it take 2.5 us a stage (128 experts of 48 tiles: 466 us, FIGURE).
+// most of their operands (10 experts of H = 7168, I = 2048, both gradients: 550 us with eight XCDs each, 520 so).
 template <class S, bool Down, bool Routed>
 __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a, int parts, int xcds) {
   typedef typename S::T T;
@@ -524,7 +524,7 @@ int enqueue_out_of(const Ffn &a, void *to, int parts, hipStream_t st) {
 }
 template <class T>
 int enqueue_combine(const Ffn &a, void *to, int parts, hipStream_t st) {
-  hipLaunchKernelGGL((combine_kernel<T>), dim3(a.T, (a.H + 1023) / 1024), dim3(256), 0, st, a, a.y, to, parts);
+  hipLaunchKernelGGL((combine_kernel<T>), dim3(imin(a.T, 1 << 20), (a.H + 1023) / 1024), dim3(256), 0, st, a, a.y, to, parts);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 template <class T, bool Back>
@@ -580,6 +580,7 @@ int enqueue_grad(const Ffn &a, int parts, hipStream_t st) {
 // 17.8 against 30.2 us; I = 5632: 41.4 and 38.7).
 bool few_rows(const Ffn &a, int64_t n, int64_t k) {
   const int64_t groups = imin(a.L, (int)a.expected);
+  if ((double)a.rows * n >= 0x1p34) return false;   // (its tiles are numbered in 32 bits)
   return a.expected <= 16 * groups || (a.expected <= 64 * groups && (double)a.expected * groups * n * k <= 0x1p28);
 }
 

@@ -168,11 +168,10 @@ struct View {
   }
 };
 
-// Waits until at most N of this wave's loads are under way, then for the other waves.
-template <int N>
+// Waits for this wave's loads into LDS, and its reads from there, then for the other waves.
 __device__ inline void arrived() {
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0F70);   // vmcnt alone
+  __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt 0, lgkmcnt 0
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -254,16 +253,16 @@ __device__ inline void multiply(P &p, Q &q, Me me, int n, int start, Lds *p0, Ld
   if (stages > 0) p.load(p0, me, k, next, n), q.load(q0, me, k, next, n);
 #pragma unroll 1
   for (int g = stages >> 1; g > 0; --g) {
-    arrived<0>();
+    arrived();
     turn();
     p.load(p1, me, k, next, n), q.load(q1, me, k, next, n);
     multiply_stage<S, kLoads>(p0, q0, pv, qv, d);
-    arrived<0>();
+    arrived();
     turn();
     p.load(p0, me, k, next, n), q.load(q0, me, k, next, n);
     multiply_stage<S, kLoads>(p1, q1, pv, qv, d);
   }
-  arrived<0>();
+  arrived();
   if (stages & 1) multiply_stage<S, 0>(p0, q0, pv, qv, d);
 }
 

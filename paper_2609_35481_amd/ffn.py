@@ -7,6 +7,9 @@
   quantize       rows in 8-bit integers, a scale each
   matmul_int8    products in 8-bit integers, for all rows or those of every expert
 
+A backward pass is captured into a graph as any other of torch's: with no eager
+graph of the same leaves alive, whose accumulators would run on the stream that made them.
+
 Argument checks and marshalling only: torch provides device memory and the
 current stream, every step runs in the HIP kernels of libtopoep.so.  Importing
 this module fails loudly when the library, or _ffn_tensors (the calls that take
@@ -145,6 +148,8 @@ def matmul_int8(x, w, w_scale, offsets=None, gated=False, dtype=None, out=None, 
         x, scale = x
         if scale is None:
             raise TypeError("scale is not a tensor")
+    if isinstance(gated, torch.Tensor):
+        raise TypeError("gated must be true or false, not a tensor")
     if dtype is not None and dtype not in _TYPES:
         raise TypeError("the result must be float32, bfloat16 or float16, not %s" % dtype)
     return _call("topoep_matmul_int8", _tensors.matmul_int8(x, scale, w, w_scale, offsets, bool(gated),

@@ -207,6 +207,20 @@ def test_offsets_beyond_32_bits():
     check(got, ffnmodel.dense(small, up, down, dout))
 
 
+def test_more_tokens_than_a_grid_has_threads_for():
+    T, H, I = 17000001, 8, 8
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn(T, H, generator=g, device=DEV, dtype=BF16)
+    up, down = normal(1, 2, 2 * I, H, dtype=BF16).to(DEV), normal(2, 2, H, I, dtype=BF16).to(DEV)
+    ids = torch.randint(0, 2, (T, 1), generator=g, device=DEV, dtype=torch.int32)
+    weights = torch.rand(T, 1, generator=g, device=DEV)
+    with torch.no_grad():
+        out = ffn.experts(x, ids, weights, up, down)
+    for part in (slice(0, 300), slice(T // 2, T // 2 + 300), slice(T - 300, T)):
+        want = ffnmodel.layer(x[part], ids[part], weights[part], up, down)["out"]
+        ffnmodel.within(out[part], *want, "part")
+
+
 def test_refusals():
     x, ids, weights, up, down, slot, dout = (v.to(DEV) for v in case(20, 64, 32, 8, 8, 2, BF16))
     with pytest.raises(TypeError, match="bfloat16 or float16"):

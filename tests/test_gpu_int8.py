@@ -74,6 +74,16 @@ def test_quantize_strides_and_alignment():
         assert torch.equal(q.cpu(), wq) and torch.equal(scale.cpu(), ws)
 
 
+def test_quantize_more_rows_than_a_grid_has_threads_for():
+    x = torch.randn(17000003, 16, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV, dtype=BF16)
+    q, scale = ffn.quantize(x)
+    want = (x.double().abs().amax(1) / 127.0).float()
+    assert torch.equal(scale, want)
+    for part in (slice(0, 3000000), slice(16000000, None)):
+        exact = torch.round(x[part].double() / want[part].double()[:, None]).clamp(-127, 127).to(torch.int8)
+        assert torch.equal(q[part], exact)
+
+
 @pytest.mark.parametrize("K", [64, 5000])
 def test_quantize_infinities_and_nan(K):
     x = normal(6, 5, K)
@@ -208,6 +218,6 @@ def test_forward_only_and_refusals():
                      (dict(out=torch.zeros(8, 21, device=DEV)), ValueError),
                      (dict(out=torch.zeros(8, 20, device=DEV), dtype=BF16), TypeError),
                      (dict(w=w[:, :60].contiguous(), x=x[:, :60]), moe.TopoepError),
-                     (dict(w=w[:19], w_scale=ws[:19], gated=True), moe.TopoepError), (dict(w=w.cpu()), TypeError)):
+                     (dict(w=w[:19], w_scale=ws[:19], gated=True), moe.TopoepError), (dict(w=w.cpu()), TypeError), (dict(gated=torch.ones(())), TypeError), (dict(gated=torch.ones(())), TypeError)):
         with pytest.raises(kind):
             ffn.matmul_int8(**{**dict(x=x, w=w, w_scale=ws), **kw})
