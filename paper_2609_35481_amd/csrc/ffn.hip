@@ -84,7 +84,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void up_kernel(Ffn a) {
     });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, me, a.H, start_of<S>(a.H, s.group), p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, a.H, start_of<S>(a.H, s.group), lds, d);
 #pragma unroll
     for (int j = 0; j < S::TQ; ++j) {
       const int m = s.first + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void out_kernel(Ffn a, void *to, in
     q.start(me, [&](int r) { return reinterpret_cast<const char *>(rows + (int64_t)imin(s.first + r, s.end - 1) * n); });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, me, imin(each, n - k0), start_of<S>(imin(each, n - k0), s.group), p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, imin(each, n - k0), start_of<S>(imin(each, n - k0), s.group), lds, d);
     const bool whole = !a.pairs && parts == 1;
     const int64_t at = (int64_t)part * a.rows * a.H;
 #pragma unroll
@@ -243,9 +243,9 @@ __global__ __launch_bounds__(S::kThreads, 2) void hidden_kernel(Ffn a) {
     });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, me, a.H, start_of<S>(a.H, s.group), p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, a.H, start_of<S>(a.H, s.group), lds, d);
     __syncthreads();   // the stages are read: sums go where they were
-    __attribute__((address_space(3))) float *sums = (__attribute__((address_space(3))) float *)p0;   // [NP, BQ]
+    __attribute__((address_space(3))) float *sums = (__attribute__((address_space(3))) float *)lds.p[0];   // [NP, BQ]
 #pragma unroll
     for (int j = 0; j < S::TQ; ++j) {
       const int col = (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15), m = s.first + col;
@@ -378,11 +378,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a, int parts, 
   if constexpr (Down) {
     Across<T, S::BP, S::kWaves> p;
     p.start(me, static_cast<const T *>(a.h) + (int64_t)first * a.I, a.I, tp * S::BP, a.I);
-    multiply<S>(p, tokens, me, n, 0, p0, p1, q0, q1, d);
+    multiply<S>(p, tokens, me, n, 0, lds, d);
   } else {
     Across<T, S::BQ, S::kWaves> q;
     q.start(me, static_cast<const T *>(a.da) + (int64_t)first * 2 * a.I, 2 * a.I, tq * S::BQ, 2 * a.I);
-    multiply<S>(tokens, q, me, n, 0, p0, p1, q0, q1, d);
+    multiply<S>(tokens, q, me, n, 0, lds, d);
   }
   void *const to = Down ? a.ddown : a.dup;
   const int64_t at = ((int64_t)part * a.L + g) * rows;

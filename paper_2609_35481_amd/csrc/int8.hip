@@ -216,7 +216,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void int8_kernel(Int8 a) {
     q.start(me, [&](int r) { return reinterpret_cast<const char *>(a.q) + imin(s.first + r, s.end - 1) * a.ldq + k0; });
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
-    multiply<S>(p, q, me, imin(each, a.K - k0), start_of<S>(imin(each, a.K - k0), s.group), p0, p1, q0, q1, d);
+    multiply<S>(p, q, me, imin(each, a.K - k0), start_of<S>(imin(each, a.K - k0), s.group), lds, d);
     if (a.parts > 1) {
 #pragma unroll
       for (int j = 0; j < S::TQ; ++j) {

@@ -74,10 +74,10 @@ __device__ inline int find_tile(const int32_t *offsets, int rows, int groups, in
 
 // Static LDS of a product: two stages of each operand, variables of their own, so
 // that the compiler sees that a stage's reads do not wait for the other's loads.
-#define TOPOEP_STAGES(S)                                                                 \
-  __shared__ v4i stage_p0[S::kBytesP / 16], stage_p1[S::kBytesP / 16];                   \
-  __shared__ v4i stage_q0[S::kBytesQ / 16], stage_q1[S::kBytesQ / 16];                   \
-  Lds *const p0 = (Lds *)stage_p0, *const p1 = (Lds *)stage_p1, *const q0 = (Lds *)stage_q0, *const q1 = (Lds *)stage_q1
+#define TOPOEP_STAGES(S)                                                                                  \
+  __shared__ v4i stage_p0[S::kBytesP / 16], stage_p1[S::kBytesP / 16], stage_p2[S::kDeep ? S::kBytesP / 16 : 1]; \
+  __shared__ v4i stage_q0[S::kBytesQ / 16], stage_q1[S::kBytesQ / 16];                                    \
+  const Stages lds = {{(Lds *)stage_p0, (Lds *)stage_p1, S::kDeep ? (Lds *)stage_p2 : nullptr}, {(Lds *)stage_q0, (Lds *)stage_q1}}
 
 // Four neighbours, rounded to nearest even.
 template <class T>

@@ -13,6 +13,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "router.h"
 
 namespace topoep_dev {
@@ -168,10 +170,12 @@ struct View {
   }
 };
 
-// Waits for this wave's loads into LDS, and its reads from there, then for the other waves.
+// Waits until at most N of this wave's loads into LDS are under way, and for its reads from there, then
+// for the other waves.
+template <int N>
 __device__ inline void arrived() {
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt 0, lgkmcnt 0
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0070);   // vmcnt N, lgkmcnt 0
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -186,6 +190,7 @@ struct Shape {
   static constexpr bool PA = PA_, QA = QA_;
   static constexpr int TP = BP / NP / 16, TQ = BQ / NQ / 16;
   static constexpr int kStage = PA ? kAcross : kLine / (int)sizeof(T);
+  static constexpr bool kDeep = !PA;                     // three stages of P in LDS, not two
   static constexpr int kBytesP = PA ? AcrossPlaces<BP, kWaves>::kBytes : BP * kLine;
   static constexpr int kBytesQ = QA ? AcrossPlaces<BQ, kWaves>::kBytes : BQ * kLine;
   typedef typename Mul<T>::Sum Sum;
@@ -215,6 +220,9 @@ __device__ inline void stage_order() {
   }
 }
 
+// LDS of the stages.
+struct Stages { Lds *p[3], *q[2]; };
+
 template <class S, int Loads>
 __device__ inline void multiply_stage(const Lds *ps, const Lds *qs, const typename S::PView &pv, const typename S::QView &qv,
                                       typename S::Sum (&d)[S::TP][S::TQ]) {
@@ -233,37 +241,86 @@ __device__ inline void multiply_stage(const Lds *ps, const Lds *qs, const typena
   stage_order<S, Loads>();
 }
 
-// d += P Q over the n elements of the inner axis, from stage `start` on and round: one stage is multiplied
-// while the next one is on its way.  Every wave is done with a stage's LDS when the next barrier
-// lets loads into it.
+// The first element of the next stage to load: from stage `start` on and round, behind the last one n
+// (zeros).
+template <int Stage>
+struct Cursor {
+  int k, left, n;
+  __device__ Cursor(int n_, int start) : k(start * Stage), left((n_ + Stage - 1) / Stage), n(n_) {}
+  __device__ int after() const { return left > 1 ? (k + Stage < n ? k + Stage : 0) : n; }
+  template <class O>
+  __device__ void load(O &o, Lds *to, Me me) {
+    const int next = after();
+    o.load(to, me, k, next, n);
+    k = next;
+    --left;
+  }
+};
+
+// d += P Q over the n elements of the inner axis: one stage is multiplied while the next one is on its
+// way, of P (weights, from memory) by rows the one after it too.  Every wave is done with a stage's LDS when the
+// next barrier lets loads into it.
 template <class S, class P, class Q>
-__device__ inline void multiply(P &p, Q &q, Me me, int n, int start, Lds *p0, Lds *p1, Lds *q0, Lds *q1,
-                                typename S::Sum (&d)[S::TP][S::TQ]) {
+__device__ inline void multiply(P &p, Q &q, Me me, int n, int start, const Stages &lds, typename S::Sum (&d)[S::TP][S::TQ]) {
   constexpr int kLoads = P::kLoads + Q::kLoads;
   const typename S::PView pv(me.wave % S::NP * S::TP * 16, me.lane);
   const typename S::QView qv(me.wave / S::NP * S::TQ * 16, me.lane);
   const int stages = (n + S::kStage - 1) / S::kStage;
-  // the stage after next; behind the last one: zeros
-  int left = stages, k = start * S::kStage, next = k;
-  const auto turn = [&] {
-    k = next;
-    next = --left > 0 ? (next + S::kStage < n ? next + S::kStage : 0) : n;
-  };
-  turn();
-  if (stages > 0) p.load(p0, me, k, next, n), q.load(q0, me, k, next, n);
+  Cursor<S::kStage> kp(n, start);
+  if constexpr (!S::kDeep) {
+    // (P's loads first: the other order takes 5 to 10 % longer)
+    const auto load = [&](int i) {
+      const int next = kp.after();
+      p.load(lds.p[i], me, kp.k, next, n), q.load(lds.q[i], me, kp.k, next, n);
+      kp.k = next;
+      --kp.left;
+    };
+    if (stages > 0) load(0);
 #pragma unroll 1
-  for (int g = stages >> 1; g > 0; --g) {
-    arrived();
-    turn();
-    p.load(p1, me, k, next, n), q.load(q1, me, k, next, n);
-    multiply_stage<S, kLoads>(p0, q0, pv, qv, d);
-    arrived();
-    turn();
-    p.load(p0, me, k, next, n), q.load(q0, me, k, next, n);
-    multiply_stage<S, kLoads>(p1, q1, pv, qv, d);
+    for (int g = stages >> 1; g > 0; --g) {
+      arrived<0>();
+      load(1);
+      multiply_stage<S, kLoads>(lds.p[0], lds.q[0], pv, qv, d);
+      arrived<0>();
+      load(0);
+      multiply_stage<S, kLoads>(lds.p[1], lds.q[1], pv, qv, d);
+    }
+    arrived<0>();
+    if (stages & 1) multiply_stage<S, 0>(lds.p[0], lds.q[0], pv, qv, d);
+  } else {
+    Cursor<S::kStage> kq(n, start);
+    if (stages > 0) {
+      kp.load(p, lds.p[0], me);
+      kq.load(q, lds.q[0], me);
+      __builtin_amdgcn_sched_barrier(0);
+      kp.load(p, lds.p[1], me);
+    }
+    const auto stage = [&](auto i) {
+      constexpr int I = decltype(i)::value;
+      arrived<P::kLoads>();
+      kq.load(q, lds.q[(I + 1) % 2], me);
+      // (the loads that a wait leaves under way are the last ones: nothing from memory passes here)
+      __builtin_amdgcn_sched_barrier(0x78F);
+      kp.load(p, lds.p[(I + 2) % 3], me);
+      multiply_stage<S, kLoads>(lds.p[I % 3], lds.q[I % 2], pv, qv, d);
+    };
+    int g = stages;
+#pragma unroll 1
+    for (; g >= 6; g -= 6) {
+      stage(std::integral_constant<int, 0>());
+      stage(std::integral_constant<int, 1>());
+      stage(std::integral_constant<int, 2>());
+      stage(std::integral_constant<int, 3>());
+      stage(std::integral_constant<int, 4>());
+      stage(std::integral_constant<int, 5>());
+    }
+    if (g > 0) stage(std::integral_constant<int, 0>());
+    if (g > 1) stage(std::integral_constant<int, 1>());
+    if (g > 2) stage(std::integral_constant<int, 2>());
+    if (g > 3) stage(std::integral_constant<int, 3>());
+    if (g > 4) stage(std::integral_constant<int, 4>());
+    arrived<0>();
   }
-  arrived();
-  if (stages & 1) multiply_stage<S, 0>(p0, q0, pv, qv, d);
 }
 
 // The stage a workgroup starts with.  Rows lie multiples of some kilobytes apart: workgroups that read the
