@@ -85,11 +85,15 @@ __global__ __launch_bounds__(S::kThreads, 2) void up_kernel(Ffn a) {
     typename S::Sum d[S::TP][S::TQ] = {};
     __syncthreads();
     multiply<S>(p, q, me, a.H, start_of<S>(a.H, s.group), lds, d);
+    float weights[S::TQ];   // (pairs, then weights: two readings deep, of all columns at once)
+#pragma unroll
+    for (int j = 0; j < S::TQ; ++j)
+      weights[j] = weight_of(a, imin(s.first + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15), s.end - 1));
 #pragma unroll
     for (int j = 0; j < S::TQ; ++j) {
       const int m = s.first + (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15);
       if (m >= s.end) continue;
-      const float weight = weight_of(a, m);
+      const float weight = weights[j];
       const int first = unit0 + me.wave % S::NP * kWaveUnits;
       store_rows<T>(me, kHalf, static_cast<T *>(a.h) + (int64_t)m * a.I, first, a.I, [&](int i) {
         const v4f g = d[i][j], u = d[i + kHalf][j];
@@ -246,47 +250,59 @@ __global__ __launch_bounds__(S::kThreads, 2) void hidden_kernel(Ffn a) {
     multiply<S>(p, q, me, a.H, start_of<S>(a.H, s.group), lds, d);
     __syncthreads();   // the stages are read: sums go where they were
     __attribute__((address_space(3))) float *sums = (__attribute__((address_space(3))) float *)lds.p[0];   // [NP, BQ]
+    // g and u of a pair of tiles, read two pairs ahead where 64 registers hold d (301 tokens, two experts each of 16,
+    // H = 520, I = 248: 16.3 us, and 20.0 where each pair waited for its own). 128 registers of d leave none for
+    // another pair (8192 rows, H = 4096, I = 14336: 1.04 ms; one pair ahead, 17 registers in scratch: 1.07).
+    constexpr int kPairs = S::TP / 2, kAll = kPairs * S::TQ, kHeld = S::TP * S::TQ > 16 ? 1 : 3;
+    const int first = tp * S::BP + me.wave % S::NP * S::TP * 16, quad = (me.lane >> 4) * 4;
+    const int col0 = me.wave / S::NP * S::TQ * 16 + (me.lane & 15);
+    float weight[S::TQ], sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < S::TQ; ++j) {
-      const int col = (me.wave / S::NP * S::TQ + j) * 16 + (me.lane & 15), m = s.first + col;
-      float sum = 0.0f;
-      if (m < s.end) {
-        const float weight = weight_of(a, m);
-        const int first = tp * S::BP + me.wave % S::NP * S::TP * 16;
-        T *const to = static_cast<T *>(a.da) + (int64_t)m * 2 * a.I;
+    for (int j = 0; j < S::TQ; ++j) weight[j] = weight_of(a, imin(s.first + col0 + j * 16, s.end - 1));
+    v4f g[kHeld][2], u[kHeld][2];
+    const auto fetch = [&](int n) {
+      const int64_t row = imin(s.first + col0 + n / kPairs * 16, s.end - 1);
 #pragma unroll
-        for (int i = 0; i < S::TP; i += 2) {
-          __builtin_amdgcn_sched_barrier(0);   // (all tiles' values loaded at once: scratch)
-          v4f dg[2], du[2];
+      for (int t = 0; t < 2; ++t) {
+        const float *from = a.gu + row * 2 * a.I + imin(first + (n % kPairs * 2 + t) * 16 + quad, a.I - 4);
+        g[n % kHeld][t] = *reinterpret_cast<const v4f *>(from);
+        u[n % kHeld][t] = *reinterpret_cast<const v4f *>(from + a.I);
+      }
+    };
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const int unit = first + (i + t) * 16 + (me.lane >> 4) * 4;
-            v4f g = {}, u = {};
-            if (unit < a.I) {
-              const float *from = a.gu + (int64_t)m * 2 * a.I + unit;
-              g = *reinterpret_cast<const v4f *>(from);
-              u = *reinterpret_cast<const v4f *>(from + a.I);
-            }
+    for (int n = 0; n < kHeld - 1 && n < kAll; ++n) fetch(n);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float sg = sigmoid(g[e]), act = g[e] * sg, dh = d[i + t][j][e];
-              sum += unit < a.I ? dh * (act * u[e]) : 0.0f;
-              dg[t][e] = weight * (dh * u[e] * (sg + act * (1.0f - sg)));
-              du[t][e] = weight * (dh * act);
-            }
-          }
-          const v4i og = pair_of<T>(dg[0], dg[1]), ou = pair_of<T>(du[0], du[1]);
-          const int unit = first + i * 16 + pair_column(me);
-          if (unit < a.I) {
-            *reinterpret_cast<v4i *>(to + unit) = og;
-            *reinterpret_cast<v4i *>(to + a.I + unit) = ou;
-          }
+    for (int n = 0; n < kAll; ++n) {
+      const int j = n / kPairs, i = n % kPairs * 2, m = s.first + col0 + j * 16;
+      if (n + kHeld - 1 < kAll) fetch(n + kHeld - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      v4f dg[2], du[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bool in = first + (i + t) * 16 + quad < a.I;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float gate = g[n % kHeld][t][e], up = u[n % kHeld][t][e];
+          const float sg = sigmoid(gate), act = gate * sg, dh = d[i + t][j][e];
+          sum += in ? dh * (act * up) : 0.0f;
+          dg[t][e] = weight[j] * (dh * up * (sg + act * (1.0f - sg)));
+          du[t][e] = weight[j] * (dh * act);
         }
       }
-      if (a.dw) {
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        if (me.lane < 16) sums[me.wave % S::NP * S::BQ + col] = sum;
+      const v4i og = pair_of<T>(dg[0], dg[1]), ou = pair_of<T>(du[0], du[1]);
+      const int unit = first + i * 16 + pair_column(me);
+      if (m < s.end && unit < a.I) {
+        T *const to = static_cast<T *>(a.da) + (int64_t)m * 2 * a.I + unit;
+        *reinterpret_cast<v4i *>(to) = og;
+        *reinterpret_cast<v4i *>(to + a.I) = ou;
+      }
+      if (i == S::TP - 2) {
+        if (a.dw) {
+          sum += __shfl_xor(sum, 16);
+          sum += __shfl_xor(sum, 32);
+          if (me.lane < 16) sums[me.wave % S::NP * S::BQ + col0 + j * 16] = sum;
+        }
+        sum = 0.0f;
       }
     }
     if (a.dw) {

@@ -74,12 +74,11 @@ struct Me {
 // every bank once.
 template <class T, int B, int W>
 struct ByRows {
-  static constexpr int kBytes = B * kLine;
-  static constexpr int kPieces = B / 8;                  // a wave's load is 8 rows
-  static constexpr int kLoads = (kPieces + W - 1) / W;   // (too few for all waves: some bring the same)
+  static constexpr int kLoads = B / 8 / W;   // a wave's load is 8 rows
+  static_assert(kLoads * W * 8 == B, "every wave as many");
   const char *from[kLoads];
 
-  static __device__ int load_of(int i, int wave) { return (i * W + wave) % kPieces; }
+  static __device__ int load_of(int i, int wave) { return i * W + wave; }
   static __device__ int row_of(int i, Me me) { return load_of(i, me.wave) * 8 + (me.lane >> 3); }
   static __device__ int piece_of(Me me) { return (me.lane & 7) ^ (me.lane >> 3); }
 
@@ -100,21 +99,22 @@ struct ByRows {
 
 // An operand across: 64 rows of k a stage, B elements of 16 bits each.  A transposing read takes, of
 // 16 elements, the rows 8 b + 4 h + r (+ 32 s): b = 0..3 by the lane's block of 16, r = 0..3 inside it, h and
-// s one read each.  A wave's load holds rows that no read takes together (h, for narrower rows s and b's
-// upper bit too), and loads lie 32 bytes more than their 1 KiB apart: a read's rows meet every
-// bank once, and every place is one lane's base and a constant.
+// s one read each.  A wave's load holds rows that no read takes together (h, for narrower rows s too),
+// and loads lie 32 bytes more than their 1 KiB apart: a read's rows meet every bank once, and every
+// place is one lane's base and a constant (turned places, as for rows, take a base a tile: spills).
 constexpr int kApart = 1024 + 32;
 template <int B, int W>
 struct AcrossPlaces {
-  static constexpr int kRowPieces = B / 8, kRows = 64 / kRowPieces;   // pieces of 16 bytes a row, rows a load
-  static constexpr int kPieces = 64 / kRows, kBytes = kPieces * kApart;
-  static constexpr int kLoads = (kPieces + W - 1) / W;
-  static __device__ int load_of(int i, int wave) { return (i * W + wave) % kPieces; }
+  static_assert(B == 128 || B == 256, "four or two rows a load");
+  static constexpr int kRowPieces = B / 8, kPieces = B / 8;   // of 16 bytes in a row; loads of a stage
+  static constexpr int kBytes = kPieces * kApart, kLoads = kPieces / W;
+  static_assert(kLoads * W == kPieces, "every wave as many");
+  static __device__ int load_of(int i, int wave) { return i * W + wave; }
   // The row of k of load j (the same for all lanes) and what the lane adds to it.
-  static __device__ int row_of_load(int j) { return (j & 3) + (j >> 2 & (B == 64 ? 1 : 3)) * 8 + (B == 256 ? j >> 4 : 0) * 32; }
+  static __device__ int row_of_load(int j) { return (j & 3) + (j >> 2 & 3) * 8 + (B == 256 ? j >> 4 : 0) * 32; }
   static __device__ int row_of_lane(Me me) {
     const int sub = me.lane / kRowPieces;
-    return (sub & 1) * 4 + (B < 256 ? sub >> 1 & 1 : 0) * 32 + (B == 64 ? sub >> 2 : 0) * 16;
+    return (sub & 1) * 4 + (B == 128 ? sub >> 1 : 0) * 32;
   }
   static __device__ int column_of(Me me) { return me.lane % kRowPieces * 8; }
   static __device__ int row_of(int i, Me me) { return row_of_load(load_of(i, me.wave)) + row_of_lane(me); }
@@ -154,7 +154,7 @@ struct View {
     } else {
       // lanes 4 r .. 4 r + 3 of a block of 16 read row r's 32 bytes
       const int b = l >> 4, r = l >> 2 & 3;
-      at[0] = ((B == 64 ? b & 1 : b) * 4 + r) * kApart + (B == 64 ? b >> 1 : 0) * 512 + row0 * 2 + (l & 3) * 8;
+      at[0] = (b * 4 + r) * kApart + row0 * 2 + (l & 3) * 8;
     }
   }
   __device__ v4i get(const Lds *from, int tile, int s) const {
@@ -198,9 +198,6 @@ struct Shape {
   typedef View<T, BQ, QA> QView;
 };
 
-#ifndef VAR
-#define VAR 1
-#endif
 // The order of a stage's instructions, which the compiler would leave to itself with
 // the next stage's loads last: operands are read from LDS two groups of matrix
 // instructions ahead, loads spread over the first groups (8192^3 in bf16, 256 x 256 tiles:
@@ -213,7 +210,7 @@ __device__ inline void stage_order() {
     constexpr int loads = Loads - G * S::Ahead < S::Ahead ? Loads - G * S::Ahead : S::Ahead;
     if constexpr (loads > 0) __builtin_amdgcn_sched_group_barrier(0x20, loads, 0);
     __builtin_amdgcn_sched_group_barrier(0x8, S::TQ, 0);
-    constexpr int kEarly = S::TP > 2 ? S::TP - 2 : 1;   // groups before which the second half's Q is read
+    constexpr int kEarly = S::TP - 2;   // groups before which the second half's Q is read
     constexpr int reads = (G + 2 < kGroups ? RP : 0) + (G < kEarly ? (S::TQ * RQ + kEarly - 1) / kEarly : 0);
     if constexpr (reads > 0) __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);
     stage_order<S, Loads, G + 1>();
@@ -258,8 +255,14 @@ struct Cursor {
 };
 
 // d += P Q over the n elements of the inner axis: one stage is multiplied while the next one is on its
-// way, of P (weights, from memory) by rows the one after it too.  Every wave is done with a stage's LDS when the
-// next barrier lets loads into it.
+// way, of P (weights, from memory) by rows the one after it too, which fills the 160 KB of LDS (64 rows, H = 4096, I
+// = 11008: 91 against 64 us).  Every wave is done with a stage's LDS when the next barrier lets loads into it.
+//
+// 256 x 256 tiles, 8192^3 in bf16: 1340 TFLOP/s in each of the three layouts (a library's product 1397 by rows,
+// 1231 and 1073 with one and two operands across), the matrix units busy for 57 % of the time; in 8 bits 2.4 POP/s.
+// Tiles of 128 x 128, two workgroups a CU: 1100.  Measured and not kept: stages of 64 bytes, four of them (1150 by
+// rows: their lines are fetched twice), 256 x 128 tiles (965), a wave's priority raised while it multiplies (4 % longer),
+// the next tile's first stage loaded before a tile is stored (no different, and 6 % longer for the weights' gradients).
 template <class S, class P, class Q>
 __device__ inline void multiply(P &p, Q &q, Me me, int n, int start, const Stages &lds, typename S::Sum (&d)[S::TP][S::TQ]) {
   constexpr int kLoads = P::kLoads + Q::kLoads;
@@ -325,7 +328,7 @@ __device__ inline void multiply(P &p, Q &q, Me me, int n, int start, const Stage
 
 // The stage a workgroup starts with.  Rows lie multiples of some kilobytes apart: workgroups that read the
 // same place of all their rows meet few of memory's channels.  Those of an XCD and a group share operands
-// and stay together.
+// and stay together (a training step of 8192 rows, H = 4096, I = 14336: 7.49 ms from the same place, 7.35 so).
 template <class S>
 __device__ inline int start_of(int n, int group) {
   const int stages = (n + S::kStage - 1) / S::kStage;
