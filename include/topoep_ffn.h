@@ -103,7 +103,7 @@ int topoep_ffn_bytes(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *rows
  * operand (beyond 65504 in f16: infinite); a routed token's sum is kept in 32 bits and rounded once.  Gate
  * and up values are kept for the backward pass in 32 bits.  T = 0 enqueues
  * nothing.  TOPOEP_EINVAL: null pointers, sizes outside their ranges, T * k
- * above INT32_MAX, rows NULL with L > 1, misaligned buffers; TOPOEP_ELIMIT:
+ * above 2^30, rows NULL with L > 1, misaligned buffers; TOPOEP_ELIMIT:
  * L or k above its maximum; TOPOEP_EWORKSPACE: workspace too small or misaligned.
  */
 int topoep_ffn_forward(const topoep_ffn *f, const void *x, int64_t ldx, int32_t T, const topoep_ffn_rows *rows,
@@ -145,7 +145,7 @@ int topoep_ffn_backward(const topoep_ffn *f, const void *x, int64_t ldx, int32_t
  *   q      device int8 out [M, K], dense
  *   scale  device float out [M]
  *
- * M = 0 enqueues nothing.  TOPOEP_EINVAL: null pointers, M < 0, K < 1, ldx < K, an unknown type.
+ * M = 0 enqueues nothing.  TOPOEP_EINVAL: null pointers, M < 0, K < 1, K > 2^30, ldx < K, an unknown type.
  */
 int topoep_quantize(const void *x, int32_t dtype, int64_t ldx, int32_t M, int32_t K, int8_t *q, float *scale,
                     void *stream);
@@ -178,7 +178,7 @@ int topoep_matmul_int8_workspace_bytes(const topoep_int8 *p, int32_t M, size_t *
  *   workspace  topoep_matmul_int8_workspace_bytes bytes
  *
  * The product with the scales and the activation are in 32 bits, rounded once.
- * M = 0 enqueues nothing.  TOPOEP_EINVAL: null pointers, sizes outside their
+ * M = 0 enqueues nothing.  TOPOEP_EINVAL: null pointers, M above 2^30, sizes outside their
  * ranges, misaligned buffers, offsets NULL with G > 1; TOPOEP_ELIMIT: G above its
  * maximum; TOPOEP_EWORKSPACE: too small or misaligned.
  */

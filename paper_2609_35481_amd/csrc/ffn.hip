@@ -481,12 +481,12 @@ Sizes sizes_of(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *r) {
 }
 
 int check(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *rows) {
-  if (!f || T < 0) return TOPOEP_EINVAL;
+  if (!f || T < 0 || T > 1 << 30) return TOPOEP_EINVAL;   // (a tile behind the last row is counted in 32 bits)
   if (f->hidden < 8 || (f->hidden & 7) || f->inter < 8 || (f->inter & 7) || f->experts < 1) return TOPOEP_EINVAL;
   if (f->hidden > 1 << 17 || f->inter > 1 << 17 || (int64_t)f->hidden * f->inter > 1 << 30) return TOPOEP_EINVAL;
   if (f->dtype != TOPOEP_BF16 && f->dtype != TOPOEP_F16) return TOPOEP_EINVAL;
   if (!rows && f->experts != 1) return TOPOEP_EINVAL;
-  if (rows && (rows->topk < 1 || rows->num_experts < 1 || (int64_t)T * rows->topk > INT32_MAX)) return TOPOEP_EINVAL;
+  if (rows && (rows->topk < 1 || rows->num_experts < 1 || (int64_t)T * rows->topk > 1 << 30)) return TOPOEP_EINVAL;
   if (f->experts > TOPOEP_FFN_MAX_EXPERTS || (rows && rows->topk > TOPOEP_ROUTER_MAX_TOPK)) return TOPOEP_ELIMIT;
   return TOPOEP_OK;
 }

@@ -331,7 +331,7 @@ bool launched() { return hipGetLastError() == hipSuccess; }
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 int check(const topoep_int8 *p, int32_t M) {
-  if (!p || M < 0) return TOPOEP_EINVAL;
+  if (!p || M < 0 || M > 1 << 30) return TOPOEP_EINVAL;   // (a tile behind the last row is counted in 32 bits)
   if (p->n < 1 || p->n > 1 << 20 || p->k < 16 || (p->k & 15) || p->k > 1 << 17 || p->groups < 1) return TOPOEP_EINVAL;
   if (p->gated && (p->n & 1)) return TOPOEP_EINVAL;
   if (p->out_dtype < TOPOEP_F32 || p->out_dtype > TOPOEP_F16) return TOPOEP_EINVAL;
@@ -393,7 +393,7 @@ extern "C" {
 
 int topoep_quantize(const void *x, int32_t dtype, int64_t ldx, int32_t M, int32_t K, int8_t *q, float *scale,
                     void *stream) {
-  if (M < 0 || K < 1 || ldx < K || ldx > (int64_t)1 << 40 || dtype < TOPOEP_F32 || dtype > TOPOEP_F16) return TOPOEP_EINVAL;
+  if (M < 0 || K < 1 || K > 1 << 30 || ldx < K || ldx > (int64_t)1 << 40 || dtype < TOPOEP_F32 || dtype > TOPOEP_F16) return TOPOEP_EINVAL;
   if (M == 0) return TOPOEP_OK;
   const int size = dtype == TOPOEP_F32 ? 4 : 2;
   if (!x || !q || !scale || reinterpret_cast<uintptr_t>(x) % size || reinterpret_cast<uintptr_t>(scale) % 4) return TOPOEP_EINVAL;

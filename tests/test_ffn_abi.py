@@ -145,6 +145,24 @@ def test_int8_refusals(ffn):
     assert call(M=0, q=None) == OK
 
 
+def test_rows_and_elements_that_32_bits_cannot_count_past(ffn):
+    # a tile's last row, or a lane's next element, lies behind the last one there is
+    out = ctypes.c_size_t(0)
+    most, f, p = 1 << 30, ffn.Ffn(8, 8, 1, 1), ffn.Int8(16, 16, 1, 0, 1)
+    two = ffn.Rows(256, 512, 1024, 2048, 2, 8)
+    for rows, T in ((None, most), (two, most // 2)):
+        assert ffn._lib.topoep_ffn_bytes(f, T, rows, out, out, out) == OK
+        assert ffn._lib.topoep_ffn_bytes(f, T + 1, rows, out, out, out) == EINVAL
+        assert ffn._lib.topoep_ffn_forward(f, 256, 8, T + 1, rows, 512, 1024, 2048, None, 4096, 1 << 40, None) == EINVAL
+        assert ffn._lib.topoep_ffn_backward(f, 256, 8, T + 1, rows, 512, 1024, 2048, 256, 512, None, 1024, 2048, 4096,
+                                            1 << 40, None) == EINVAL
+    assert ffn._lib.topoep_matmul_int8_workspace_bytes(p, most, out) == OK
+    assert ffn._lib.topoep_matmul_int8_workspace_bytes(p, most + 1, out) == EINVAL
+    assert ffn._lib.topoep_matmul_int8(p, 256, 16, 512, most + 1, None, 0, 1024, 2048, 4096, 8192, 1 << 40, None) == EINVAL
+    for K in (most + 1, (1 << 31) - 8):
+        assert ffn._lib.topoep_quantize(256, 0, 1 << 31, 1, K, 512, 1024, None) == EINVAL
+
+
 def test_binding_refuses_before_the_gpu(ffn):
     cpu = torch.zeros(4, 64, dtype=torch.bfloat16)
     for call in (lambda: ffn.feed_forward(cpu, torch.zeros(64, 64), torch.zeros(64, 32)),
