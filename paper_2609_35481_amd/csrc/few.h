@@ -34,7 +34,9 @@ struct FewPlace {
 template <class T, int C>
 __device__ inline void few_steps(const char *(&row)[4], const char *(&col)[C], int place, int first, int every, int n,
                                  typename Mul<T>::Sum (&d)[4][C]) {
-  constexpr int U = C == 1 ? 4 : 3;    // steps whose loads are under way together
+  // steps whose loads are under way together, as many as leave few_per_simd its waves (128 experts, four rows on average, H =
+  // 2048, I = 768: 203 us with three for C = 2, 190 so; for C = 4 no different)
+  constexpr int U = C <= 2 ? 4 : 3;
   const v4i zero = {0, 0, 0, 0};
   v4i a[U][4], b[U][C];
   const auto load = [&](int k, bool whole) {

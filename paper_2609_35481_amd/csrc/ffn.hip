@@ -364,7 +364,7 @@ struct Tokens : AcrossPlaces<B, W> {
 // dout[token][r] h[m][c] (Down true).  `parts` workgroups share a group's rows where there are few
 // tiles, each with sums of its own in a.sums.
 //
-// A group's tiles (and parts) go to `xcds` 64Ds, groups in turn: an L2 that has few tiles of every group reads
+// A group's tiles (and parts) go to `xcds` XCDs, groups in turn: an L2 that has few tiles of every group reads
 // most of their operands (10 experts of H = 7168, I = 2048, both gradients: 550 us with eight XCDs each, 520 so).
 template <class S, bool Down, bool Routed>
 __global__ __launch_bounds__(S::kThreads, 2) void grad_kernel(Ffn a, int parts, int xcds) {
@@ -569,7 +569,7 @@ int enqueue_hidden(const Ffn &a, hipStream_t st) {
 
 template <class S, bool Down>
 int enqueue_grad_of(const Ffn &a, int64_t tiles, int parts, hipStream_t st) {
-  // 64Ds of a group: 32 tiles for each, which its CUs take at once; all where there are few groups
+  // XCDs of a group: 32 tiles for each, which its CUs take at once; all where there are few groups
   const int64_t all = tiles / a.L * parts;
   int xcds = 1;
   while (xcds < 8 && (all >= 24 * xcds || a.L * 2 < 8 / xcds * 4)) xcds *= 2;
@@ -601,7 +601,7 @@ bool few_rows(const Ffn &a, int64_t n, int64_t k) {
 }
 
 // Columns for a group's rows at once: groups differ, and twice the mean is what most have at most (128
-// experts, four rows on average: 202 against 225 us with the mean).
+// experts, four rows on average: 190 against 225 us with the mean).
 int64_t few_each(const Ffn &a) {
   const int64_t groups = imin(a.L, (int)a.expected), mean = (a.expected + groups - 1) / groups;
   return groups > 1 ? 2 * mean : mean;
