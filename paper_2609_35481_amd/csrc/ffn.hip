@@ -206,14 +206,24 @@ __global__ __launch_bounds__(64 * few_waves(KS), few_per_simd(C)) void few_down_
   }
 }
 
+// A row's parts, in order, as its pair's gradient; 0 without a row.
+__device__ inline float weight_grad(const Ffn &a, int row, int parts) {
+  float s = 0.0f;
+  if ((unsigned)row < (unsigned)a.rows)
+    for (int p = 0; p < parts; ++p) s += a.part[(int64_t)p * a.rows + row];
+  return s;
+}
+
 // out_t = the sum of its rows of `from`, in the order of its choices (dense: its row), each the sum
-// of its parts.  A workgroup has a token and 1024 columns of it.
+// of its parts.  A workgroup has a token and 1024 columns of it, the first also the token's weights' gradients
+// of `of_weights` parts (0: none; a launch of their own took 4 us).
 template <class T>
-__global__ __launch_bounds__(256) void combine_kernel(Ffn a, const float *from, void *to, int parts) {
+__global__ __launch_bounds__(256) void combine_kernel(Ffn a, const float *from, void *to, int parts, int of_weights) {
   const int c = (blockIdx.y * 256 + threadIdx.x) * 4;
   for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
     int place = -1;
     if (lane_id() < a.k) place = a.pairs ? a.places[t * a.k + lane_id()] : (int)t;
+    if (of_weights && blockIdx.y == 0 && (int)threadIdx.x < a.k) a.dw[t * a.k + threadIdx.x] = weight_grad(a, place, of_weights);
     uint64_t here = __ballot((unsigned)place < (unsigned)a.rows);
     v4f s = {0.0f, 0.0f, 0.0f, 0.0f};
     for (; here != 0; here &= here - 1) {
@@ -317,15 +327,10 @@ __global__ __launch_bounds__(S::kThreads, 2) void hidden_kernel(Ffn a) {
   }
 }
 
-// A row's parts, in order, as its pair's gradient.
+// The weights' gradients where the tokens' are not wanted.
 __global__ __launch_bounds__(256) void weights_kernel(Ffn a, int parts) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)a.T * a.k) return;
-  const int m = a.places[i];
-  float s = 0.0f;
-  if ((unsigned)m < (unsigned)a.rows)
-    for (int p = 0; p < parts; ++p) s += a.part[(int64_t)p * a.rows + m];
-  a.dw[i] = s;
+  if (i < (int64_t)a.T * a.k) a.dw[i] = weight_grad(a, a.places[i], parts);
 }
 
 // An operand across whose rows of the inner axis are tokens', through the pairs.
@@ -539,32 +544,34 @@ int enqueue_out_of(const Ffn &a, void *to, int parts, hipStream_t st) {
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 template <class T>
-int enqueue_combine(const Ffn &a, void *to, int parts, hipStream_t st) {
-  hipLaunchKernelGGL((combine_kernel<T>), dim3(imin(a.T, 1 << 20), (a.H + 1023) / 1024), dim3(256), 0, st, a, a.y, to, parts);
+int enqueue_combine(const Ffn &a, void *to, int parts, int of_weights, hipStream_t st) {
+  hipLaunchKernelGGL((combine_kernel<T>), dim3(imin(a.T, 1 << 20), (a.H + 1023) / 1024), dim3(256), 0, st, a, a.y, to, parts, of_weights);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 template <class T, bool Back>
-int enqueue_out(const Ffn &a, void *to, int parts, hipStream_t st) {
+int enqueue_out(const Ffn &a, void *to, int parts, int of_weights, hipStream_t st) {
   void *const product = a.pairs || parts > 1 ? static_cast<void *>(a.y) : to;
   const int rc = parts == 1 && large_rows(a, a.H, 256) ? enqueue_out_of<Large<T, Back>, Back>(a, product, 1, st)
                                                        : enqueue_out_of<Small<T, Back>, Back>(a, product, parts, st);
-  return rc != TOPOEP_OK || product == to ? rc : enqueue_combine<T>(a, to, parts, st);
+  return rc != TOPOEP_OK || product == to ? rc : enqueue_combine<T>(a, to, parts, of_weights, st);
 }
 
 template <class S>
-int enqueue_hidden_of(const Ffn &a, hipStream_t st) {
+int enqueue_hidden_of(const Ffn &a, int *of_weights, hipStream_t st) {
   const int parts = (a.I + S::BP - 1) / S::BP;
+  *of_weights = a.dw ? parts : 0;
   const int64_t tiles = most_spans<S::BQ>(a.offsets, a.rows, a.L) * parts;
   hipLaunchKernelGGL((hidden_kernel<S>), dim3(grid_of<S>(tiles)), dim3(S::kThreads), 0, st, a);
   if (!launched()) return TOPOEP_EHIP;
-  if (!a.dw) return TOPOEP_OK;
+  if (!a.dw || a.dx) return TOPOEP_OK;   // (combine_kernel sums them)
   hipLaunchKernelGGL(weights_kernel, dim3((unsigned)((a.rows + (int64_t)255) / 256)), dim3(256), 0, st, a, parts);
   return launched() ? TOPOEP_OK : TOPOEP_EHIP;
 }
 template <class T>
-int enqueue_hidden(const Ffn &a, hipStream_t st) {
+int enqueue_hidden(const Ffn &a, int *of_weights, hipStream_t st) {
   static_assert(Small<T, true>::BP >= kPartUnits, "parts of the weights' gradient");
-  return large_rows(a, a.I, 256) ? enqueue_hidden_of<Large<T, true>>(a, st) : enqueue_hidden_of<Small<T, true>>(a, st);
+  return large_rows(a, a.I, 256) ? enqueue_hidden_of<Large<T, true>>(a, of_weights, st)
+                                 : enqueue_hidden_of<Small<T, true>>(a, of_weights, st);
 }
 
 template <class S, bool Down>
@@ -627,21 +634,21 @@ int enqueue_few_down(const Ffn &a, hipStream_t st) {
     hipLaunchKernelGGL((few_down_kernel<T, C, KS>), grid, block, 0, st, a, a.pairs ? static_cast<void *>(a.y) : a.out);
   });
   if (!launched()) return TOPOEP_EHIP;
-  return a.pairs ? enqueue_combine<T>(a, a.out, 1, st) : TOPOEP_OK;
+  return a.pairs ? enqueue_combine<T>(a, a.out, 1, 0, st) : TOPOEP_OK;
 }
 
 template <class T>
 int forward(const Ffn &a, int parts, hipStream_t st) {
   const int rc = few_rows(a, 2 * a.I, a.H) ? enqueue_few_up<T>(a, st) : enqueue_up<T>(a, st);
   if (rc != TOPOEP_OK) return rc;
-  return few_rows(a, a.H, a.I) ? enqueue_few_down<T>(a, st) : enqueue_out<T, false>(a, a.out, parts, st);
+  return few_rows(a, a.H, a.I) ? enqueue_few_down<T>(a, st) : enqueue_out<T, false>(a, a.out, parts, 0, st);
 }
 
 template <class T>
 int backward(const Ffn &a, int parts, int up_parts, int down_parts, hipStream_t st) {
-  int rc = TOPOEP_OK;
-  if (a.rows > 0 && (a.dx || a.dw || a.dup)) rc = enqueue_hidden<T>(a, st);
-  if (rc == TOPOEP_OK && a.rows > 0 && a.dx) rc = enqueue_out<T, true>(a, a.dx, parts, st);
+  int rc = TOPOEP_OK, of_weights = 0;
+  if (a.rows > 0 && (a.dx || a.dw || a.dup)) rc = enqueue_hidden<T>(a, &of_weights, st);
+  if (rc == TOPOEP_OK && a.rows > 0 && a.dx) rc = enqueue_out<T, true>(a, a.dx, parts, of_weights, st);
   if (rc == TOPOEP_OK && a.dup) rc = enqueue_grad<T, false>(a, up_parts, st);
   if (rc == TOPOEP_OK && a.ddown) rc = enqueue_grad<T, true>(a, down_parts, st);
   return rc;
