@@ -119,11 +119,11 @@ struct Block {
   int32_t T;
   int64_t ldx;
   size_t forward, saved, backward;
-  Block(const Tensor &x, const Tensor &weights, const Tensor &up, const Tensor &down, const Rows &by, int64_t E) {
+  Block(const Tensor &x, int64_t stride, const Tensor &weights, const Tensor &up, const Tensor &down, const Rows &by, int64_t E) {
     const bool routed = weights.defined();
     f = topoep_ffn{fits(down.size(-2)), fits(down.size(-1)), routed ? fits(up.size(0)) : 1, dtype_of(x)};
     T = fits(x.size(0));
-    ldx = stride_of(x, "x");
+    ldx = stride;
     rows = routed ? &r : nullptr;
     if (routed)
       r = topoep_ffn_rows{by.offsets.data_ptr<int32_t>(), by.pairs.data_ptr<int32_t>(), by.places.data_ptr<int32_t>(),
@@ -134,7 +134,7 @@ struct Block {
 
 Tensor forward(const Tensor &x, const Tensor &weights, const Tensor &up, const Tensor &down, const Rows &by, int64_t E,
                Tensor *saved, void *stream) {
-  const Block b(x, weights, up, down, by, E);
+  const Block b(x, stride_of(x, "x"), weights, up, down, by, E);
   Tensor out = at::empty(x.sizes(), x.options());
   if (saved) *saved = scratch(b.saved, x);
   const Tensor ws = scratch(b.forward, x);
@@ -143,28 +143,67 @@ Tensor forward(const Tensor &x, const Tensor &weights, const Tensor &up, const T
   return out;
 }
 
+// What a hook on saved tensors gave back for one of them.  It keeps the value, shape and type of what was saved, and the
+// GPU, but not its layout; the kernels read dense tensors at multiples of 16 bytes.  (No Python here: a backward pass does
+// not hold its lock.)
+void is_alike(const Tensor &t, const char *name, at::ScalarType type, const Tensor &like, at::IntArrayRef shape) {
+  TORCH_CHECK(t.defined() && t.layout() == at::kStrided && t.scalar_type() == type && t.device() == like.device() &&
+                  t.sizes().equals(shape),
+              "a hook on saved tensors gave back another ", name, " than was saved: it has to be ", type, " of shape ", shape, " on ", like.device());
+}
+bool aligned(const Tensor &t) { return reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0; }
+Tensor at_16(const Tensor &t) { return aligned(t) ? t : t.clone(); }
+Tensor given_back(const Tensor &t, const char *name, at::ScalarType type, const Tensor &like, at::IntArrayRef shape) {
+  is_alike(t, name, type, like, shape);
+  return at_16(t.contiguous());
+}
+
 struct FeedForward : torch::autograd::Function<FeedForward> {
   static Tensor forward(AutogradContext *ctx, const Tensor &x, const std::optional<Tensor> &routers, const Tensor &up,
                         const Tensor &down, const Rows &by, int64_t E, int64_t stream) {
     const Tensor weights = routers.value_or(Tensor());
     Tensor saved;
     const Tensor out = ::forward(x, weights, up, down, by, E, &saved, reinterpret_cast<void *>(stream));
-    ctx->save_for_backward({x, weights, up, down, saved, by.offsets, by.pairs, by.places});
+    ctx->save_for_backward({x, weights, up, down, saved});
     ctx->saved_data["E"] = E;
+    ctx->saved_data["I"] = down.size(-1);
+    if (weights.defined()) {   // out of a hook's reach: kernels read at what these name
+      ctx->saved_data["offsets"] = by.offsets;
+      ctx->saved_data["pairs"] = by.pairs;
+      ctx->saved_data["places"] = by.places;
+    }
     return out;
   }
   static variable_list backward(AutogradContext *ctx, variable_list grads) {
     const variable_list s = ctx->get_saved_variables();
-    const Tensor &x = s[0], &weights = s[1], &up = s[2], &down = s[3];
-    const Rows by{s[5], s[6], s[7]};
     variable_list out(7);
     int rc = TOPOEP_OK;
     {
       at::AutoGradMode off(false);
-      Tensor grad = grads[0].contiguous();
-      if (reinterpret_cast<uintptr_t>(grad.data_ptr()) % 16) grad = grad.clone();
+      const Tensor grad = at_16(grads[0].contiguous());   // [T, H]: autograd sees to that
+      const bool routed = ctx->saved_data.count("offsets") > 0;
+      const at::ScalarType type = grad.scalar_type();
+      const int64_t T = grad.size(0), H = grad.size(1);
+      Tensor weights;
+      Rows by;
+      std::vector<int64_t> shape;                         // of the experts, if there are any
+      if (routed) {
+        by = Rows{ctx->saved_data["offsets"].toTensor(), ctx->saved_data["pairs"].toTensor(), ctx->saved_data["places"].toTensor()};
+        weights = given_back(s[1], "weights", at::kFloat, grad, by.places.sizes());
+        shape.push_back(by.offsets.size(0) - 1);
+      }
+      const int64_t I = ctx->saved_data["I"].toInt();
+      const size_t n = shape.size();
+      shape.insert(shape.end(), {2 * I, H});
+      const Tensor up = given_back(s[2], "up", type, grad, shape);
+      shape[n] = H, shape[n + 1] = I;
+      const Tensor down = given_back(s[3], "down", type, grad, shape);
+      is_alike(s[0], "x", type, grad, {T, H});
+      const bool rows = s[0].stride(1) == 1 && (T < 2 || (s[0].stride(0) >= H && s[0].stride(0) % 8 == 0)) && aligned(s[0]);
+      const Tensor x = rows ? s[0] : at_16(s[0].contiguous());
       try {
-        const Block b(x, weights, up, down, by, ctx->saved_data["E"].toInt());
+        const Block b(x, T > 1 ? x.stride(0) : H, weights, up, down, by, ctx->saved_data["E"].toInt());
+        const Tensor saved = given_back(s[4], "block's values", at::kByte, grad, {(int64_t)(b.saved ? b.saved : 1)});
         size_t edge = 0;
         const Tensor *like[] = {&x, &weights, &up, &down};
         for (int i = 0; i < 4; ++i) {
@@ -173,7 +212,7 @@ struct FeedForward : torch::autograd::Function<FeedForward> {
         }
         const Tensor ws = scratch(b.backward, x);
         void *stream = c10::hip::getCurrentHIPStreamMasqueradingAsCUDA(x.get_device()).stream();
-        rc = entry.backward(&b.f, x.data_ptr(), b.ldx, b.T, b.rows, up.data_ptr(), down.data_ptr(), s[4].data_ptr(),
+        rc = entry.backward(&b.f, x.data_ptr(), b.ldx, b.T, b.rows, up.data_ptr(), down.data_ptr(), saved.data_ptr(),
                             grad.data_ptr(), at_of(out[0]), static_cast<float *>(at_of(out[1])), at_of(out[2]),
                             at_of(out[3]), ws.data_ptr(), (size_t)ws.numel(), stream);
       } catch (const Code &c) {
