@@ -152,7 +152,7 @@ int topoep_quantize(const void *x, int32_t dtype, int64_t ldx, int32_t M, int32_
 
 typedef struct topoep_int8 {
   int32_t n;         /* N, rows (channels) of a weight matrix, 1 .. 2^20; even where gated */
-  int32_t k;         /* K, a multiple of 16, at most 2^17 (sums fit 32 bits)         */
+  int32_t k;         /* K, a multiple of 16, at most 2^17 (sums are at most 2^31)    */
   int32_t groups;    /* G weight matrices, 1 .. TOPOEP_FFN_MAX_EXPERTS               */
   int32_t gated;     /* nonzero: out = silu(a[0:N/2]) * a[N/2:N]                     */
   int32_t out_dtype;
@@ -177,7 +177,8 @@ int topoep_matmul_int8_workspace_bytes(const topoep_int8 *p, int32_t M, size_t *
  *   out      device out [M, N] (gated: [M, N / 2]) of out_dtype, dense
  *   workspace  topoep_matmul_int8_workspace_bytes bytes
  *
- * The product with the scales and the activation are in 32 bits, rounded once.
+ * Any of the 256 values may be in q and w.  The product with the scales and the
+ * activation are in 32 bits, rounded once.
  * M = 0 enqueues nothing.  TOPOEP_EINVAL: null pointers, M above 2^30, sizes outside their
  * ranges, misaligned buffers, offsets NULL with G > 1; TOPOEP_ELIMIT: G above its
  * maximum; TOPOEP_EWORKSPACE: too small or misaligned.

@@ -81,9 +81,12 @@ __device__ inline float quad_sum(float v) {
   v += dpp_movf<0xB1>(v);
   return v + dpp_movf<0x4E>(v);
 }
+// (whole numbers wrap round: of 2^31 its 32 bits are kept)
+__device__ inline float plus(float a, float b) { return a + b; }
+__device__ inline int plus(int a, int b) { return (int)((uint32_t)a + (uint32_t)b); }
 __device__ inline int quad_sum(int v) {
-  v += (int)dpp_mov<0xB1>((uint32_t)v);
-  return v + (int)dpp_mov<0x4E>((uint32_t)v);
+  v = plus(v, (int)dpp_mov<0xB1>((uint32_t)v));
+  return plus(v, (int)dpp_mov<0x4E>((uint32_t)v));
 }
 
 // LDS of a workgroup: each wave's sums, [row][column].
@@ -124,7 +127,7 @@ __device__ inline void few_product(const FR &row_at, const FC &col_at, int count
   const auto sum = [&](int r, int c) {
     E v = lds.at[KS == 1 ? wave : 0][r][c];
 #pragma unroll
-    for (int w = 1; w < KS; ++w) v += lds.at[w][r][c];
+    for (int w = 1; w < KS; ++w) v = plus(v, lds.at[w][r][c]);
     return v;
   };
   for (int i = KS == 1 ? lane : (int)threadIdx.x; i < rows * count; i += KS == 1 ? 64 : 64 * KS) {

@@ -169,6 +169,10 @@ __device__ inline void store1(void *out, int type, int64_t at, float v) {
   else static_cast<F16 *>(out)[at] = from_float<F16>(v);
 }
 
+// A sum as a float.  2^31, which 2^17 products of -128 and -128 reach and nothing else does, is in 32 bits -2^31, which
+// no sum is: the least is -127 * 128 * 2^17.
+__device__ inline float of_sum(int s) { return s == INT32_MIN ? 0x1p31f : (float)s; }
+
 // Four neighbours of a row of `n`, from column c on.
 __device__ inline void store_row(void *out, int type, int64_t row, int n, int c, v4f v) {
   const int64_t at = row * n + c;
@@ -249,9 +253,9 @@ __global__ __launch_bounds__(S::kThreads, 2) void int8_kernel(Int8 a) {
         v4f v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          v[e] = (float)d[i][j][e] * scale * w0[e];
+          v[e] = of_sum(d[i][j][e]) * scale * w0[e];
           if (Gated) {
-            const float u = (float)d[i + kTiles * (Gated ? 1 : 0)][j][e] * scale * w1[e];
+            const float u = of_sum(d[i + kTiles * (Gated ? 1 : 0)][j][e]) * scale * w1[e];
             v[e] = v[e] * sigmoid(v[e]) * u;
           }
         }
@@ -281,11 +285,12 @@ __global__ __launch_bounds__(256) void parts_kernel(Int8 a) {
   const float scale = a.scale[m], *ws = a.ws + (int64_t)group * a.N;
   for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < a.No; c += gridDim.y * 1024) {
     const auto sum = [&](int at) {
-      v4i s = *reinterpret_cast<const v4i *>(a.sums + (int64_t)m * a.N + at);
-      for (int p = 1; p < a.parts; ++p) s += *reinterpret_cast<const v4i *>(a.sums + ((int64_t)p * a.M + m) * a.N + at);
+      typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+      v4u s = *reinterpret_cast<const v4u *>(a.sums + (int64_t)m * a.N + at);
+      for (int p = 1; p < a.parts; ++p) s += *reinterpret_cast<const v4u *>(a.sums + ((int64_t)p * a.M + m) * a.N + at);
       v4f v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = (float)s[e] * scale * ws[at + e];
+      for (int e = 0; e < 4; ++e) v[e] = of_sum((int)s[e]) * scale * ws[at + e];
       return v;
     };
     v4f v = sum(c);
@@ -318,8 +323,8 @@ __global__ __launch_bounds__(64 * few_waves(KS), few_per_simd(C)) void few_int8_
           if (c0 + r >= a.No) return;
           const float *ws = a.ws + (int64_t)s.group * a.N + c0 + r;
           const float scale = a.scale[s.first + c];
-          float v = (float)first * scale * ws[0];
-          if (Gated) v = v * sigmoid(v) * ((float)second * scale * ws[a.No]);
+          float v = of_sum(first) * scale * ws[0];
+          if (Gated) v = v * sigmoid(v) * (of_sum(second) * scale * ws[a.No]);
           store1(a.out, a.type, (int64_t)(s.first + c) * a.No + c0 + r, v);
         });
   }
