@@ -614,12 +614,25 @@ int64_t few_each(const Ffn &a) {
   return groups > 1 ? 2 * mean : mean;
 }
 
+// Grid of the tiles of a few rows, np of the weights' each.  Of T k rows that could be here about T k L / E are, and a
+// workgroup without a tile starts, counts the groups and ends all the same: tiles are those of twice
+// the expected rows, or as many as fill the chip, and more rows than that take turns (512 tokens, eight of 256 experts each, one
+// of which is here, H = I = 4096: 660 us with all that could be, 354 so; eight here, H = 7168, I = 2048: 242 and 236).
+template <int C, int KS>
+dim3 few_blocks(const Ffn &a, int64_t np) {
+  constexpr int64_t kFill = KS == 1 ? 4096 : 1024;
+  const int64_t rows = a.expected * 2 < a.rows ? a.expected * 2 : a.rows;
+  const int64_t most = most_spans<4 * C>(a.offsets, a.rows, a.L) * np, likely = most_spans<4 * C>(a.offsets, (int)rows, a.L) * np;
+  const int64_t tiles = likely > kFill ? likely : kFill;
+  return few_grid<KS>(tiles < most ? tiles : most);
+}
+
 template <class T>
 int enqueue_few_up(const Ffn &a, hipStream_t st) {
   const int64_t groups = imin(a.L, (int)a.expected), nu = (a.I + 7) / 8;
   few_shape(few_each(a), groups * nu, [&](auto c, auto ks) {
     constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
-    const dim3 grid = few_grid<KS>(most_spans<4 * C>(a.offsets, a.rows, a.L) * nu), block(64 * few_waves(KS));
+    const dim3 grid = few_blocks<C, KS>(a, nu), block(64 * few_waves(KS));
     if (a.gu) hipLaunchKernelGGL((few_up_kernel<T, true, C, KS>), grid, block, 0, st, a);
     else hipLaunchKernelGGL((few_up_kernel<T, false, C, KS>), grid, block, 0, st, a);
   });
@@ -630,7 +643,7 @@ int enqueue_few_down(const Ffn &a, hipStream_t st) {
   const int64_t groups = imin(a.L, (int)a.expected), nh = (a.H + kFewRows - 1) / kFewRows;
   few_shape(few_each(a), groups * nh, [&](auto c, auto ks) {
     constexpr int C = decltype(c)::value, KS = decltype(ks)::value;
-    const dim3 grid = few_grid<KS>(most_spans<4 * C>(a.offsets, a.rows, a.L) * nh), block(64 * few_waves(KS));
+    const dim3 grid = few_blocks<C, KS>(a, nh), block(64 * few_waves(KS));
     hipLaunchKernelGGL((few_down_kernel<T, C, KS>), grid, block, 0, st, a, a.pairs ? static_cast<void *>(a.y) : a.out);
   });
   if (!launched()) return TOPOEP_EHIP;
