@@ -75,9 +75,10 @@ typedef struct topoep_ffn_rows {
 } topoep_ffn_rows;
 
 /*
- * Bytes of a forward pass's workspace, of what it keeps for a backward pass
+ * Bytes of a forward pass's workspace (the same with saved and without), of what it keeps for a backward pass
  * (saved), and of the backward pass's workspace, for T tokens; rows: whether
- * the layer is a routed one, and its k and E (these alone are read).  NULL outputs are not written.
+ * the layer is a routed one, and its k and E (these alone are read).  All three hold T k rows, however many
+ * of them have their expert here.  NULL outputs are not written.
  */
 int topoep_ffn_bytes(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *rows, size_t *forward, size_t *saved,
                      size_t *backward);
@@ -100,7 +101,8 @@ int topoep_ffn_bytes(const topoep_ffn *f, int32_t T, const topoep_ffn_rows *rows
  *
  * Products are accumulated in 32 bits.  The hidden values, times their row's
  * weight, are rounded once to the weights' type, the second product's
- * operand (beyond 65504 in f16: infinite); a routed token's sum is kept in 32 bits and rounded once.  Gate
+ * operand (f16: beyond 65504 infinite, below 2^-14 to multiples of 2^-24, so that a small weight costs
+ * bits); a routed token's sum is kept in 32 bits and rounded once.  Gate
  * and up values are kept for the backward pass in 32 bits.  T = 0 enqueues
  * nothing.  TOPOEP_EINVAL: null pointers, sizes outside their ranges, T * k
  * above 2^30, rows NULL with L > 1, misaligned buffers; TOPOEP_ELIMIT:

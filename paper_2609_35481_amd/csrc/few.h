@@ -142,8 +142,8 @@ template <int KS> __device__ inline int few_first() {
 }
 template <int KS> __device__ inline int few_next() { return (int)gridDim.x * (KS == 1 ? few_waves(1) : 1); }
 
-// Calls f<C, KS> for about `rows` rows a group and `tiles` tiles in all (of 16 rows of weights, n bytes):
-// waves of their own where there are enough of them and a wave's loads are many.
+// Calls f<C, KS> for about `rows` rows a group and `tiles` tiles in all (of 16 rows of weights): a wave has
+// a tile of its own where there are enough of them, whatever the length of the inner axis.
 template <class F>
 inline void few_shape(int64_t rows, int64_t tiles, const F &f) {
   const auto by_ks = [&](auto c) {

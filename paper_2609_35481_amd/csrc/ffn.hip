@@ -600,7 +600,8 @@ int enqueue_grad(const Ffn &a, int parts, hipStream_t st) {
 
 // A few rows a group, 16 and fewer: the weights' bytes count, not the tiles.  Up to 64 also where a product
 // of `n` rows of weights is small (rows times weights of 512 MiB: 32 rows, H = I = 2048, both products:
-// 17.8 against 30.2 us; I = 5632: 41.4 and 38.7).
+// 17.8 against 30.2 us; I = 5632: 41.4 and 38.7).  The mean decides: a group far above it reads its weights once for
+// every 4 C rows that it has.
 bool few_rows(const Ffn &a, int64_t n, int64_t k) {
   const int64_t groups = imin(a.L, (int)a.expected);
   if ((double)a.rows * n >= 0x1p34) return false;   // (its tiles are numbered in 32 bits)

@@ -143,7 +143,8 @@ inline int64_t likely_spans(bool by_groups, int64_t expected, int groups, int B)
 }
 
 // Whether tiles of 256 x 256 take less time than their number of 128 x 128: one of the former a CU,
-// two of the latter, which reach 1340 and 1100 TFLOP/s (8192^3 in bf16).
+// two of the latter, which reach 1340 and 1100 TFLOP/s (8192^3 in bf16: an inner axis of 128 stages, and the rule
+// takes these rates for short ones too).
 inline bool large_tiles(int64_t large, int64_t small) { return (large + 255) / 256 * 10 < (small + 511) / 512 * 6; }
 
 inline int64_t ceil_of(int64_t a, int64_t b) { return (a + b - 1) / b; }

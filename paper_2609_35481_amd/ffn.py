@@ -9,6 +9,8 @@
 
 A backward pass is captured into a graph as any other of torch's: with no eager
 graph of the same leaves alive, whose accumulators would run on the stream that made them.
+What it was given may come through hooks on saved tensors (from the host, computed again), in any
+layout; another shape, type or device than was saved is a RuntimeError.
 
 Argument checks and marshalling only: torch provides device memory and the
 current stream, every step runs in the HIP kernels of libtopoep.so.  Importing
@@ -107,7 +109,8 @@ def experts(x, ids, weights, up, down, expert_slot=None, stream=None):
     times the block of that expert, up [L, 2I, H] and down [L, H, I], bfloat16 or
     float16.  expert_slot int32 [E] says where an expert lies among the L here
     (-1: elsewhere; it adds nothing); None: expert e at slot e.  Differentiable in x,
-    weights, up and down; for the backward pass it keeps 10 I bytes for each of T k rows."""
+    weights, up and down; for the backward pass it keeps 10 I bytes for each of T k rows, whether
+their experts are here or not."""
     if stream is not None:
         return _on_stream(stream, experts, x, ids, weights, up, down, expert_slot)
     if ids is None:
@@ -126,7 +129,7 @@ def quantize(x, stream=None):
 
 def matmul_int8(x, w, w_scale, offsets=None, gated=False, dtype=None, out=None, stream=None):
     """Enqueue topoep_matmul_int8: the rows x [M, K] times the weights w int8 [N,
-    K] with the scales w_scale float32 [N] of its rows, as quantize makes them.
+    K] with the scales w_scale float32 [N] of its rows, as quantize makes them.  K is a multiple of 16, at most 2^17.
 
     x        float32, bfloat16 or float16, which is quantised row by row first, or what
              quantize returned for it: (q, scale)
